@@ -306,6 +306,81 @@ gkv_status gkv_evict_static(gkv_ctx* ctx, const void* qwin, void* K, void* V, fl
                             int32_t* d_state, int32_t step, int32_t len_max_host,
                             void* workspace, void* stream);
 
+/*
+ * ---- Cache in 8 bits ------------------------------------------------------------------------
+ * K and V of the cache held in 8 bits an element, half of bf16's memory and of what a decode step reads.  An element is an
+ * e4m3 code (1-4-3 bits, no infinity, NaN 0x7f and 0xff) times its row's scale, a power of two:
+ *     e = min { e >= -126 : max |x| <= 448 * 2^e } over the row's finite elements (0 if they are all zero),
+ *     code = x * 2^-e rounded to the nearest e4m3 number, ties to even;  value = code * 2^e.
+ * So an element is at most 2^-4 of its value off, or 2^-10 * 2^e where it is below 2^-6 * 2^e.  What is not finite is held
+ * as NaN.
+ *   K8, V8  [L,B,h_kv,capacity,d] codes.  The layout is that of the other caches with elements of one byte: rows of K
+ *           below N_TILED in tiled format with E = 16, the others and V row-major.
+ *   scales  [L,B,h_kv,capacity,2] bfloat16: the scales 2^e of a row of K and of the same row of V.
+ * q, k_new, v_new, qwin and out are of config.dtype as before, d_state, pos, F_hist and the workspace are the same, and
+ * so are the rules for steps, lengths and no-ops.  head_dim has to be a multiple of 16 (else GKV_ERR_SHAPE).  K8, V8, scales
+ * and the rows of gkv_q8_store_prompt and gkv_q8_read have to be 16-byte aligned (else GKV_ERR_INVALID_ARG).
+ * gkv_global_update, gkv_select_topk, gkv_pool_scores and gkv_evicted_positions do not look at K or V and serve such a cache
+ * as they are; for gkv_redundancy_combine read K back first.
+ *
+ * gkv_q8_store_prompt: prompt rows into the cache.  k, v [n,L,B,h_kv,d] hold the positions t_first .. t_first + n - 1 of
+ * every sequence's token stream; sequence i's prompt is the positions [t0 - P_i, t0) with P_i = d_prompt_len[i] (device,
+ * int32 [B]) and goes to rows [0, P_i), row-major, with pos their positions.  May be called chunk by chunk.  Rows that
+ * would lie at or beyond the capacity are left out; all other rows stay as they are.  The records are the caller's to set, to
+ * {P_i, t0, 0, 0}.
+ */
+gkv_status gkv_q8_store_prompt(gkv_ctx* ctx, const void* k, const void* v, int32_t n, int32_t t_first, int32_t t0,
+                               const int32_t* d_prompt_len, void* K8, void* V8, void* scales, int32_t* pos,
+                               void* stream);
+
+/* The values of the rows below the length before decode step `step`, as a cache of config.dtype (which holds them exactly,
+ * but for magnitudes below 2^-126 in bf16, and of 2^128, what 1.9375 * 2^127 and more is rounded to) in the layout that d_state
+ * describes: the other calls take it with the same d_state.  K, V [L,B,h_kv,capacity,d]; either may be NULL, and its codes then too.  Other rows stay as they are. */
+gkv_status gkv_q8_read(gkv_ctx* ctx, const void* K8, const void* V8, const void* scales, const int32_t* d_state,
+                       int32_t step, void* K, void* V, void* stream);
+
+/* gkv_attend_decode on such a cache.  The new row is attended to as it is held: as its codes.
+ * part: as gkv_attend_decode_prefix takes it, or NULL. */
+gkv_status gkv_q8_attend_decode(gkv_ctx* ctx, const void* q, const void* k_new, const void* v_new,
+                                void* K8, void* V8, void* scales, int32_t* pos, int32_t step, void* qwin,
+                                const int32_t* d_state, int32_t len_max_host, const void* part, void* out,
+                                void* workspace, void* stream);
+
+/* gkv_score_window, gkv_compact and gkv_evict on such a cache. */
+gkv_status gkv_q8_score_window(gkv_ctx* ctx, const void* qwin, const void* K8, const void* scales,
+                               const int32_t* d_state, int32_t step, int32_t len_max_host, float* S,
+                               void* workspace, void* stream);
+gkv_status gkv_q8_compact(gkv_ctx* ctx, const int32_t* keep_idx, const float* F, void* K8, void* V8, void* scales,
+                          float* F_hist, int32_t* pos, int32_t* d_state, int32_t step, void* workspace, void* stream);
+gkv_status gkv_q8_evict(gkv_ctx* ctx, const void* qwin, void* K8, void* V8, void* scales, float* F_hist, int32_t* pos,
+                        int32_t* d_state, int32_t step, int32_t len_max_host,
+                        float* S, float* F, int32_t* keep_idx, void* workspace, void* stream);
+
+/*
+ * ---- Prefix that sequences share ----------------------------------------------------------------
+ * Answers to one prompt share its keys and values: they are held once, Kp, Vp [L,h_kv,prefix_capacity,d] of config.dtype, both
+ * row-major, and attended to once for all of them.  A decode step is then
+ *   gkv_prefix_attend          the newest queries of `count` sequences, from `first` on, over the prefix's `rows` rows;
+ *   gkv_attend_decode_prefix   gkv_attend_decode whose out is the softmax over the prefix and the sequence's own rows
+ *                              together (or gkv_q8_attend_decode with the same `part`).
+ * The prefix is not part of the sequences' caches: it has no positions there, does not count to the budget, is never
+ * evicted, and the local score stays a softmax over the sequence's own rows.
+ * part: device memory of at least gkv_prefix_bytes(rows) bytes, 16-byte aligned, zeroed once by the caller.  gkv_prefix_attend
+ * leaves there, for each query head of its sequences, sum, maximum and weighted values, in 32 bits; those of other sequences stay as
+ * they are, so a batch of several prompts takes one call for each of them (on one stream, or ordered by events), and a sequence
+ * that has none a part that still is zero.  Results stay until they are written again: call it in every step.
+ * rows may be 0 (Kp and Vp are not looked at then).  A call with more rows than the context's gkv_prefix_bytes calls were asked for
+ * returns GKV_ERR_WORKSPACE.  Both calls can be recorded; the rows are frozen then.  head_dim has to be a multiple of 4.
+ * The result is the same to the last bit for the same rows, first, count and alignment of the arguments.
+ */
+gkv_status gkv_prefix_bytes(gkv_ctx* ctx, int32_t rows, size_t* out_bytes);
+gkv_status gkv_prefix_attend(gkv_ctx* ctx, const void* q, const void* Kp, const void* Vp, int32_t rows,
+                             int32_t prefix_capacity, int32_t first, int32_t count, void* part, void* stream);
+gkv_status gkv_attend_decode_prefix(gkv_ctx* ctx, const void* q, const void* k_new, const void* v_new,
+                                    void* K, void* V, int32_t* pos, int32_t step, void* qwin,
+                                    const int32_t* d_state, int32_t len_max_host, const void* part, void* out,
+                                    void* workspace, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

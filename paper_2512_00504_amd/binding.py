@@ -29,6 +29,8 @@ EXPORTS = [
     "gkv_global_update", "gkv_select_topk", "gkv_compact", "gkv_evict", "gkv_profile_enable",
     "gkv_profile_read", "gkv_profile_reset", "gkv_probe_attend_read", "gkv_redundancy_combine", "gkv_evicted_positions", "gkv_pool_scores",
     "gkv_evict_static", "gkv_set_step_base", "gkv_advance_step_base",
+    "gkv_q8_store_prompt", "gkv_q8_read", "gkv_q8_attend_decode", "gkv_q8_score_window", "gkv_q8_compact", "gkv_q8_evict",
+    "gkv_prefix_bytes", "gkv_prefix_attend", "gkv_attend_decode_prefix",
 ]
 
 
@@ -80,6 +82,15 @@ def load_library():
     lib.gkv_redundancy_combine.argtypes = [vp, vp, vp, i32, i32, vp, c_float, c_float, c_float, i32, vp, vp, vp, vp]
     lib.gkv_pool_scores.argtypes = [vp, vp, vp, i32, i32, vp, vp]
     lib.gkv_evicted_positions.argtypes = [vp, vp, vp, vp, i32, vp, vp]
+    lib.gkv_q8_store_prompt.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.gkv_q8_read.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    lib.gkv_q8_attend_decode.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp]
+    lib.gkv_q8_score_window.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.gkv_q8_compact.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp]
+    lib.gkv_q8_evict.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+    lib.gkv_prefix_bytes.argtypes = [vp, i32, POINTER(c_size_t)]
+    lib.gkv_prefix_attend.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, vp]
+    lib.gkv_attend_decode_prefix.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp]
     lib.gkv_profile_enable.argtypes = [vp, i32]
     lib.gkv_profile_read.argtypes = [vp, i32, POINTER(c_double), POINTER(c_int64)]
     lib.gkv_profile_reset.argtypes = [vp]
@@ -267,6 +278,72 @@ class Context:
                                                 _ptr(evicted), _stream())
         if st:
             raise GkvError(st, "gkv_evicted_positions")
+
+    # cache in 8 bits: K8, V8 torch.float8_e4m3fn [L,B,h_kv,capacity,d], scales bfloat16 [L,B,h_kv,capacity,2]
+    def q8_store_prompt(self, k, v, n, t_first, t0, d_prompt_len, K8, V8, scales, pos):
+        self._check(self.lib.gkv_q8_store_prompt(self.h, _ptr(k), _ptr(v), n, t_first, t0, _ptr(d_prompt_len), _ptr(K8),
+                                                 _ptr(V8), _ptr(scales), _ptr(pos), _stream()), "gkv_q8_store_prompt")
+
+    def q8_read(self, K8, V8, scales, d_state, step, K, V):
+        self._check(self.lib.gkv_q8_read(self.h, _ptr(K8), _ptr(V8), _ptr(scales), _ptr(d_state), step, _ptr(K), _ptr(V),
+                                         _stream()), "gkv_q8_read")
+
+    def q8_attend_decode(self, q, k_new, v_new, K8, V8, scales, pos, step, qwin, d_state, len_max_host, part, out, workspace):
+        st = self._call.gkv_q8_attend_decode(self._handle, q, k_new, v_new, K8, V8, scales, pos, step, qwin, d_state, len_max_host, part, out, workspace)
+        if st is None:
+            st = self.lib.gkv_q8_attend_decode(self.h, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(K8), _ptr(V8), _ptr(scales),
+                                               _ptr(pos), step, _ptr(qwin), _ptr(d_state), len_max_host, _ptr(part),
+                                               _ptr(out), _ptr(workspace), _stream())
+        if st:
+            raise GkvError(st, "gkv_q8_attend_decode")
+
+    def q8_score_window(self, qwin, K8, scales, d_state, step, len_max_host, S, workspace):
+        st = self._call.gkv_q8_score_window(self._handle, qwin, K8, scales, d_state, step, len_max_host, S, workspace)
+        if st is None:
+            st = self.lib.gkv_q8_score_window(self.h, _ptr(qwin), _ptr(K8), _ptr(scales), _ptr(d_state), step, len_max_host,
+                                              _ptr(S), _ptr(workspace), _stream())
+        if st:
+            raise GkvError(st, "gkv_q8_score_window")
+
+    def q8_compact(self, keep_idx, F, K8, V8, scales, F_hist, pos, d_state, step, workspace):
+        st = self._call.gkv_q8_compact(self._handle, keep_idx, F, K8, V8, scales, F_hist, pos, d_state, step, workspace)
+        if st is None:
+            st = self.lib.gkv_q8_compact(self.h, _ptr(keep_idx), _ptr(F), _ptr(K8), _ptr(V8), _ptr(scales), _ptr(F_hist),
+                                         _ptr(pos), _ptr(d_state), step, _ptr(workspace), _stream())
+        if st:
+            raise GkvError(st, "gkv_q8_compact")
+
+    def q8_evict(self, qwin, K8, V8, scales, F_hist, pos, d_state, step, len_max_host, S, F, keep_idx, workspace):
+        st = self._call.gkv_q8_evict(self._handle, qwin, K8, V8, scales, F_hist, pos, d_state, step, len_max_host, S, F, keep_idx, workspace)
+        if st is None:
+            st = self.lib.gkv_q8_evict(self.h, _ptr(qwin), _ptr(K8), _ptr(V8), _ptr(scales), _ptr(F_hist), _ptr(pos),
+                                       _ptr(d_state), step, len_max_host, _ptr(S), _ptr(F), _ptr(keep_idx),
+                                       _ptr(workspace), _stream())
+        if st:
+            raise GkvError(st, "gkv_q8_evict")
+
+    # prefix that sequences share: Kp, Vp [L,h_kv,prefix_capacity,d]; part: prefix_bytes(rows) bytes, zeroed once
+    def prefix_bytes(self, rows: int) -> int:
+        n = c_size_t()
+        self._check(self.lib.gkv_prefix_bytes(self.h, rows, byref(n)), "gkv_prefix_bytes")
+        return n.value
+
+    def prefix_attend(self, q, Kp, Vp, rows, prefix_capacity, first, count, part):
+        st = self._call.gkv_prefix_attend(self._handle, q, Kp, Vp, rows, prefix_capacity, first, count, part)
+        if st is None:
+            st = self.lib.gkv_prefix_attend(self.h, _ptr(q), _ptr(Kp), _ptr(Vp), rows, prefix_capacity, first, count,
+                                            _ptr(part), _stream())
+        if st:
+            raise GkvError(st, "gkv_prefix_attend")
+
+    def attend_decode_prefix(self, q, k_new, v_new, K, V, pos, step, qwin, d_state, len_max_host, part, out, workspace):
+        st = self._call.gkv_attend_decode_prefix(self._handle, q, k_new, v_new, K, V, pos, step, qwin, d_state, len_max_host, part, out, workspace)
+        if st is None:
+            st = self.lib.gkv_attend_decode_prefix(self.h, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(K), _ptr(V), _ptr(pos),
+                                                   step, _ptr(qwin), _ptr(d_state), len_max_host, _ptr(part), _ptr(out),
+                                                   _ptr(workspace), _stream())
+        if st:
+            raise GkvError(st, "gkv_attend_decode_prefix")
 
     def profile_enable(self, on: bool):
         self._check(self.lib.gkv_profile_enable(self.h, int(on)), "gkv_profile_enable")

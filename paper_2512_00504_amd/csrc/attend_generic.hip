@@ -10,8 +10,9 @@ namespace {
 
 constexpr int NWG = 4;     // wavefronts per workgroup
 
+// PREFIX: joined with a.prefix; the logits are in log2 units then, as its maxima are.
 // Dynamic LDS, per wavefront: float prob[cap + 1]; float qs[d]
-template <typename T>
+template <typename T, bool PREFIX>
 __global__ __launch_bounds__(NWG * 64) void attend_generic_kernel(GkvDims dm, AttendArgs a) {
   a.step = resolve_step(dm, a.step);
   extern __shared__ float smem[];
@@ -42,7 +43,7 @@ __global__ __launch_bounds__(NWG * 64) void attend_generic_kernel(GkvDims dm, At
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     // logits: a lane per key
-    float mx = -INFINITY;
+    float mx = PREFIX ? GKV_NO_MAX : -INFINITY;
     for (int n = lane; n < n_tot; n += 64) {
       float acc = 0.f;
       if (n == len0 && has_new) {
@@ -51,14 +52,14 @@ __global__ __launch_bounds__(NWG * 64) void attend_generic_kernel(GkvDims dm, At
         for (int c = 0; c < d; ++c)
           acc = fmaf(qs[c], Elem<T>::ld(Kh + k_elem_offset<EPC>(n, c, d, st.n_tiled)), acc);
       }
-      acc *= dm.scale;
+      if constexpr (!PREFIX) acc *= dm.scale;
       prob[n] = acc;
-      mx = fmaxf(mx, acc);
+      mx = fmaxf(mx, PREFIX ? rounded_product(acc, dm.scale_l2_hi) : acc);
     }
     mx = wave_max(mx);
     float sm = 0.f;
     for (int n = lane; n < n_tot; n += 64) {
-      float e = expf(prob[n] - mx);
+      float e = PREFIX ? exp2f(log2_weight(prob[n], dm.scale_l2_hi, dm.scale_l2_lo, mx)) : expf(prob[n] - mx);
       prob[n] = e;
       sm += e;
     }
@@ -66,14 +67,18 @@ __global__ __launch_bounds__(NWG * 64) void attend_generic_kernel(GkvDims dm, At
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    const float inv = sm > 0.f ? 1.f / sm : 0.f;
+    const size_t row = (size_t)lb * dm.Hq + head;
+    PrefixWeight pw{sm > 0.f ? 1.f / sm : 0.f, 0.f};
+    if constexpr (PREFIX) pw = prefix_weight(a.prefix, row, mx, sm, n_tot > 0);
     // output: a lane per channel, keys in order
     T* oh = (T*)a.out + ((size_t)lb * dm.Hq + head) * d;
     for (int c = lane; c < d; c += 64) {
       float acc = 0.f;
       for (int n = 0; n < len0; ++n) acc = fmaf(prob[n], Elem<T>::ld(Vh + (size_t)n * d + c), acc);
       if (has_new) acc = fmaf(prob[len0], Elem<T>::ld(vn + c), acc);
-      Elem<T>::st(oh + c, acc * inv);
+      acc *= pw.own;
+      if (PREFIX && pw.prefix != 0.f) acc = fmaf(a.prefix.o[row * d + c], pw.prefix, acc);
+      Elem<T>::st(oh + c, acc);
     }
     __builtin_amdgcn_wave_barrier();           // prob / qs are reused by this wavefront's next head
   }
@@ -103,10 +108,13 @@ __global__ __launch_bounds__(NWG * 64) void attend_generic_kernel(GkvDims dm, At
 
 }  // namespace
 
-hipError_t gkv_launch_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const AttendArgs& a) {
-  const int units = dm.L * dm.B * dm.Hkv;
+template <typename T>
+static hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const AttendArgs& a) {
   const size_t shmem = sizeof(float) * NWG * (size_t)(dm.cap + 1 + dm.d);
-  if (dtype == GKV_F32)
-    return gkv_launch(ln, attend_generic_kernel<float>, dim3(units), dim3(NWG * 64), shmem, dm, a);
-  return gkv_launch(ln, attend_generic_kernel<uint16_t>, dim3(units), dim3(NWG * 64), shmem, dm, a);
+  return gkv_launch(ln, a.prefix.o ? attend_generic_kernel<T, true> : attend_generic_kernel<T, false>, dim3(dm.L * dm.B * dm.Hkv),
+                    dim3(NWG * 64), shmem, dm, a);
+}
+
+hipError_t gkv_launch_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const AttendArgs& a) {
+  return dtype == GKV_F32 ? launch<float>(ln, dm, a) : launch<uint16_t>(ln, dm, a);
 }

@@ -432,6 +432,7 @@ struct KernelArgs {
   int32_t splits, split_iters, Hq, Hkv, g, cap, LB, w, step;
   int32_t has_base, copy_q, write_stats;
   float scale_hi, scale_lo;
+  PrefixPart prefix;
 };
 
 // When a wavefront with one slice in flight asks for the next one: BEHIND the products with this one, or K EARLY, as soon as
@@ -442,8 +443,9 @@ enum class Next { BEHIND, IN_STEP, PACED, EARLY };
 
 // KT = 16-key tiles per wavefront iteration (1 or 2); DEPTH = slices in flight (1 or 2: twice the registers, for launches
 // that leave them free).  STAGED: the rows to store wait in LDS instead of registers (32 units of 577 rows 6.1 us against 6.2
-// in registers, whatever the room; fp32, D = 128 9.15 / 8.8).
-template <typename T, int D, int NW, int KT, int OCC, int DEPTH, Next NEXT, bool STAGED>
+// in registers, whatever the room; fp32, D = 128 9.15 / 8.8).  PREFIX: the result is joined with a.prefix; the softmax statistics
+// stay those of the sequence's own rows.
+template <typename T, int D, int NW, int KT, int OCC, int DEPTH, Next NEXT, bool STAGED, bool PREFIX>
 __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a) {
   using G = Geo<T, D>;
   constexpr int KEYS = 16 * KT;             // keys per iteration
@@ -646,6 +648,17 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
   float* part = a.partials + (size_t)(unit * splits) * g * PSTR;      // [ns][g][PSTR]
   const int slot = step - quotient(step, a.by_w) * a.w;
   float2* stats = a.stats + (size_t)slot * a.LB * a.Hq + head0;
+  // the unit's result, from its own sum of weighted values
+  auto finish = [&](int x, int h, int c4, float M, float L, const f32x4& o, bool fast) {
+    if constexpr (PREFIX) {
+      const PrefixWeight pw = prefix_weight(a.prefix, head0 + h, M, L, n_tot > 0);
+      f32x4 y = o * pw.own;
+      if (pw.prefix != 0.f) y += *(const f32x4*)(a.prefix.o + (head0 + h) * D + c4) * pw.prefix;
+      store_row4(out + (uint32_t)(x * 4), y);
+    } else {
+      store_row4(out + (uint32_t)(x * 4), o * inv_sum(L, n_tot > 0, fast));
+    }
+  };
   for (int x = tid; x < g * TPH; x += NW * 64) {
     const int h = x / TPH, c4 = (x % TPH) * 4;
     float mw[NW], lw[NW];
@@ -667,7 +680,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
       o += *(const f32x4*)(so + (wv * g + h) * OSTR + c4) * f;
     }
     if (ns == 1) {
-      store_row4(out + (uint32_t)(x * 4), o * inv_sum(Lsum, n_tot > 0, !G::F32 && D == 128));
+      finish(x, h, c4, M, Lsum, o, !G::F32 && D == 128);
       // softmax statistics of this head's row (running max in log2 units, sum), into the ring slot
       // that also receives q: the window score of the next compression reuses them
       if (c4 == 0 && a.write_stats) stats[h] = make_float2(M, Lsum);
@@ -746,7 +759,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
             o += f32x4{got[i][1].x, got[i][1].y, got[i][2].x, got[i][2].y} * f;
           }
       }
-      store_row4(out + (uint32_t)(x * 4), o * inv_sum(Lsum, n_tot > 0, false));
+      finish(x, h, c4, M, Lsum, o, false);
       if (c4 == 0 && a.write_stats) stats[h] = make_float2(M, Lsum);
     }
   }
@@ -772,8 +785,11 @@ static hipError_t launch_attend(const GkvLaunch& ln, const GkvDims& dm, const At
   k.Hq = dm.Hq; k.Hkv = dm.Hkv; k.g = dm.g; k.cap = dm.cap; k.LB = dm.L * dm.B; k.w = dm.w; k.step = a.step;
   k.has_base = dm.step_base != nullptr; k.copy_q = a.copy_q; k.write_stats = a.write_stats;
   k.scale_hi = dm.scale_l2_hi; k.scale_lo = dm.scale_l2_lo;
+  k.prefix = a.prefix;
   const size_t shmem = gkv_attend_mfma_lds(sizeof(T), D, dm.g, NW);
-  return gkv_launch(ln, attend_mfma_kernel<T, D, NW, KT, OCC, DEPTH, NEXT, STAGED>, dim3(units * a.splits), dim3(NW * 64), shmem, k);
+  auto kern = a.prefix.o ? attend_mfma_kernel<T, D, NW, KT, OCC, DEPTH, NEXT, STAGED, true>
+                         : attend_mfma_kernel<T, D, NW, KT, OCC, DEPTH, NEXT, STAGED, false>;
+  return gkv_launch(ln, kern, dim3(units * a.splits), dim3(NW * 64), shmem, k);
 }
 
 // The form of a launch of 4 or 8 wavefronts, by its number of workgroups.

@@ -56,7 +56,9 @@ void convert(PyObject* o, float& out) {
 // (the library is loaded through ctypes).
 #define GKV_CALLS(X)                                                                                 \
   X(gkv_attend_decode) X(gkv_score_window) X(gkv_global_update) X(gkv_select_topk) X(gkv_compact)    \
-  X(gkv_evict) X(gkv_redundancy_combine) X(gkv_evicted_positions)
+  X(gkv_evict) X(gkv_redundancy_combine) X(gkv_evicted_positions)                                   \
+  X(gkv_q8_attend_decode) X(gkv_q8_score_window) X(gkv_q8_compact) X(gkv_q8_evict)                   \
+  X(gkv_prefix_attend) X(gkv_attend_decode_prefix)
 #define GKV_TYPE(name) struct call_##name { static inline decltype(&::name) address = nullptr; };
 GKV_CALLS(GKV_TYPE)
 

@@ -213,10 +213,11 @@ hipError_t launch_score_topk(const GkvLaunch& ln, const GkvDims& dm, const float
 // POW2: rows of 2^np_log pieces (bf16 and fp32 at d = 64 and 128, among others): a thread's piece is the same in every row it moves, rows
 // follow by a constant, and nothing is divided at run time (us with the copy of the record, in a graph, before -> now: 4 units of b =
 // 98 6.2 -> 5.7, of 512 8.7 -> 8.0, 32 of 512 10.7 -> 10.2, fp32 8 of 322 9.3 -> 8.7).
-template <int PPT, int NT, bool SHARED, bool POW2>
+// WORDS: each row of K and V has a word of `words` too (the scales of a cache in 8 bits), which moves with its position.
+template <int PPT, int NT, bool SHARED, bool POW2, bool WORDS>
 __global__ __launch_bounds__(NT) void compact_kernel(GkvDims dm, int esz, int np_log, const int32_t* __restrict__ keep_idx,
                                                      const float* __restrict__ F, void* K, void* V,
-                                                     float* __restrict__ F_hist, int32_t* pos,
+                                                     float* __restrict__ F_hist, int32_t* pos, uint32_t* words,
                                                      int32_t* d_state, int step, int32_t* state_ticket, int shares) {
   step = resolve_step(dm, step);
   if constexpr (!SHARED) shares = 1;             // known to the compiler
@@ -326,10 +327,13 @@ __global__ __launch_bounds__(NT) void compact_kernel(GkvDims dm, int esz, int np
       buf[i] = base[so];
     }
     int pos_val[PR];
+    uint32_t word[WORDS ? PR : 1];
 #pragma unroll
     for (int i = 0; i < PR; ++i) {
       const int rr = tid + NT * i;
-      pos_val[i] = pu[isPos && rr < R && r0 + rr < b ? source(r0 + rr) : 0];
+      const int src = isPos && rr < R && r0 + rr < b ? source(r0 + rr) : 0;
+      pos_val[i] = pu[src];
+      if constexpr (WORDS) word[i] = words[(size_t)unit * dm.cap + src];
     }
     __syncthreads();
 #pragma unroll
@@ -338,7 +342,10 @@ __global__ __launch_bounds__(NT) void compact_kernel(GkvDims dm, int esz, int np
 #pragma unroll
     for (int i = 0; i < PR; ++i) {
       const int rr = tid + NT * i;
-      if (isPos && rr < R && r0 + rr < b) pu[r0 + rr] = pos_val[i];
+      if (isPos && rr < R && r0 + rr < b) {
+        pu[r0 + rr] = pos_val[i];
+        if constexpr (WORDS) words[(size_t)unit * dm.cap + r0 + rr] = word[i];
+      }
     }
   }
   // (every wavefront of this workgroup passed the barrier above after reading the record)
@@ -448,12 +455,12 @@ hipError_t gkv_launch_update_and_select(const GkvLaunch& ln, const GkvDims& dm, 
   return launch_score_topk<true, true>(ln, dm, S, F_hist, d_state, step, F_out, keep_idx);
 }
 
-hipError_t gkv_launch_compact(const GkvLaunch& ln, const GkvDims& dm, int esz, const int32_t* keep_idx,
-                              const float* F, void* K, void* V, float* F_hist, int32_t* pos,
-                              int32_t* d_state, int32_t step, int32_t* state_ticket) {
+template <bool WORDS>
+static hipError_t launch_compact(const GkvLaunch& ln, const GkvDims& dm, int esz, int ppt, const int32_t* keep_idx,
+                                 const float* F, void* K, void* V, float* F_hist, int32_t* pos, uint32_t* words,
+                                 int32_t* d_state, int32_t step, int32_t* state_ticket) {
   const int units = dm.L * dm.B * dm.Hkv;
   const size_t shmem = sizeof(int) * (size_t)(dm.b - dm.w);
-  const int ppt = ln.ctx ? ln.ctx->compact_ppt : 8;
   // A workgroup moves its rows in rounds of 32 KiB whose loads wait for the stores before them, about
   // 2.5 us each; with few units the chip is empty meanwhile, so the rows' columns are shared out (at
   // least 64 bytes of a row each) and a share of more than 64 KiB gets 1024 threads, four times the round; up to 16 units
@@ -478,17 +485,35 @@ hipError_t gkv_launch_compact(const GkvLaunch& ln, const GkvDims& dm, int esz, c
   // 804.8, fp32 600 of 400 136.6 -> 138.1, but 9216 of 90 224.1 -> 220.8, bf16, d = 64 640 of 500 46.8 -> 44.1.
   const bool pow2 = (pieces & (pieces - 1)) == 0 && units <= 512;
   const int np_log = pow2 ? __builtin_ctz(pieces) : 0;
-#define GKV_COMPACT(PPT_, NT_) (shares > 1 ? (pow2 ? compact_kernel<PPT_, NT_, true, true> : compact_kernel<PPT_, NT_, true, false>) \
-                                           : (pow2 ? compact_kernel<PPT_, NT_, false, true> : compact_kernel<PPT_, NT_, false, false>))
-  auto kern = ppt == 16 ? GKV_COMPACT(16, 256) : ppt == 4 ? GKV_COMPACT(4, 256) : wide ? GKV_COMPACT(8, 1024) : GKV_COMPACT(8, 256);
+#define GKV_COMPACT(PPT_, NT_) (shares > 1 ? (pow2 ? compact_kernel<PPT_, NT_, true, true, WORDS> : compact_kernel<PPT_, NT_, true, false, WORDS>) \
+                                           : (pow2 ? compact_kernel<PPT_, NT_, false, true, WORDS> : compact_kernel<PPT_, NT_, false, false, WORDS>))
+  auto kern = wide ? GKV_COMPACT(8, 1024) : GKV_COMPACT(8, 256);
+  if constexpr (!WORDS) {
+    if (ppt == 16) kern = GKV_COMPACT(16, 256);
+    if (ppt == 4) kern = GKV_COMPACT(4, 256);
+  }
 #undef GKV_COMPACT
   const int threads = wide ? 1024 : 256;
   hipError_t e = gkv_launch(ln, kern, dim3(units, 2 * shares), dim3(threads), shmem, dm, esz, np_log, keep_idx, F, K, V,
-                            F_hist, pos, d_state, (int)step, state_ticket, shares);
+                            F_hist, pos, words, d_state, (int)step, state_ticket, shares);
   if (e != hipSuccess || state_ticket != nullptr) return e;
   const int nlb = dm.L * dm.B;
   GkvLaunch plain{ln.ctx, -1, ln.stream};
   return gkv_launch(plain, finalize_state_kernel, dim3((nlb + 255) / 256), dim3(256), 0, dm, d_state, (int)step);
+}
+
+hipError_t gkv_launch_compact(const GkvLaunch& ln, const GkvDims& dm, int esz, const int32_t* keep_idx,
+                              const float* F, void* K, void* V, float* F_hist, int32_t* pos,
+                              int32_t* d_state, int32_t step, int32_t* state_ticket) {
+  return launch_compact<false>(ln, dm, esz, ln.ctx ? ln.ctx->compact_ppt : 8, keep_idx, F, K, V, F_hist, pos, nullptr, d_state,
+                               step, state_ticket);
+}
+
+// Rows of d bytes: the same moves as for rows of half as many bf16 elements, and the scales go with the positions.
+hipError_t gkv_launch_q8_compact(const GkvLaunch& ln, const GkvDims& dm, const int32_t* keep_idx, const float* F, void* K8,
+                                 void* V8, uint32_t* scales, float* F_hist, int32_t* pos, int32_t* d_state, int32_t step,
+                                 int32_t* state_ticket) {
+  return launch_compact<true>(ln, dm, 1, 8, keep_idx, F, K8, V8, F_hist, pos, scales, d_state, step, state_ticket);
 }
 
 hipError_t gkv_launch_pool_scores(const GkvLaunch& ln, const GkvDims& dm, const float* F, const int32_t* d_state,

@@ -128,6 +128,7 @@ extern "C" gkv_status gkv_create(const gkv_config* cfg, gkv_ctx** out_ctx) {
   c->stats_mixed = false;
   c->mfma_redundancy = cfg->dtype == GKV_BF16 && d.d == 128 && d.g <= 16;
   c->mfma_shape = (d.d == 64 || d.d == 128) && d.g <= 16;
+  c->prefix_rows = -1;
   c->prof = new (std::nothrow) GkvProfile();
   *out_ctx = c;
   return GKV_OK;
@@ -431,32 +432,54 @@ static int split_set(gkv_ctx* ctx, const void* workspace, hipStream_t stream) {
   return ctx->n_split_keys++;
 }
 
-extern "C" gkv_status gkv_attend_decode(gkv_ctx* ctx, const void* q, const void* k_new, const void* v_new,
-                                        void* K, void* V, int32_t* pos, int32_t step, void* qwin,
-                                        const int32_t* d_state, int32_t len_max_host, void* out,
-                                        void* workspace, void* stream) {
+// Where a decode call's partial results go and how its units are cut; `plan` as the library would have it.
+static gkv_status place_pieces(gkv_ctx* ctx, AttendPlan* plan, void* workspace, void* stream, GkvWorkspace* ws) {
+  int set = auto_sets(ctx);                                       // "attend_splits"
+  if (ctx->attend_splits > 0) {
+    if (plan->splits > ctx->ws_splits) return GKV_ERR_WORKSPACE;  // partials would not fit the workspace as sized
+  } else if (plan->splits > 1) {
+    set = plan->splits > ctx->ws_auto_splits ? -1 : split_set(ctx, workspace, (hipStream_t)stream);
+    if (set < 0) { *plan = attend_plan(ctx, 1); set = 0; }        // not cut
+  }
+  *ws = gkv_carve_workspace(ctx, workspace, set);
+  return GKV_OK;
+}
+static int32_t copies_q(const gkv_ctx* ctx, const void* q, const void* qwin, int32_t step) {
+  const size_t slot_bytes = (size_t)ctx->dims.L * ctx->dims.B * ctx->dims.Hq * ctx->dims.d * ctx->esz;
+  return (const char*)q != (const char*)qwin + (size_t)(step % ctx->dims.w) * slot_bytes;
+}
+
+// What gkv_prefix_attend leaves at the start of its buffer.
+static size_t prefix_o_bytes(const gkv_ctx* ctx) {
+  return gkv_align256((size_t)ctx->dims.L * ctx->dims.B * ctx->dims.Hq * ctx->dims.d * sizeof(float));
+}
+static PrefixPart prefix_part(const gkv_ctx* ctx, const void* part) {
+  if (!part) return PrefixPart{nullptr, nullptr};
+  return PrefixPart{(const float*)part, (const float2*)((const char*)part + prefix_o_bytes(ctx))};
+}
+static bool aligned16(std::initializer_list<const void*> ptrs) {
+  uintptr_t bits = 0;
+  for (const void* p : ptrs) bits |= (uintptr_t)p;
+  return (bits & 15) == 0;
+}
+
+static gkv_status attend_decode(gkv_ctx* ctx, const void* q, const void* k_new, const void* v_new,
+                                void* K, void* V, int32_t* pos, int32_t step, void* qwin,
+                                const int32_t* d_state, int32_t len_max_host, const void* part, void* out,
+                                void* workspace, void* stream) {
   if (!ctx || !q || !K || !V || !pos || !qwin || !d_state || !out || step < 0) return GKV_ERR_INVALID_ARG;
   if ((k_new == nullptr) != (v_new == nullptr)) return GKV_ERR_INVALID_ARG;
   if (!workspace) return GKV_ERR_WORKSPACE;
   gkv_status st = check_len(ctx, len_max_host, k_new != nullptr);
   if (st != GKV_OK) return st;
   AttendArgs a{q, k_new, v_new, K, V, pos, step, qwin, d_state, out, gkv_carve_workspace(ctx, workspace), 1,
-               ctx->attend_tile, 1, 0, 4, 0};
-  {
-    const size_t slot_bytes = (size_t)ctx->dims.L * ctx->dims.B * ctx->dims.Hq * ctx->dims.d * ctx->esz;
-    a.copy_q = (const char*)q != (const char*)qwin + (size_t)(step % ctx->dims.w) * slot_bytes;
-  }
+               ctx->attend_tile, 1, 0, 4, 0, prefix_part(ctx, part)};
+  a.copy_q = copies_q(ctx, q, qwin, step);
   GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
   if (use_mfma(ctx, {q, k_new, v_new, K, V, qwin, out})) {
     AttendPlan plan = attend_plan(ctx, ctx->attend_splits);
-    int set = auto_sets(ctx);                                       // "attend_splits"
-    if (ctx->attend_splits > 0) {
-      if (plan.splits > ctx->ws_splits) return GKV_ERR_WORKSPACE;   // partials would not fit the workspace as sized
-    } else if (plan.splits > 1) {
-      set = plan.splits > ctx->ws_auto_splits ? -1 : split_set(ctx, workspace, (hipStream_t)stream);
-      if (set < 0) { plan = attend_plan(ctx, 1); set = 0; }         // not cut
-    }
-    a.ws = gkv_carve_workspace(ctx, workspace, set);
+    st = place_pieces(ctx, &plan, workspace, stream, &a.ws);
+    if (st != GKV_OK) return st;
     a.waves = plan.waves; a.splits = plan.splits; a.split_iters = plan.iters;
     // An appending step leaves (max, sum) of every query head's softmax in the ring slot
     // of this step; the window score can then skip its own pass over the keys for them.
@@ -466,6 +489,21 @@ extern "C" gkv_status gkv_attend_decode(gkv_ctx* ctx, const void* q, const void*
   }
   note_stats(ctx, step, false, workspace, K, qwin, (hipStream_t)stream);
   return hip_status(gkv_launch_attend_generic(ln, ctx->dims, ctx->cfg.dtype, a));
+}
+
+extern "C" gkv_status gkv_attend_decode(gkv_ctx* ctx, const void* q, const void* k_new, const void* v_new,
+                                        void* K, void* V, int32_t* pos, int32_t step, void* qwin,
+                                        const int32_t* d_state, int32_t len_max_host, void* out,
+                                        void* workspace, void* stream) {
+  return attend_decode(ctx, q, k_new, v_new, K, V, pos, step, qwin, d_state, len_max_host, nullptr, out, workspace, stream);
+}
+
+extern "C" gkv_status gkv_attend_decode_prefix(gkv_ctx* ctx, const void* q, const void* k_new, const void* v_new,
+                                               void* K, void* V, int32_t* pos, int32_t step, void* qwin,
+                                               const int32_t* d_state, int32_t len_max_host, const void* part, void* out,
+                                               void* workspace, void* stream) {
+  if (!part || !aligned16({part})) return GKV_ERR_INVALID_ARG;
+  return attend_decode(ctx, q, k_new, v_new, K, V, pos, step, qwin, d_state, len_max_host, part, out, workspace, stream);
 }
 
 extern "C" gkv_status gkv_score_window(gkv_ctx* ctx, const void* qwin, const void* K, const int32_t* d_state,
@@ -613,6 +651,141 @@ extern "C" gkv_status gkv_evicted_positions(gkv_ctx* ctx, const int32_t* keep_id
   if (!ctx || !keep_idx || !pos || !d_state || !evicted || step < 0) return GKV_ERR_INVALID_ARG;
   GkvLaunch ln{ctx, -1, (hipStream_t)stream};
   return hip_status(gkv_launch_evicted_positions(ln, ctx->dims, keep_idx, pos, d_state, step, evicted));
+}
+
+// ---- cache in 8 bits -----------------------------------------------------------------------------
+// Pieces of 16 codes, and the rows' scales in words of 32 bits.
+static gkv_status check_q8(const gkv_ctx* ctx, std::initializer_list<const void*> ptrs) {
+  if (ctx->dims.d % 16 != 0) return GKV_ERR_SHAPE;
+  return aligned16(ptrs) ? GKV_OK : GKV_ERR_INVALID_ARG;
+}
+
+extern "C" gkv_status gkv_q8_store_prompt(gkv_ctx* ctx, const void* k, const void* v, int32_t n, int32_t t_first, int32_t t0,
+                                          const int32_t* d_prompt_len, void* K8, void* V8, void* scales, int32_t* pos,
+                                          void* stream) {
+  if (!ctx || !k || !v || !d_prompt_len || !K8 || !V8 || !scales || !pos || n < 1 || t_first < 0 || t0 < 0)
+    return GKV_ERR_INVALID_ARG;
+  const gkv_status st = check_q8(ctx, {k, v, K8, V8, scales});
+  if (st != GKV_OK) return st;
+  Q8StoreArgs a{k, v, n, t_first, t0, d_prompt_len, (uint8_t*)K8, (uint8_t*)V8, (uint32_t*)scales, pos, 0, 0};
+  GkvLaunch ln{ctx, -1, (hipStream_t)stream};
+  return hip_status(gkv_launch_q8_store(ln, ctx->dims, ctx->cfg.dtype, a));
+}
+
+extern "C" gkv_status gkv_q8_read(gkv_ctx* ctx, const void* K8, const void* V8, const void* scales, const int32_t* d_state,
+                                  int32_t step, void* K, void* V, void* stream) {
+  if (!ctx || !scales || !d_state || (!K && !V) || (K && !K8) || (V && !V8) || step < 0) return GKV_ERR_INVALID_ARG;
+  const gkv_status st = check_q8(ctx, {K8, V8, scales, K, V});
+  if (st != GKV_OK) return st;
+  Q8ReadArgs a{(const uint8_t*)K8, (const uint8_t*)V8, (const uint32_t*)scales, d_state, step, K, V, K && V ? 2 : K ? 0 : 1, 0};
+  GkvLaunch ln{ctx, -1, (hipStream_t)stream};
+  return hip_status(gkv_launch_q8_read(ln, ctx->dims, ctx->cfg.dtype, a));
+}
+
+extern "C" gkv_status gkv_q8_attend_decode(gkv_ctx* ctx, const void* q, const void* k_new, const void* v_new,
+                                           void* K8, void* V8, void* scales, int32_t* pos, int32_t step, void* qwin,
+                                           const int32_t* d_state, int32_t len_max_host, const void* part, void* out,
+                                           void* workspace, void* stream) {
+  if (!ctx || !q || !K8 || !V8 || !scales || !pos || !qwin || !d_state || !out || step < 0) return GKV_ERR_INVALID_ARG;
+  if ((k_new == nullptr) != (v_new == nullptr)) return GKV_ERR_INVALID_ARG;
+  if (!workspace) return GKV_ERR_WORKSPACE;
+  gkv_status st = check_len(ctx, len_max_host, k_new != nullptr);
+  if (st == GKV_OK) st = check_q8(ctx, {K8, V8, scales, part});
+  if (st != GKV_OK) return st;
+  Q8AttendArgs a{q, k_new, v_new, (uint8_t*)K8, (uint8_t*)V8, (uint32_t*)scales, pos, step, qwin, d_state, out,
+                 prefix_part(ctx, part), gkv_carve_workspace(ctx, workspace), 1, 0, 4, copies_q(ctx, q, qwin, step), 0};
+  GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
+  note_stats(ctx, step, false, workspace, K8, qwin, (hipStream_t)stream);
+  return hip_status(gkv_launch_q8_attend_generic(ln, ctx->dims, ctx->cfg.dtype, a));
+}
+
+extern "C" gkv_status gkv_q8_score_window(gkv_ctx* ctx, const void* qwin, const void* K8, const void* scales,
+                                          const int32_t* d_state, int32_t step, int32_t len_max_host, float* S,
+                                          void* workspace, void* stream) {
+  if (!ctx || !qwin || !K8 || !scales || !d_state || !S || step < 0) return GKV_ERR_INVALID_ARG;
+  gkv_status st = check_len(ctx, len_max_host, false);
+  if (st == GKV_OK) st = check_q8(ctx, {K8, scales});
+  if (st != GKV_OK) return st;
+  Q8ScoreArgs a{qwin, (const uint8_t*)K8, (const uint32_t*)scales, d_state, step, S, nullptr};
+  GkvLaunch ln{ctx, GKV_K_SCORE, (hipStream_t)stream};
+  return hip_status(gkv_launch_q8_score_generic(ln, ctx->dims, ctx->cfg.dtype, a));
+}
+
+extern "C" gkv_status gkv_q8_compact(gkv_ctx* ctx, const int32_t* keep_idx, const float* F, void* K8, void* V8, void* scales,
+                                     float* F_hist, int32_t* pos, int32_t* d_state, int32_t step,
+                                     void* workspace, void* stream) {
+  if (!ctx || !keep_idx || !F || !K8 || !V8 || !scales || !F_hist || !pos || !d_state || step < 0) return GKV_ERR_INVALID_ARG;
+  if (F == F_hist) return GKV_ERR_INVALID_ARG;
+  const gkv_status st = check_q8(ctx, {K8, V8, scales});
+  if (st != GKV_OK) return st;
+  GkvLaunch ln{ctx, GKV_K_COMPACT, (hipStream_t)stream};
+  int32_t* ticket = workspace ? gkv_carve_workspace(ctx, workspace).state_ticket : nullptr;
+  return hip_status(gkv_launch_q8_compact(ln, ctx->dims, keep_idx, F, K8, V8, (uint32_t*)scales, F_hist, pos, d_state, step, ticket));
+}
+
+extern "C" gkv_status gkv_q8_evict(gkv_ctx* ctx, const void* qwin, void* K8, void* V8, void* scales, float* F_hist, int32_t* pos,
+                                   int32_t* d_state, int32_t step, int32_t len_max_host,
+                                   float* S, float* F, int32_t* keep_idx, void* workspace, void* stream) {
+  if (!ctx || !qwin || !K8 || !V8 || !scales || !F_hist || !pos || !d_state || !S || !F || !keep_idx || step < 0)
+    return GKV_ERR_INVALID_ARG;
+  if (F == F_hist) return GKV_ERR_INVALID_ARG;
+  gkv_status st = check_q8(ctx, {K8, V8, scales});
+  if (st != GKV_OK) return st;
+  st = gkv_q8_score_window(ctx, qwin, K8, scales, d_state, step, len_max_host, S, workspace, stream);
+  if (st != GKV_OK) return st;
+  GkvLaunch ln{ctx, GKV_K_TOPK, (hipStream_t)stream};
+  st = hip_status(gkv_launch_update_and_select(ln, ctx->dims, S, F_hist, d_state, step, F, keep_idx));
+  if (st != GKV_OK) return st;
+  return gkv_q8_compact(ctx, keep_idx, F, K8, V8, scales, F_hist, pos, d_state, step, workspace, stream);
+}
+
+// ---- shared prefix ---------------------------------------------------------------------------------
+// Pieces of a prefix of `rows` rows for `count` sequences: about two thousand workgroups, one a (sequence, KV head, piece), of
+// 256 rows at least.  More rows never make fewer pieces, so a buffer for more rows holds those of fewer.
+static int prefix_splits(const gkv_ctx* ctx, int rows, int count) {
+  const int64_t units = (int64_t)ctx->dims.L * count * ctx->dims.Hkv;
+  const int64_t want = 2048 / units, most = ((int64_t)rows + 255) / 256;
+  int64_t n = want < most ? want : most;
+  return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+}
+
+extern "C" gkv_status gkv_prefix_bytes(gkv_ctx* ctx, int32_t rows_max, size_t* out_bytes) {
+  if (!ctx || !out_bytes || rows_max < 0) return GKV_ERR_INVALID_ARG;
+  size_t pieces = 0;                                              // of one KV head's share of a call, in sequences
+  for (int count = 1; count <= ctx->dims.B; ++count) {
+    const int n = prefix_splits(ctx, rows_max, count);
+    if (n > 1 && (size_t)n * count > pieces) pieces = (size_t)n * count;
+  }
+  const size_t heads = (size_t)ctx->dims.L * ctx->dims.Hq;
+  if (rows_max > ctx->prefix_rows) ctx->prefix_rows = rows_max;
+  *out_bytes = prefix_o_bytes(ctx) + gkv_align256(heads * ctx->dims.B * sizeof(float2)) +
+               gkv_align256(pieces * heads * ctx->dims.d * sizeof(float)) + gkv_align256(pieces * heads * sizeof(float2));
+  return GKV_OK;
+}
+
+extern "C" gkv_status gkv_prefix_attend(gkv_ctx* ctx, const void* q, const void* Kp, const void* Vp, int32_t rows,
+                                        int32_t capacity, int32_t first, int32_t count, void* part, void* stream) {
+  if (!ctx || !q || !part || rows < 0 || rows > capacity || (rows > 0 && (!Kp || !Vp))) return GKV_ERR_INVALID_ARG;
+  if (first < 0 || count < 1 || first > ctx->dims.B - count) return GKV_ERR_INVALID_ARG;
+  if (!aligned16({part})) return GKV_ERR_INVALID_ARG;
+  if (ctx->dims.d % 4 != 0) return GKV_ERR_SHAPE;
+  if (rows > ctx->prefix_rows) return GKV_ERR_WORKSPACE;          // the buffer was not sized for them
+  const GkvDims& d = ctx->dims;
+  const size_t heads = (size_t)d.L * d.Hq;
+  PrefixArgs a{q, Kp, Vp, rows, capacity, first, count, 1, 0, nullptr, nullptr, nullptr, nullptr};
+  char* p = (char*)part;
+  a.o = (float*)p; p += prefix_o_bytes(ctx);
+  a.ms = (float2*)p; p += gkv_align256(heads * d.B * sizeof(float2));
+  const int n = prefix_splits(ctx, rows, count);
+  a.split_rows = ((rows + n - 1) / n + 63) / 64 * 64;
+  if (a.split_rows < 64) a.split_rows = 64;
+  a.splits = rows > 0 ? (rows + a.split_rows - 1) / a.split_rows : 1;
+  a.part_o = (float*)p; p += gkv_align256((size_t)a.splits * heads * count * d.d * sizeof(float));
+  a.part_ms = (float2*)p;
+  GkvLaunch ln{ctx, -1, (hipStream_t)stream};
+  gkv_status st = hip_status(gkv_launch_prefix_generic(ln, d, ctx->cfg.dtype, a));
+  if (st != GKV_OK || a.splits == 1) return st;
+  return hip_status(gkv_launch_prefix_join(ln, d, a));
 }
 
 // ---- profiling API ------------------------------------------------------------------------------

@@ -61,6 +61,7 @@ struct gkv_ctx {
   int32_t compact_ppt;    // 16-byte pieces per thread and chunk round of the compaction kernel: 4, 8 or 16
   int32_t reuse_stats;    // window score may reuse the softmax statistics the decode kernel recorded
   bool mfma_shape;        // d == 64 or 128, g <= 16: the matrix-core decode and window-score kernels cover it
+  int32_t prefix_rows;    // prefix rows that gkv_prefix_bytes has been asked for
   bool mfma_redundancy;   // bf16, d == 128, g <= 16: the matrix-core redundancy kernel does
   GkvProfile* prof;
   // Host record of which ring slots hold softmax statistics written by the matrix-core decode
@@ -101,6 +102,10 @@ struct GkvLaunch {
   bool continued = false;   // a further launch of the same call: its time counts, the call does not count again
 };
 
+// The results over a shared prefix of every (layer, sequence, query head): unnormalised outputs, and maximum (log2 units) and
+// sum.  A sum of zero: nothing there.  o == nullptr: no prefix.
+struct PrefixPart { const float* o; const float2* ms; };
+
 // ---- launch wrappers implemented in the kernel files -------------------------------------
 struct AttendArgs {
   const void* q; const void* k_new; const void* v_new;
@@ -110,6 +115,7 @@ struct AttendArgs {
   int32_t write_stats;   // record (max, sum) of every query head's softmax in ws.stats
   int32_t waves;         // wavefronts per workgroup of the matrix-core kernel: 4, 8 or 16
   int32_t split_iters;   // slices per piece (a unit of n slices is cut into ceil(n / split_iters)); 0 = all splits
+  PrefixPart prefix;     // joined to the result
 };
 hipError_t gkv_launch_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const AttendArgs& a);
 hipError_t gkv_launch_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const AttendArgs& a);
@@ -139,6 +145,46 @@ hipError_t gkv_launch_pool_scores(const GkvLaunch& ln, const GkvDims& dm, const 
                                   int32_t step, int32_t kernel, float* F_out);
 hipError_t gkv_launch_evicted_positions(const GkvLaunch& ln, const GkvDims& dm, const int32_t* keep_idx,
                                         const int32_t* pos, const int32_t* d_state, int32_t step, int32_t* evicted);
+
+// ---- cache in 8 bits (see e4m3.h) ----------------------------------------------------------
+struct Q8StoreArgs {
+  const void* k; const void* v; int32_t n, t_first, t0; const int32_t* prompt_len;
+  uint8_t* K8; uint8_t* V8; uint32_t* scales; int32_t* pos;
+  int32_t rows, lanes_log;      // of a workgroup; lanes a row (set by the launch)
+};
+struct Q8ReadArgs {
+  const uint8_t* K8; const uint8_t* V8; const uint32_t* scales; const int32_t* d_state; int32_t step;
+  void* K; void* V; int32_t which;   // 0: K, 1: V, 2: both
+  int32_t rows;                 // of a workgroup (set by the launch)
+};
+struct Q8AttendArgs {
+  const void* q; const void* k_new; const void* v_new;
+  uint8_t* K8; uint8_t* V8; uint32_t* scales; int32_t* pos; int32_t step; void* qwin; const int32_t* d_state; void* out;
+  PrefixPart prefix;
+  GkvWorkspace ws; int32_t splits, split_iters, waves, copy_q, write_stats;   // as in AttendArgs
+};
+struct Q8ScoreArgs {
+  const void* qwin; const uint8_t* K8; const uint32_t* scales; const int32_t* d_state; int32_t step; float* S;
+  const float2* stats;
+};
+hipError_t gkv_launch_q8_store(const GkvLaunch& ln, const GkvDims& dm, int dtype, Q8StoreArgs a);
+hipError_t gkv_launch_q8_read(const GkvLaunch& ln, const GkvDims& dm, int dtype, Q8ReadArgs a);
+hipError_t gkv_launch_q8_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8AttendArgs& a);
+hipError_t gkv_launch_q8_score_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8ScoreArgs& a);
+hipError_t gkv_launch_q8_compact(const GkvLaunch& ln, const GkvDims& dm, const int32_t* keep_idx, const float* F, void* K8,
+                                 void* V8, uint32_t* scales, float* F_hist, int32_t* pos, int32_t* d_state, int32_t step,
+                                 int32_t* state_ticket);
+
+// ---- shared prefix ---------------------------------------------------------------------------
+struct PrefixArgs {
+  const void* q; const void* K; const void* V;
+  int32_t rows, capacity, first, count;
+  int32_t splits, split_rows;   // pieces, rows of each; with one piece the results go to o and ms
+  float* o; float2* ms;         // [L,B,h_q,d], [L,B,h_q]
+  float* part_o; float2* part_ms;   // [splits][L,count,h_q] of each
+};
+hipError_t gkv_launch_prefix_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a);
+hipError_t gkv_launch_prefix_join(const GkvLaunch& ln, const GkvDims& dm, const PrefixArgs& a);
 hipError_t gkv_launch_fill_zero(hipStream_t stream, int32_t* p, size_t n);
 hipError_t gkv_launch_add_int(hipStream_t stream, int32_t* p, int32_t delta);
 
@@ -247,6 +293,24 @@ __device__ __forceinline__ float rounded_product(float a, float b) {
 __device__ __forceinline__ float log2_weight(float z, float hi, float lo, float m) {
   if (fabsf(m) >= GKV_HUGE_LOG2) return rounded_product(z, hi) - m;
   return fmaf(fmaxf(z, -3.402823466e38f), lo, fmaf(z, hi, -m));
+}
+
+// The maximum as a prefix result holds it: -inf where there were keys, all of weight zero.
+__device__ __forceinline__ float prefix_max(float m, float sum, bool any_key) {
+  return sum == 0.f ? (any_key ? -INFINITY : GKV_NO_MAX) : m;
+}
+// Factors of the sequence's own sum of weighted values (maximum m, sum l) and of the prefix's in the joint result.  Nothing
+// attended to: 0; keys whose logits are all -inf: NaN, as softmax gives.
+struct PrefixWeight { float own, prefix; };
+__device__ __forceinline__ PrefixWeight prefix_weight(const PrefixPart& p, size_t head, float m, float l, bool any_key) {
+  float2 ms = make_float2(GKV_NO_MAX, 0.f);
+  if (p.o) ms = p.ms[head];
+  const bool there = !(ms.y == 0.f);
+  const float both = there ? fmaxf(m, ms.x) : m;
+  const float own = there ? __builtin_amdgcn_exp2f(m - both) : 1.f, prefix = there ? __builtin_amdgcn_exp2f(ms.x - both) : 0.f;
+  const float total = l * own + ms.y * prefix;
+  if (total == 0.f) return PrefixWeight{any_key || ms.x == -INFINITY ? __builtin_nanf("") : 0.f, 0.f};
+  return PrefixWeight{own / total, there ? prefix / total : 0.f};   // (0 where there is none, whatever the total: p.o may be null)
 }
 
 __device__ __forceinline__ float wave_max(float v) {

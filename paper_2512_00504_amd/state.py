@@ -52,8 +52,7 @@ class DecodeState:
         dev = torch.device(device)
         self.device = dev
         z = lambda *s, dtype: torch.zeros(*s, dtype=dtype, device=dev)
-        self.K = z(L, B, Hkv, cap, d, dtype=dt)          # rows below N_TILED tiled, the rest row-major
-        self.V = z(L, B, Hkv, cap, d, dtype=dt)
+        self._allocate_cache()
         self.pos = torch.full((L, B, Hkv, cap), -1, dtype=torch.int32, device=dev)
         self.qwin = z(w, L, B, Hq, d, dtype=dt)          # ring of the last w q tensors
         self.d_state = z(L, B, 4, dtype=torch.int32)     # {len, len_step, n_hist, n_tiled}
@@ -71,6 +70,12 @@ class DecodeState:
         # the cache length and the steps decoded since the cache was loaded or last compacted, both as
         # of the last time they were set apart; _grown rows and _stepped steps later for all of them
         self._set_host([0] * B, [0] * B)
+
+    def _allocate_cache(self):
+        cfg = self.cfg
+        shape = (cfg.n_layers, cfg.batch, cfg.n_kv_heads, cfg.capacity, cfg.head_dim)
+        # rows of K below N_TILED tiled, the rest row-major
+        self.K, self.V = (torch.zeros(shape, dtype=_TORCH_DTYPE[cfg.dtype], device=self.device) for _ in range(2))
 
     @classmethod
     def from_workload(cls, wl, device="cuda:0", params=None, **over):
@@ -160,9 +165,18 @@ class DecodeState:
         self._set_host([b if x else n for x, n in zip(done, self._len)], [0 if x else k for x, k in zip(done, self._since)])
 
     # one call each -------------------------------------------------------------------------
-    def attend_decode(self, q, k_new, v_new, step):
-        self.ctx.attend_decode(q, k_new, v_new, self.K, self.V, self.pos, step, self.qwin, self.d_state,
-                               self.len_host, self.out, self.workspace)
+    def attend_decode(self, q, k_new, v_new, step, prefix=None):
+        """prefix: a SharedPrefix, attended to together with the sequences' own rows."""
+        if prefix is None:
+            self.ctx.attend_decode(q, k_new, v_new, self.K, self.V, self.pos, step, self.qwin, self.d_state,
+                                   self.len_host, self.out, self.workspace)
+        else:
+            prefix.attend(q)
+            self.ctx.attend_decode_prefix(q, k_new, v_new, self.K, self.V, self.pos, step, self.qwin, self.d_state,
+                                          self.len_host, prefix.part, self.out, self.workspace)
+        return self._stepped_on(k_new)
+
+    def _stepped_on(self, k_new):
         if k_new is not None:
             self._grown += 1
         self._stepped += 1
@@ -202,3 +216,89 @@ class DecodeState:
         b, w = self.cfg.budget, self.cfg.window
         return (step + 1) % self.cfg.interval == 0 and any(
             n > b and k >= w for n, k in zip(self._len, self._since))
+
+
+class Q8DecodeState(DecodeState):
+    """The same with K and V held in 8 bits: K8, V8 (codes) and scales (of a row of K and of V) in place of K and V.
+
+    The redundancy term needs K in the configuration's type: redundancy_combine() reads it back into a buffer that is
+    made at its first call."""
+
+    def _allocate_cache(self):
+        cfg = self.cfg
+        shape = (cfg.n_layers, cfg.batch, cfg.n_kv_heads, cfg.capacity)
+        self.K8, self.V8 = (torch.zeros(*shape, cfg.head_dim, dtype=torch.uint8, device=self.device).view(torch.float8_e4m3fn)
+                            for _ in range(2))
+        self.scales = torch.ones(*shape, 2, dtype=torch.bfloat16, device=self.device)
+        self.K = self.V = None
+
+    def load_prompt_rows(self, t_first, k, v, t0, prompt_lens):
+        """As DecodeState's, quantised on the way."""
+        dt = self.qwin.dtype
+        lens = torch.tensor(prompt_lens, dtype=torch.int32).to(self.device)
+        self.ctx.q8_store_prompt(k.to(dt).contiguous(), v.to(dt).contiguous(), k.shape[0], t_first, t0, lens, self.K8, self.V8,
+                                 self.scales, self.pos)
+
+    def load_prefix(self, k, v, t0=0):
+        """As DecodeState's, quantised on the way."""
+        n = k.shape[0]
+        assert n <= self.cfg.budget
+        self.pos.fill_(-1)
+        self.load_prompt_rows(t0, k, v, t0 + n, [n] * self.cfg.batch)
+        self.set_state(n, t0 + n, 0, 0)
+
+    def read(self, step, K=None, V=None):
+        """The rows held before decode step `step` as a cache of the configuration's type, in the layout of d_state: into
+        K and V, or into new buffers (rows that are not held are zero then)."""
+        if K is None and V is None:
+            K, V = (torch.zeros(self.K8.shape, dtype=self.qwin.dtype, device=self.device) for _ in range(2))
+        self.ctx.q8_read(self.K8, self.V8, self.scales, self.d_state, step, K, V)
+        return K, V
+
+    def attend_decode(self, q, k_new, v_new, step, prefix=None):
+        if prefix is not None:
+            prefix.attend(q)
+        self.ctx.q8_attend_decode(q, k_new, v_new, self.K8, self.V8, self.scales, self.pos, step, self.qwin, self.d_state,
+                                  self.len_host, None if prefix is None else prefix.part, self.out, self.workspace)
+        return self._stepped_on(k_new)
+
+    def score_window(self, step):
+        self.ctx.q8_score_window(self.qwin, self.K8, self.scales, self.d_state, step, self.len_host, self.S, self.workspace)
+
+    def redundancy_combine(self, step, lam, tau, n_recent, eps=1e-8):
+        if self.K is None:
+            self.K = torch.zeros(self.K8.shape, dtype=self.qwin.dtype, device=self.device)
+        self.read(step + 1, K=self.K)
+        super().redundancy_combine(step, lam, tau, n_recent, eps)
+
+    def compact(self, step):
+        self.ctx.q8_compact(self.keep_idx, self.F, self.K8, self.V8, self.scales, self.F_hist, self.pos, self.d_state, step,
+                            self.workspace)
+        self._after_compression()
+
+    def evict(self, step):
+        self.ctx.q8_evict(self.qwin, self.K8, self.V8, self.scales, self.F_hist, self.pos, self.d_state, step, self.len_host,
+                          self.S, self.F, self.keep_idx, self.workspace)
+        self._after_compression()
+
+
+class SharedPrefix:
+    """Keys and values [L, h_kv, rows, d] of a prompt that the sequences of a DecodeState (or Q8DecodeState) share, held
+    once; with first and count, those sequences of the batch alone."""
+
+    def __init__(self, state: DecodeState, k, v, first=0, count=None, part=None):
+        """part: another SharedPrefix of the same state whose sequences are others: one step then joins both, through
+        attend() of this one and attend_decode(..., prefix=the other)."""
+        dt = state.qwin.dtype
+        self.ctx = state.ctx
+        self.K, self.V = k.to(state.device, dt).contiguous(), v.to(state.device, dt).contiguous()
+        self.rows, self.first = k.shape[2], first
+        self.count = state.cfg.batch - first if count is None else count
+        need = self.ctx.prefix_bytes(self.rows)
+        self.part = torch.zeros(need, dtype=torch.uint8, device=state.device) if part is None else part.part
+        if self.part.numel() < need:
+            raise ValueError("gkv: make the longer prefix first, its buffer holds the shorter one's pieces too")
+
+    def attend(self, q):
+        """The newest queries over the prefix; attend_decode() with a prefix does it by itself."""
+        self.ctx.prefix_attend(q, self.K, self.V, self.rows, self.rows, self.first, self.count, self.part)
