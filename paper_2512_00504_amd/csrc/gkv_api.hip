@@ -206,15 +206,17 @@ static int explicit_splits(const gkv_ctx* ctx) {
 // have 8 (2 x 64 units of 2000 fp32 rows, D = 64 18.8 -> 17.8).
 struct AttendPlan { int waves, splits, iters; };
 
-static AttendPlan attend_plan(const gkv_ctx* ctx, int asked) {
+static AttendPlan attend_plan(const gkv_ctx* ctx, int asked, bool q8 = false) {
   const GkvDims& d = ctx->dims;
-  auto fits = [&](int waves) { return gkv_attend_mfma_lds(ctx->esz, d.d, d.g, waves) <= 65000; };
+  auto fits = [&](int waves) {
+    return (q8 ? gkv_q8_attend_mfma_lds(d.d, d.g, waves) : gkv_attend_mfma_lds(ctx->esz, d.d, d.g, waves)) <= 65000;
+  };
   const int64_t units = (int64_t)d.L * d.B * d.Hkv;
-  const int row_bytes = d.d * ctx->esz;
+  const int row_bytes = q8 ? d.d : d.d * ctx->esz;
   const bool wide = row_bytes > 256;                                  // 16 KiB slices
-  const int keys = row_bytes == 128 ? 32 : 16;                        // per slice
+  const int keys = q8 ? 4096 / d.d : row_bytes == 128 ? 32 : 16;      // per slice
   const int typical = (d.b + d.s / 2 + keys - 1) / keys, full = d.cap / keys;   // slices of a unit
-  const bool long_slices = ctx->attend_tile == 32 && ctx->cfg.dtype == GKV_BF16 && d.d == 128;   // 4 wavefronts only
+  const bool long_slices = !q8 && ctx->attend_tile == 32 && ctx->cfg.dtype == GKV_BF16 && d.d == 128;   // 4 wavefronts only
   const bool may_have_8 = !wide && fits(8) && !long_slices;
   AttendPlan p{4, 1, 0};
   if (asked > 0) {
@@ -222,8 +224,8 @@ static AttendPlan attend_plan(const gkv_ctx* ctx, int asked) {
   } else if (units <= 128) {
     const int most = (int)(256 / units) < 16 ? (int)(256 / units) : 16;
     const int aim = typical > 24 * 7 ? (typical + 23) / 24 : 7, n = aim < most ? aim : most;
-    const bool bf16 = ctx->cfg.dtype == GKV_BF16;
-    const int enough = n == 2 ? (wide ? 12 : bf16 ? 40 : 30) : wide ? 9 : keys == 32 ? 10 : 18;
+    const bool bf16 = q8 || ctx->cfg.dtype == GKV_BF16;
+    const int enough = n == 2 ? (wide ? 12 : bf16 ? 40 : 30) : wide ? 9 : keys >= 32 ? 10 : 18;
     const int prompt = n == 2 && !wide ? (bf16 ? 64 : 48) : 2 * enough;
     if (n == most && typical >= enough && typical >= 20 * n && may_have_8) {
       p = AttendPlan{8, most, 8};
@@ -235,10 +237,11 @@ static AttendPlan attend_plan(const gkv_ctx* ctx, int asked) {
     if (p.splits < 2) p = AttendPlan{4, 1, 0};
   }
   const int slices = (int)((int64_t)d.cap * 2 * row_bytes / 8192);    // in units of 8 KiB, at full capacity
-  const bool more = p.splits == 1 ? (units <= 256 && slices >= (keys == 32 ? 12 : 16)) || (units > 512 && slices >= 64)
+  const bool more = p.splits == 1 ? (units <= 256 && slices >= (keys >= 32 ? 12 : 16)) || (units > 512 && slices >= 64)
                                   : asked > 0 && slices / p.splits >= 48;
   if (more && may_have_8) p.waves = 8;
   if (ctx->attend_waves > 0) p.waves = fits(ctx->attend_waves) ? ctx->attend_waves : 4;
+  if (q8 && p.waves == 16) p.waves = 8;
   return p;
 }
 
@@ -278,7 +281,11 @@ extern "C" gkv_status gkv_workspace_bytes(gkv_ctx* ctx, size_t* out_bytes) {
   // the workspace is sized for the split counts in force now: the decode call refuses a larger one
   // that was asked for, and does without one of its own choice
   ctx->ws_splits = explicit_splits(ctx);
-  ctx->ws_auto_splits = ctx->mfma_shape && !ctx->force_generic ? attend_plan(ctx, 0).splits : 1;
+  ctx->ws_auto_splits = 1;
+  if (ctx->mfma_shape && !ctx->force_generic) {
+    const int plain = attend_plan(ctx, 0).splits, q8 = attend_plan(ctx, 0, true).splits;
+    ctx->ws_auto_splits = plain > q8 ? plain : q8;
+  }
   const size_t automatic = auto_sets(ctx) * ws_partials_bytes(ctx, ctx->ws_auto_splits);
   *out_bytes = ws_ticket_bytes(ctx) + gkv_align256((size_t)ctx->dims.L * ctx->dims.B * 4) +
                gkv_align256(ws_stats_bytes(ctx)) +
@@ -433,13 +440,13 @@ static int split_set(gkv_ctx* ctx, const void* workspace, hipStream_t stream) {
 }
 
 // Where a decode call's partial results go and how its units are cut; `plan` as the library would have it.
-static gkv_status place_pieces(gkv_ctx* ctx, AttendPlan* plan, void* workspace, void* stream, GkvWorkspace* ws) {
+static gkv_status place_pieces(gkv_ctx* ctx, AttendPlan* plan, bool q8, void* workspace, void* stream, GkvWorkspace* ws) {
   int set = auto_sets(ctx);                                       // "attend_splits"
   if (ctx->attend_splits > 0) {
     if (plan->splits > ctx->ws_splits) return GKV_ERR_WORKSPACE;  // partials would not fit the workspace as sized
   } else if (plan->splits > 1) {
     set = plan->splits > ctx->ws_auto_splits ? -1 : split_set(ctx, workspace, (hipStream_t)stream);
-    if (set < 0) { *plan = attend_plan(ctx, 1); set = 0; }        // not cut
+    if (set < 0) { *plan = attend_plan(ctx, 1, q8); set = 0; }    // not cut
   }
   *ws = gkv_carve_workspace(ctx, workspace, set);
   return GKV_OK;
@@ -478,7 +485,7 @@ static gkv_status attend_decode(gkv_ctx* ctx, const void* q, const void* k_new, 
   GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
   if (use_mfma(ctx, {q, k_new, v_new, K, V, qwin, out})) {
     AttendPlan plan = attend_plan(ctx, ctx->attend_splits);
-    st = place_pieces(ctx, &plan, workspace, stream, &a.ws);
+    st = place_pieces(ctx, &plan, false, workspace, stream, &a.ws);
     if (st != GKV_OK) return st;
     a.waves = plan.waves; a.splits = plan.splits; a.split_iters = plan.iters;
     // An appending step leaves (max, sum) of every query head's softmax in the ring slot
@@ -695,6 +702,15 @@ extern "C" gkv_status gkv_q8_attend_decode(gkv_ctx* ctx, const void* q, const vo
   Q8AttendArgs a{q, k_new, v_new, (uint8_t*)K8, (uint8_t*)V8, (uint32_t*)scales, pos, step, qwin, d_state, out,
                  prefix_part(ctx, part), gkv_carve_workspace(ctx, workspace), 1, 0, 4, copies_q(ctx, q, qwin, step), 0};
   GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
+  if (use_mfma(ctx, {q, k_new, v_new, qwin, out})) {
+    AttendPlan plan = attend_plan(ctx, ctx->attend_splits, true);
+    st = place_pieces(ctx, &plan, true, workspace, stream, &a.ws);
+    if (st != GKV_OK) return st;
+    a.waves = plan.waves; a.splits = plan.splits; a.split_iters = plan.iters;
+    a.write_stats = k_new != nullptr;
+    note_stats(ctx, step, a.write_stats != 0, workspace, K8, qwin, (hipStream_t)stream);
+    return hip_status(gkv_launch_q8_attend_mfma(ln, ctx->dims, ctx->cfg.dtype, a));
+  }
   note_stats(ctx, step, false, workspace, K8, qwin, (hipStream_t)stream);
   return hip_status(gkv_launch_q8_attend_generic(ln, ctx->dims, ctx->cfg.dtype, a));
 }

@@ -170,6 +170,8 @@ struct Q8ScoreArgs {
 hipError_t gkv_launch_q8_store(const GkvLaunch& ln, const GkvDims& dm, int dtype, Q8StoreArgs a);
 hipError_t gkv_launch_q8_read(const GkvLaunch& ln, const GkvDims& dm, int dtype, Q8ReadArgs a);
 hipError_t gkv_launch_q8_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8AttendArgs& a);
+size_t gkv_q8_attend_mfma_lds(int d, int g, int waves);   // LDS of a workgroup of that kernel (bytes)
+hipError_t gkv_launch_q8_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8AttendArgs& a);
 hipError_t gkv_launch_q8_score_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8ScoreArgs& a);
 hipError_t gkv_launch_q8_compact(const GkvLaunch& ln, const GkvDims& dm, const int32_t* keep_idx, const float* F, void* K8,
                                  void* V8, uint32_t* scales, float* F_hist, int32_t* pos, int32_t* d_state, int32_t step,
