@@ -756,22 +756,39 @@ extern "C" gkv_status gkv_q8_evict(gkv_ctx* ctx, const void* qwin, void* K8, voi
 }
 
 // ---- shared prefix ---------------------------------------------------------------------------------
-// Pieces of a prefix of `rows` rows for `count` sequences: about two thousand workgroups, one a (sequence, KV head, piece), of
-// 256 rows at least.  More rows never make fewer pieces, so a buffer for more rows holds those of fewer.
-static int prefix_splits(const gkv_ctx* ctx, int rows, int count) {
-  const int64_t units = (int64_t)ctx->dims.L * count * ctx->dims.Hkv;
-  const int64_t want = 2048 / units, most = ((int64_t)rows + 255) / 256;
-  int64_t n = want < most ? want : most;
-  return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+// Pieces of a prefix of `rows` rows for `count` sequences.  More rows never make fewer pieces, so a buffer for more rows holds
+// those of fewer.
+//   Matrix cores: rows of queries in blocks of 32, at most 4 to a workgroup, and as many pieces as make about two workgroups a CU,
+//   of 128 keys at least.
+//   Plain kernel: about two thousand workgroups, one a (sequence, KV head, piece), of 256 keys at least.
+static PrefixPlan prefix_plan(const gkv_ctx* ctx, bool mfma, int rows, int count) {
+  const GkvDims& d = ctx->dims;
+  PrefixPlan p{1, 1, 1};
+  int64_t want, least;
+  if (mfma) {
+    const int64_t blocks = ((int64_t)count * d.g + 31) / 32;
+    p.tiles = (int)((blocks + 3) / 4);
+    p.blocks = (int)((blocks + p.tiles - 1) / p.tiles);
+    want = 512 / ((int64_t)d.L * d.Hkv * p.tiles);
+    least = 128;
+  } else {
+    want = 2048 / ((int64_t)d.L * count * d.Hkv);
+    least = 256;
+  }
+  const int64_t most = ((int64_t)rows + least - 1) / least;
+  const int64_t n = want < most ? want : most;
+  p.splits = (int)(n < 1 ? 1 : n > 128 ? 128 : n);
+  return p;
 }
 
 extern "C" gkv_status gkv_prefix_bytes(gkv_ctx* ctx, int32_t rows_max, size_t* out_bytes) {
   if (!ctx || !out_bytes || rows_max < 0) return GKV_ERR_INVALID_ARG;
-  size_t pieces = 0;                                              // of one KV head's share of a call, in sequences
-  for (int count = 1; count <= ctx->dims.B; ++count) {
-    const int n = prefix_splits(ctx, rows_max, count);
-    if (n > 1 && (size_t)n * count > pieces) pieces = (size_t)n * count;
-  }
+  size_t pieces = 0;                                              // of one query head of every sequence of a call
+  for (int count = 1; count <= ctx->dims.B; ++count)
+    for (int mfma = 0; mfma <= (int)ctx->mfma_shape; ++mfma) {
+      const int n = prefix_plan(ctx, mfma, rows_max, count).splits;
+      if (n > 1 && (size_t)n * count > pieces) pieces = (size_t)n * count;
+    }
   const size_t heads = (size_t)ctx->dims.L * ctx->dims.Hq;
   if (rows_max > ctx->prefix_rows) ctx->prefix_rows = rows_max;
   *out_bytes = prefix_o_bytes(ctx) + gkv_align256(heads * ctx->dims.B * sizeof(float2)) +
@@ -792,14 +809,16 @@ extern "C" gkv_status gkv_prefix_attend(gkv_ctx* ctx, const void* q, const void*
   char* p = (char*)part;
   a.o = (float*)p; p += prefix_o_bytes(ctx);
   a.ms = (float2*)p; p += gkv_align256(heads * d.B * sizeof(float2));
-  const int n = prefix_splits(ctx, rows, count);
-  a.split_rows = ((rows + n - 1) / n + 63) / 64 * 64;
+  const bool mfma = use_mfma(ctx, {q, Kp, Vp});
+  const PrefixPlan plan = prefix_plan(ctx, mfma, rows, count);
+  a.split_rows = (int)((((int64_t)rows + plan.splits - 1) / plan.splits + 63) / 64 * 64);
   if (a.split_rows < 64) a.split_rows = 64;
-  a.splits = rows > 0 ? (rows + a.split_rows - 1) / a.split_rows : 1;
+  a.splits = rows > 0 ? (int)(((int64_t)rows + a.split_rows - 1) / a.split_rows) : 1;
   a.part_o = (float*)p; p += gkv_align256((size_t)a.splits * heads * count * d.d * sizeof(float));
   a.part_ms = (float2*)p;
   GkvLaunch ln{ctx, -1, (hipStream_t)stream};
-  gkv_status st = hip_status(gkv_launch_prefix_generic(ln, d, ctx->cfg.dtype, a));
+  gkv_status st = hip_status(mfma ? gkv_launch_prefix_mfma(ln, d, ctx->cfg.dtype, a, plan)
+                                  : gkv_launch_prefix_generic(ln, d, ctx->cfg.dtype, a));
   if (st != GKV_OK || a.splits == 1) return st;
   return hip_status(gkv_launch_prefix_join(ln, d, a));
 }

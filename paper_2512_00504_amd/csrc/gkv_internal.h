@@ -185,6 +185,9 @@ struct PrefixArgs {
   float* o; float2* ms;         // [L,B,h_q,d], [L,B,h_q]
   float* part_o; float2* part_ms;   // [splits][L,count,h_q] of each
 };
+// How the matrix-core kernel's rows are dealt out: `tiles` workgroups of up to `blocks` wavefronts of 32 rows per piece.
+struct PrefixPlan { int32_t splits, tiles, blocks; };
+hipError_t gkv_launch_prefix_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a, const PrefixPlan& plan);
 hipError_t gkv_launch_prefix_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a);
 hipError_t gkv_launch_prefix_join(const GkvLaunch& ln, const GkvDims& dm, const PrefixArgs& a);
 hipError_t gkv_launch_fill_zero(hipStream_t stream, int32_t* p, size_t n);

@@ -1,0 +1,254 @@
+// Attention over a shared prefix on the matrix cores: bf16 or fp32, head_dim 64 or 128, any number of query rows.
+//
+// The rows of one (layer, KV head) are its query heads of all sequences that share the prefix: count * g of them, row
+// i * g + h.  A workgroup takes up to 4 blocks of 32 rows, a wavefront each, and a piece of the prefix, which passes through LDS in
+// tiles of TK keys, brought there once for all of its wavefronts without going through registers, two tiles in turn.
+//   S^T[key, row] = K Q^T with products over 32 keys and 32 rows: lane (row = lane % 32, h = lane / 32) gets the keys
+//   8 i + 4 h + e of its row, so the softmax stays in the lane but for one exchange with the other half, and they are what the
+//   product  O^T[channel, row] += V^T P^T  wants of P in that lane, if V's keys are taken in the same order:
+//     bf16: 16x16-transposing reads of LDS give a lane four keys of one channel;  fp32: a lane reads one channel of one key.
+//   bf16 rounds P to bf16 (to the nearest; 2^-9 of the value, and the sum is of the unrounded weights).
+// LDS holds a tile's rows as they are, their 16-byte pieces exchanged within the row so that neither kind of read finds two
+// rows in the same banks.
+// Bound: HBM with few rows; with several hundred the vector unit: 32 keys of 32 rows take 16 products (512 cycles) and about
+// 16 x (maximum, fma, exponential, sum, conversion).
+#include "gkv_internal.h"
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ u32x4 ld16(const void* p) { return *(const u32x4*)p; }
+
+// Maximum or sum over the two halves of a wavefront.
+__device__ __forceinline__ float over_halves(float x, bool max) {
+  const uint32_t u = __float_as_uint(x);
+  const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(u, u, false, false));
+  const float a = __uint_as_float(y[0]), b = __uint_as_float(y[1]);
+  return max ? fmaxf(a, b) : a + b;
+}
+
+template <typename T, int D>
+struct Geo {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int TK = F32 ? 32 : 64;                   // keys of a tile
+  static constexpr int ROW = D * (int)sizeof(T);             // bytes
+  static constexpr int CHUNKS = ROW / 16;
+  static constexpr int TILE = TK * ROW;                      // bytes of K, and of V
+  static constexpr int PIECES = TILE / 1024;                 // of K, and of V
+  static constexpr int ROWS_PIECE = 1024 / ROW;
+  // what the 16-byte chunks of a row are exchanged by
+  __device__ static __forceinline__ int k_swap(int row) { return row & (CHUNKS < 16 ? CHUNKS - 1 : 15); }
+  __device__ static __forceinline__ int v_swap(int row) {
+    if (F32) return 0;
+    return CHUNKS == 8 ? 2 * (row & 1) + 4 * ((row >> 1) & 1) : 4 * (row & 3) + 2 * ((row >> 1) & 1);
+  }
+};
+
+// A 1 KiB piece from memory to LDS, 16 bytes a lane; `lds` is uniform.  (Written out, because the compiler makes every later read of LDS
+// wait for every such request; the wait is the one before the barrier below.  Nothing else in this file uses m0.)
+__device__ __forceinline__ void to_lds(const char* base, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds), "v"(offset), "s"(base) : "memory");
+}
+
+struct KernelArgs {
+  PrefixArgs p;
+  int32_t L, B, Hq, Hkv, g, tiles, blocks, groups;          // row tiles; blocks of 32 rows per tile at most; (layer, KV head, piece)s
+  GkvDivisor by_tiles, by_splits, by_hkv, by_g;
+  float scale_hi, scale_lo;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void prefix_mfma_kernel(KernelArgs a) {
+  using G = Geo<T, D>;
+  constexpr int SUB = G::TK / 32, CB = D / 32;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];     // [2][K, V][TILE]
+  const int tid = threadIdx.x, lane = tid & 63, nw = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, h = lane >> 5;
+
+  // Workgroups go to the XCDs in turn: the row tiles of one piece of the prefix go to the same one, and find it in its L2.
+  const int eighth = blockIdx.x >> 3;
+  const int round = quotient(eighth, a.by_tiles), tile = eighth - round * a.tiles;
+  const int group = round * 8 + (blockIdx.x & 7);
+  if (group >= a.groups) return;
+  const int unit = quotient(group, a.by_splits), split = group - unit * a.p.splits;
+  const int layer = quotient(unit, a.by_hkv), j = unit - layer * a.Hkv;
+  const int n0 = split * a.p.split_rows, n1 = min(a.p.rows, n0 + a.p.split_rows);
+  const int n_tiles = (n1 - n0 + G::TK - 1) / G::TK;
+  const char* Kp = (const char*)a.p.K + (((size_t)layer * a.Hkv + j) * a.p.capacity + n0) * G::ROW;
+  const char* Vp = (const char*)a.p.V + (((size_t)layer * a.Hkv + j) * a.p.capacity + n0) * G::ROW;
+
+  const int n_rows = a.p.count * a.g;
+  const int row = (tile * a.blocks + wave) * 32 + lr, safe = min(row, n_rows - 1);
+  const int seq = quotient(safe, a.by_g);
+  const size_t head = ((size_t)layer * a.B + a.p.first + seq) * a.Hq + j * a.g + (safe - seq * a.g);
+  u32x4 q[D * sizeof(T) / 32];                               // chunks 2 c + h
+#pragma unroll
+  for (int c = 0; c < D * (int)sizeof(T) / 32; ++c) q[c] = ld16((const char*)a.p.q + head * G::ROW + (2 * c + h) * 16);
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+  auto bring = [&](int t, int buf) {
+    const int first = t * G::TK, last = n1 - n0 - 1;
+    const char* kt = Kp + (size_t)first * G::ROW;
+    const char* vt = Vp + (size_t)first * G::ROW;
+    for (int x = wave; x < G::PIECES; x += nw) {
+      const int at = x * G::ROWS_PIECE + lane / G::CHUNKS, chunk = lane % G::CHUNKS;
+      const int src = min(at, last - first);                 // rows behind the end repeat its last one
+      const uint32_t ko = src * G::ROW + (chunk ^ G::k_swap(at)) * 16, vo = src * G::ROW + (chunk ^ G::v_swap(at)) * 16;
+      to_lds(kt, ko, lds0 + buf * 2 * G::TILE + x * 1024);
+      to_lds(vt, vo, lds0 + buf * 2 * G::TILE + G::TILE + x * 1024);
+    }
+  };
+
+  float m = GKV_NO_MAX, l = 0.f;
+  f32x16 o[CB];
+#pragma unroll
+  for (int i = 0; i < CB; ++i) o[i] = f32x16{};
+  if (n_tiles > 0) bring(0, 0);
+  for (int t = 0; t < n_tiles; ++t) {
+    const int buf = t & 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wavefront's share of the tile is there
+    __syncthreads();                                         // everybody's is, and nobody reads the other buffer any more
+    if (t + 1 < n_tiles) bring(t + 1, buf ^ 1);
+    const char* Kt = smem + buf * 2 * G::TILE;
+    char* Vt = smem + buf * 2 * G::TILE + G::TILE;
+    const int there = n1 - n0 - t * G::TK;                   // keys of this tile that count
+    if (there < G::TK) {                                     // the last one: V behind the end is zero
+      for (int x = tid; x < (G::TK - there) * G::CHUNKS; x += nw * 64) *(u32x4*)(Vt + there * G::ROW + x * 16) = u32x4{0u, 0u, 0u, 0u};
+      __syncthreads();
+    }
+    f32x16 s[SUB];
+#pragma unroll
+    for (int i = 0; i < SUB; ++i) {
+      s[i] = f32x16{};
+      const char* kr = Kt + (32 * i + lr) * G::ROW;
+#pragma unroll
+      for (int c = 0; c < G::ROW / 32; ++c) {
+        const u32x4 k = ld16(kr + ((2 * c + h) ^ G::k_swap(lr)) * 16);
+        if constexpr (G::F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[e]), __uint_as_float(q[c][e]), s[i], 0, 0, 0);
+        } else {
+          s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[c]), s[i], 0, 0, 0);
+        }
+      }
+    }
+    if (there < G::TK) {
+#pragma unroll
+      for (int i = 0; i < SUB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (32 * i + 8 * (e >> 2) + 4 * h + (e & 3) >= there) s[i][e] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int i = 0; i < SUB; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[i][e]);
+    mx = over_halves(mx, true);
+    const float mn = fmaxf(m, rounded_product(mx, a.scale_hi));
+    if (__any(mn > m)) {
+      const float f = __builtin_amdgcn_exp2f(m - mn);
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < CB; ++i) o[i] *= f;
+      m = mn;
+    }
+    // bf16: the scale's lower part is 2^-25 of the exponent, below what its products are rounded by
+    if (__any(fabsf(m) >= GKV_HUGE_LOG2 && m != GKV_NO_MAX)) {
+#pragma unroll
+      for (int i = 0; i < SUB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[i][e] = log2_weight(s[i][e], a.scale_hi, a.scale_lo, m);
+    } else {
+#pragma unroll
+      for (int i = 0; i < SUB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          s[i][e] = G::F32 ? fmaf(fmaxf(s[i][e], -3.402823466e38f), a.scale_lo, fmaf(s[i][e], a.scale_hi, -m))
+                           : fmaf(s[i][e], a.scale_hi, -m);
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < SUB; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[i][e] = __builtin_amdgcn_exp2f(s[i][e]);
+        sum += s[i][e];
+      }
+    l += sum;
+#pragma unroll
+    for (int i = 0; i < SUB; ++i) {
+      if constexpr (G::F32) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const char* vr = Vt + (32 * i + 8 * (e >> 2) + 4 * h + (e & 3)) * G::ROW + lr * 4;
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb)
+            o[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float*)(vr + cb * 128), s[i][e], o[cb], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {                        // 16 keys: 8 (2 k) + 4 h + e and 8 (2 k + 1) + 4 h + e
+          u32x4 p;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            p[y] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{s[i][8 * k + 2 * y], s[i][8 * k + 2 * y + 1]}), bf16x2));
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) {
+            s16x4 v[2];
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              // lane: row 4 h + (lane % 16) / 4 of eight, piece lane % 4 of the 16 channels that its 16 lanes share
+              const int at = 32 * i + 16 * k + 8 * y + 4 * h + ((lane & 15) >> 2);
+              const int chunk = 4 * cb + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+              const char* vp = Vt + at * G::ROW + (chunk ^ G::v_swap(at)) * 16 + (lane & 1) * 8;
+              v[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)vp);
+            }
+            const u32x2 v0 = __builtin_bit_cast(u32x2, v[0]), v1 = __builtin_bit_cast(u32x2, v[1]);
+            o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, (u32x4{v0[0], v0[1], v1[0], v1[1]})),
+                                                            __builtin_bit_cast(bf16x8, p), o[cb], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+  if (row >= n_rows) return;
+  l = over_halves(l, false);
+  const bool pieces = a.p.splits > 1;
+  const size_t piece = (((size_t)split * a.L + layer) * a.p.count + seq) * a.Hq + j * a.g + (row - seq * a.g);
+  float* to = pieces ? a.p.part_o + piece * D : a.p.o + head * D;
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *(f32x4*)(to + 32 * cb + 8 * i + 4 * h) = f32x4{o[cb][4 * i], o[cb][4 * i + 1], o[cb][4 * i + 2], o[cb][4 * i + 3]};
+  if (h == 0) (pieces ? a.p.part_ms[piece] : a.p.ms[head]) = make_float2(prefix_max(m, l, n1 > n0), l);
+}
+
+template <typename T, int D>
+hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const PrefixArgs& p, const PrefixPlan& plan) {
+  KernelArgs a{p, dm.L, dm.B, dm.Hq, dm.Hkv, dm.g, plan.tiles, plan.blocks, dm.L * dm.Hkv * p.splits,
+               gkv_divisor(plan.tiles), gkv_divisor(p.splits), dm.by_hkv, gkv_divisor(dm.g), dm.scale_l2_hi, dm.scale_l2_lo};
+  const int64_t grid = (int64_t)(a.groups + 7) / 8 * 8 * plan.tiles;
+  if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+  constexpr size_t shmem = 4 * Geo<T, D>::TILE;
+  static_assert(shmem <= GKV_LDS_LIMIT, "a workgroup gets 64 KiB");
+  return gkv_launch(ln, prefix_mfma_kernel<T, D>, dim3((unsigned)grid), dim3(plan.blocks * 64), shmem, a);
+}
+
+}  // namespace
+
+hipError_t gkv_launch_prefix_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a, const PrefixPlan& plan) {
+  if (dtype == GKV_F32) return dm.d == 64 ? launch<float, 64>(ln, dm, a, plan) : launch<float, 128>(ln, dm, a, plan);
+  return dm.d == 64 ? launch<uint16_t, 64>(ln, dm, a, plan) : launch<uint16_t, 128>(ln, dm, a, plan);
+}
