@@ -722,8 +722,12 @@ extern "C" gkv_status gkv_q8_score_window(gkv_ctx* ctx, const void* qwin, const 
   gkv_status st = check_len(ctx, len_max_host, false);
   if (st == GKV_OK) st = check_q8(ctx, {K8, scales});
   if (st != GKV_OK) return st;
-  Q8ScoreArgs a{qwin, (const uint8_t*)K8, (const uint32_t*)scales, d_state, step, S, nullptr};
+  ScoreArgs a{qwin, K8, d_state, step, S, nullptr, (const uint32_t*)scales};
   GkvLaunch ln{ctx, GKV_K_SCORE, (hipStream_t)stream};
+  if (use_mfma(ctx, {qwin})) {
+    if (stats_cover_window(ctx, step, workspace, K8, qwin)) a.stats = gkv_carve_workspace(ctx, workspace).stats;
+    return hip_status(gkv_launch_score_mfma(ln, ctx->dims, ctx->cfg.dtype, a, len_max_host));
+  }
   return hip_status(gkv_launch_q8_score_generic(ln, ctx->dims, ctx->cfg.dtype, a));
 }
 

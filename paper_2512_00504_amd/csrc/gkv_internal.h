@@ -125,6 +125,7 @@ size_t gkv_attend_mfma_lds(int esz, int d, int g, int waves);
 struct ScoreArgs {
   const void* qwin; const void* K; const int32_t* d_state; int32_t step; float* S;
   const float2* stats;   // softmax statistics of the window's decode steps, or null: compute them
+  const uint32_t* scales = nullptr;   // of the rows of a K in 8 bits
 };
 hipError_t gkv_launch_score_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const ScoreArgs& a);
 hipError_t gkv_launch_score_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const ScoreArgs& a, int len_max);
@@ -163,16 +164,12 @@ struct Q8AttendArgs {
   PrefixPart prefix;
   GkvWorkspace ws; int32_t splits, split_iters, waves, copy_q, write_stats;   // as in AttendArgs
 };
-struct Q8ScoreArgs {
-  const void* qwin; const uint8_t* K8; const uint32_t* scales; const int32_t* d_state; int32_t step; float* S;
-  const float2* stats;
-};
 hipError_t gkv_launch_q8_store(const GkvLaunch& ln, const GkvDims& dm, int dtype, Q8StoreArgs a);
 hipError_t gkv_launch_q8_read(const GkvLaunch& ln, const GkvDims& dm, int dtype, Q8ReadArgs a);
 hipError_t gkv_launch_q8_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8AttendArgs& a);
 size_t gkv_q8_attend_mfma_lds(int d, int g, int waves);   // LDS of a workgroup of that kernel (bytes)
 hipError_t gkv_launch_q8_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8AttendArgs& a);
-hipError_t gkv_launch_q8_score_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8ScoreArgs& a);
+hipError_t gkv_launch_q8_score_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const ScoreArgs& a);
 hipError_t gkv_launch_q8_compact(const GkvLaunch& ln, const GkvDims& dm, const int32_t* keep_idx, const float* F, void* K8,
                                  void* V8, uint32_t* scales, float* F_hist, int32_t* pos, int32_t* d_state, int32_t step,
                                  int32_t* state_ticket);

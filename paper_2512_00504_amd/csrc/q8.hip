@@ -245,7 +245,7 @@ __global__ __launch_bounds__(NWG * 64) void q8_attend_generic_kernel(GkvDims dm,
 // added up in wavefront order.
 // Dynamic LDS, per wavefront: float z[cap]; float rowmax[cap]; float sacc[cap]; float qs[d]
 template <typename T>
-__global__ void q8_score_generic_kernel(GkvDims dm, Q8ScoreArgs a) {
+__global__ void q8_score_generic_kernel(GkvDims dm, ScoreArgs a) {
   const int step = resolve_step(dm, a.step);
   extern __shared__ float smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nw = blockDim.x >> 6;
@@ -260,7 +260,7 @@ __global__ void q8_score_generic_kernel(GkvDims dm, Q8ScoreArgs a) {
   const int l = compression_length(st, step, dm.b, w, cap);
   if (l == 0) return;
   const int c = l - w;
-  const uint8_t* Kh = a.K8 + (size_t)unit * cap * d;
+  const uint8_t* Kh = (const uint8_t*)a.K + (size_t)unit * cap * d;
   const uint32_t* scales = a.scales + (size_t)unit * cap;
   for (int n = lane; n < c; n += 64) sacc[n] = 0.f;
   for (int k = wave; k < w; k += nw) {
@@ -325,7 +325,7 @@ hipError_t gkv_launch_q8_attend_generic(const GkvLaunch& ln, const GkvDims& dm, 
   return gkv_launch(ln, q8_attend_generic_kernel<uint16_t>, dim3(units), dim3(NWG * 64), shmem, dm, a);
 }
 
-hipError_t gkv_launch_q8_score_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8ScoreArgs& a) {
+hipError_t gkv_launch_q8_score_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const ScoreArgs& a) {
   const int units = dm.L * dm.B * dm.Hkv;
   const size_t per_wave = sizeof(float) * (3 * (size_t)dm.cap + dm.d);
   int nw = (int)(GKV_LDS_LIMIT / per_wave);

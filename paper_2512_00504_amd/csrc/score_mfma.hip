@@ -27,7 +27,7 @@
 // Blocks of rows: a window of more than 8 rows takes 16 lanes per head and 16 window rows (block =
 // one head); up to 8 rows, two heads share a block.  Rows beyond the window or the group have a
 // huge offset and add nothing.
-#include "gkv_internal.h"
+#include "e4m3.h"
 
 #include <type_traits>
 
@@ -53,6 +53,37 @@ struct Geo {
 
 template <typename T, int D> using Tile = u32x4[Geo<T, D>::NL];
 
+// A tile of K as it is loaded.  K8: codes of 8 bits, 16 channels a piece, and behind them the scales' words (see e4m3.h): those of
+// keys 4 kb .. 4 kb + 3 where the lanes of a quarter share their keys, that of key r where each lane has one (KEY_A_LANE).
+template <typename T, int D, bool K8> using Raw = u32x4[K8 ? D / 64 + 1 : Geo<T, D>::NL];
+// Where piece c of a query row begins for lane kb (bytes): the channels that the piece of K has.
+template <typename T, bool K8>
+__device__ __forceinline__ int query_piece(int c, int kb) {
+  constexpr int PER = sizeof(T);                             // pieces of 16 bytes that 16 channels take: 2 or 4
+  return K8 ? (c / PER) * 64 * PER + kb * 16 * PER + (c % PER) * 16 : c * 64 + kb * 16;
+}
+template <typename T, int D>
+__device__ __forceinline__ void expand(Tile<T, D>& k, const Raw<T, D, true>& raw) {
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x[4];
+        q8_values(raw[c][i], x);
+        k[4 * c + i] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        k[2 * c + i] = u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i], 1.0f, false)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i], 1.0f, true)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i + 1], 1.0f, false)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i + 1], 1.0f, true))};
+    }
+  }
+}
+
 // A operand of tile t: lane (row r, kb) gets chunk 4c+kb of key 16t+r; tiled tiles are
 // lane-contiguous, row-major tiles (rows appended since the last compaction) are not.
 template <typename T, int D, bool ONCE = false>
@@ -63,6 +94,17 @@ __device__ __forceinline__ void load_k_tile(Tile<T, D>& kA, const char* Kh, int 
 #pragma unroll
   for (int c = 0; c < Geo<T, D>::NL; ++c)
     kA[c] = ONCE ? __builtin_nontemporal_load((const u32x4*)(p + c * step_off)) : ld16(p + c * step_off);
+}
+template <typename T, int D, bool ONCE, bool KEY_A_LANE>
+__device__ __forceinline__ void load_k8_tile(Raw<T, D, true>& k, const char* Kh, const uint32_t* scales, int t, int n_tiled, int lane, int r, int kb) {
+  const bool tiled = 16 * t < n_tiled;
+  const char* p = Kh + (size_t)t * 16 * D + (tiled ? lane * 16 : r * D + kb * 16);
+  const int step_off = tiled ? 1024 : 64;
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c)
+    k[c] = ONCE ? __builtin_nontemporal_load((const u32x4*)(p + c * step_off)) : ld16(p + c * step_off);
+  if constexpr (KEY_A_LANE) k[D / 64] = u32x4{scales[16 * t + r], 0u, 0u, 0u};
+  else k[D / 64] = ld16(scales + 16 * t + 4 * kb);
 }
 
 // logits[row, key] of 16 staged rows and 16 keys: lane (key = lane % 16, kb) gets rows 4 kb + e
@@ -132,7 +174,8 @@ struct ScorePlan {
 // Dynamic LDS: q pieces [nt_pass*n_blk][NL][1 KiB]; float row_hi[rows], row_lo[rows]; float sbuf[cap] if
 // use_sbuf; and, when the row statistics are computed here, float2 red_ms[NW][rows].
 // HAVE_STATS: a.stats holds (max, sum) of every window row, recorded by the decode kernel.
-template <typename T, int D, int NW, int KT, bool HAVE_STATS>
+// K8: the keys are codes of 8 bits; a key's scale, a power of two, goes into the logits' factor.
+template <typename T, int D, int NW, int KT, bool HAVE_STATS, bool K8>
 __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreArgs a, ScorePlan pl) {
   using G = Geo<T, D>;
   constexpr int NL = G::NL;
@@ -170,11 +213,11 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
   auto fetch_queries = [&](int nt0, int nts) {
     for (int nt = 0; nt < nts; ++nt) {
       const int k = min(pair ? (r & 7) : 16 * (nt0 + nt) + r, w - 1);
-      const char* row = (const char*)a.qwin + ring_row(0, k) * G::ROW_BYTES + kb * 16;
+      const char* row = (const char*)a.qwin + ring_row(0, k) * G::ROW_BYTES;
       for (int x = wave; x < pl.n_blk * NL; x += NW) {
         const int i = x / NL, c = x % NL;
         const int h = min(pair ? 2 * i + (r >> 3) : i, g - 1);
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(row + h * G::ROW_BYTES + c * 64),
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(row + h * G::ROW_BYTES + query_piece<T, K8>(c, kb)),
                                          (__attribute__((address_space(3))) void*)(qs + (size_t)(nt * pl.n_blk * NL + x) * 1024), 16, 0, 0);
       }
     }
@@ -191,8 +234,24 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
   const int l = compression_length(seq, a.step, dm.b, w, cap);
   const int cc = l - w;                     // number of candidates
 
-  const char* Kh = (const char*)a.K + (size_t)unit * cap * G::ROW_BYTES;
-  const float s_hi = dm.scale_l2_hi, s_lo = dm.scale_l2_lo;
+  const char* Kh = (const char*)a.K + (size_t)unit * cap * (K8 ? D : G::ROW_BYTES);
+  const uint32_t* scales = K8 ? a.scales + (size_t)unit * cap : nullptr;
+  const float hi = dm.scale_l2_hi, lo = dm.scale_l2_lo;
+  // a tile: f(operand, the logits' factor as hi + lo)
+  auto load_tile = [&](Raw<T, D, K8>& k, int t) {
+    if constexpr (K8) load_k8_tile<T, D, false, true>(k, Kh, scales, t, seq.n_tiled, lane, r, kb);
+    else load_k_tile<T, D>(k, Kh, t, seq.n_tiled, lane, r, kb);
+  };
+  auto opened = [&](const Raw<T, D, K8>& raw, auto f) {
+    if constexpr (K8) {
+      Tile<T, D> k;
+      expand<T, D>(k, raw);
+      const float scale = q8_k_scale(raw[D / 64][0]);
+      f(k, hi * scale, lo * scale);
+    } else {
+      f(raw, hi, lo);
+    }
+  };
   float* So = a.S + (size_t)unit * cap;
 
   // this workgroup's groups of KT candidate tiles
@@ -212,10 +271,10 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
       __syncthreads();                      // the previous pass has been read
       fetch_queries(nt0, nts);
     }
-    u32x4 kA[KT][NL], kN[KT][NL];
-    auto load_group = [&](u32x4 (&k)[KT][NL], int p) {
+    Raw<T, D, K8> kA[KT], kN[KT];
+    auto load_group = [&](Raw<T, D, K8> (&k)[KT], int p) {
 #pragma unroll
-      for (int tt = 0; tt < KT; ++tt) load_k_tile<T, D>(k[tt], Kh, p * KT + tt, seq.n_tiled, lane, r, kb);
+      for (int tt = 0; tt < KT; ++tt) load_tile(k[tt], p * KT + tt);
     };
     if (HAVE_STATS && g0 + wave < g1) load_group(kA, g0 + wave);
     auto store_offset = [&](int x, float m, float s) {
@@ -254,7 +313,7 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
             rm[i][e] = GKV_NO_MAX; rs[i][e] = 0.f;
             last_vis[i][e] = cc + k_of(16 * min(b0 + i, n_blocks - 1) + 4 * kb + e, nt0);
           }
-        auto stats_tile = [&](const u32x4 (&kA)[NL], int t, auto exact) {
+        auto stats_tile = [&](const Raw<T, D, K8>& raw, int t, auto exact) { opened(raw, [&](const Tile<T, D>& kA, float s_hi, float s_lo) {
           constexpr bool EXACT = decltype(exact)::value;
           const int key = 16 * t + r;
 #pragma unroll
@@ -265,22 +324,24 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               // a key the row did not see has the logit -inf: it never becomes the maximum and adds 0
-              if (EXACT && key > last_vis[i][e]) z[e] = -INFINITY;
-              add_to_stats<EXACT>(z[e], s_hi, s_lo, rm[i][e], rs[i][e]);
+              // (nor does its scale, which may be anything behind the last row)
+              const bool unseen = EXACT && key > last_vis[i][e];
+              if (unseen) z[e] = -INFINITY;
+              add_to_stats<EXACT>(z[e], K8 && unseen ? hi : s_hi, K8 && unseen ? lo : s_lo, rm[i][e], rs[i][e]);
             }
           }
-        };
+        }); };
         auto exact_tiles = [&](int t0) {
           for (int t = t0; t < n_tiles; t += NW) {
-            u32x4 kA[NL];
-            load_k_tile<T, D>(kA, Kh, t, seq.n_tiled, lane, r, kb);
+            Raw<T, D, K8> kA;
+            load_tile(kA, t);
             stats_tile(kA, t, std::true_type{});
           }
         };
         int t = wave;
         for (; t < n_full; t += NW) {
-          u32x4 kA[NL];
-          load_k_tile<T, D>(kA, Kh, t, seq.n_tiled, lane, r, kb);
+          Raw<T, D, K8> kA;
+          load_tile(kA, t);
           stats_tile(kA, t, std::false_type{});
         }
         bool again = false;
@@ -345,9 +406,10 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
     if (__any(huge)) {
       // seldom: a tile at a time, by the wavefront that has it in the other passes too
       for (int t = (g0 + wave) * KT; t < g1 * KT; t = t % KT == KT - 1 ? t + (NW - 1) * KT + 1 : t + 1) {
-        u32x4 kT[NL];
-        load_k_tile<T, D>(kT, Kh, t, seq.n_tiled, lane, r, kb);
+        Raw<T, D, K8> raw;
+        load_tile(raw, t);
         float tot = 0.f;
+        opened(raw, [&](const Tile<T, D>& kT, float s_hi, float s_lo) {
 #pragma unroll 1
         for (int nt = 0; nt < nts; ++nt) {
           f32x4 ymax = {-1e30f, -1e30f, -1e30f, -1e30f};
@@ -365,6 +427,7 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
 #pragma unroll
           for (int e = 0; e < 4; ++e) tot += __builtin_amdgcn_exp2f(pair ? fmaxf(ymax[e], __shfl_xor(ymax[e], 32)) : ymax[e]);
         }
+        });
         finish(tot, t);
       }
       continue;
@@ -375,8 +438,18 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
       // the same number of requests in flight on every path keeps the wait for this group short)
       load_group(kN, min(p + NW, g1 - 1));
       float tot[KT];
+      Tile<T, D> open[K8 ? KT : 1];
+      float t_hi[KT], t_lo[KT];
 #pragma unroll
-      for (int tt = 0; tt < KT; ++tt) tot[tt] = 0.f;
+      for (int tt = 0; tt < KT; ++tt) {
+        tot[tt] = 0.f;
+        t_hi[tt] = hi; t_lo[tt] = lo;
+        if constexpr (K8) {
+          const float scale = q8_k_scale(kA[tt][D / 64][0]);
+          expand<T, D>(open[tt], kA[tt]);
+          t_hi[tt] *= scale; t_lo[tt] *= scale;
+        }
+      }
       for (int nt = 0; nt < nts; ++nt) {
         f32x4 ymax[KT];
 #pragma unroll
@@ -389,10 +462,12 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
 #pragma unroll
           for (int tt = 0; tt < KT; ++tt) {
             // candidates are visible to every window row; keys >= cc are discarded below
-            const f32x4 z = logits<T, NL>(q, kA[tt]);
+            f32x4 z;
+            if constexpr (K8) z = logits<T, NL>(q, open[tt]);
+            else z = logits<T, NL>(q, kA[tt]);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              ymax[tt][e] = fmaxf(ymax[tt][e], log2_score<false>(z[e], s_hi, s_lo, c_hi[e], c_lo[e]));
+              ymax[tt][e] = fmaxf(ymax[tt][e], log2_score<false>(z[e], t_hi[tt], t_lo[tt], c_hi[e], c_lo[e]));
           }
         }
 #pragma unroll
@@ -410,7 +485,7 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
 #pragma unroll
       for (int tt = 0; tt < KT; ++tt)
 #pragma unroll
-        for (int c = 0; c < NL; ++c) kA[tt][c] = kN[tt][c];
+        for (int c = 0; c < (int)(sizeof(kA[tt]) / 16); ++c) kA[tt][c] = kN[tt][c];
     }
   }
 }
@@ -428,7 +503,7 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
 // g = 7, w = 16 20.8 -> 17.8 us; 4 units 11.1 -> 5.8 us.  Against the plain kernel: bf16 D = 64, 128 units
 // 2780 -> 7.4 us; fp32 D = 128, 32 units 3495 -> 14.1 us (kernel above, bound by fp32 MFMAs).
 // Dynamic LDS: q pieces [NT*NB][NL][1 KiB]; float2 row_c[16*NT*NB]; OWN: float2 red_ms[NW][16*NT*NB].
-template <int D, int NW, int NB, int NT, bool ONCE, bool OWN>
+template <int D, int NW, int NB, int NT, bool ONCE, bool OWN, bool K8>
 __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, ScoreArgs a, int pair, int ksplit, GkvDivisor by_ksplit) {
   using T = uint16_t;
   using G = Geo<T, D>;
@@ -465,7 +540,7 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
     const int blk = x / NL, c = x % NL;
     int h, k;
     row_src(blk / NB, blk % NB, r, h, k);
-    const char* src = (const char*)a.qwin + ring_row(h, k) * G::ROW_BYTES + (4 * c + kb) * 16;
+    const char* src = (const char*)a.qwin + ring_row(h, k) * G::ROW_BYTES + query_piece<T, K8>(c, kb);
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
                                      (__attribute__((address_space(3))) void*)(qs + x * 1024), 16, 0, 0);
   }
@@ -484,7 +559,12 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
   const int tiles = l == 0 ? 0 : (cc + 15) >> 4;
   const int per_share = (tiles + ksplit - 1) / ksplit;
   const int g0 = share * per_share, g1 = min(tiles, g0 + per_share);
-  const char* Kh = (const char*)a.K + (size_t)unit * cap * G::ROW_BYTES;
+  const char* Kh = (const char*)a.K + (size_t)unit * cap * (K8 ? D : G::ROW_BYTES);
+  const uint32_t* scales = K8 ? a.scales + (size_t)unit * cap : nullptr;
+  auto load_tile = [&](Raw<T, D, K8>& k, int t, auto once) {
+    if constexpr (K8) load_k8_tile<T, D, decltype(once)::value, false>(k, Kh, scales, t, seq.n_tiled, lane, r, kb);
+    else load_k_tile<T, D, decltype(once)::value>(k, Kh, t, seq.n_tiled, lane, r, kb);
+  };
   // Two tiles on their way while a third is worked on where K comes from memory and the registers allow it: 1792
   // units of 1152 rows, g = 7 124 -> 114 us, g = 8 117 -> 103, g = 4 100 -> 97; K within the memory-side cache 30.3 -> 29.7
   // (896 units), 64 units 6.7 -> 7.0; ten blocks of 128 bytes 72 -> 79.  A fourth: 115, 114, 99.
@@ -492,27 +572,45 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
   // objects where the rows' own statistics come first: with the array that pass took 8 to 34 registers more, and 38
   // spilled took 18432 units, g = 5, w = 32 from 2480 to 4530 us.
   constexpr int DEPTH = ONCE && NT * NB <= 8 ? 3 : 2;
-  Tile<T, D> kA, kN, ring[DEPTH];
+  Raw<T, D, K8> kA, kN, ring[DEPTH];
   const int n_full = OWN ? (cc + 1) >> 4 : 0;            // tiles whose keys every window row sees
   if constexpr (OWN) {
-    if (wave < n_full) load_k_tile<T, D>(kA, Kh, wave, seq.n_tiled, lane, r, kb);
+    if (wave < n_full) load_tile(kA, wave, std::false_type{});
   } else {
-    if (g0 + wave < g1) load_k_tile<T, D, ONCE>(ring[0], Kh, g0 + wave, seq.n_tiled, lane, r, kb);
+    if (g0 + wave < g1) load_tile(ring[0], g0 + wave, std::bool_constant<ONCE>{});
     if (tid < NT * NB * 16) row_c[tid] = row_offset(row_valid, ms.x, ms.y);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the queries are in LDS
   __syncthreads();
   if (g0 >= g1) return;
-  const float s_hi = dm.scale_l2_hi, s_lo = dm.scale_l2_lo;
+  // a tile: f(operand, the logits' factors of keys 4 kb + e as hi + lo)
+  auto opened = [&](const Raw<T, D, K8>& raw, auto f) {
+    const float hi = dm.scale_l2_hi, lo = dm.scale_l2_lo;
+    if constexpr (K8) {
+      Tile<T, D> k;
+      expand<T, D>(k, raw);
+      f32x4 s_hi, s_lo;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float scale = q8_k_scale(raw[D / 64][e]);
+        s_hi[e] = hi * scale; s_lo[e] = lo * scale;
+      }
+      f(k, s_hi, s_lo);
+    } else {
+      f(raw, f32x4{hi, hi, hi, hi}, f32x4{lo, lo, lo, lo});
+    }
+  };
   u32x4 q[NT * NB][NL];
   auto load_q = [&](u32x4 (&x)[NL], int b) {
 #pragma unroll
     for (int c = 0; c < NL; ++c) x[c] = *(const u32x4*)(qs + (b * NL + c) * 1024 + lane * 16);
   };
   // ten blocks of 16 x 256 bytes and the first pass of OWN need more registers than there are: it takes two of them from LDS each time
-  constexpr int HELD = OWN && NL == 4 && NT * NB > 8 ? 8 : NT * NB;
+  constexpr int HELD = OWN && NL == 4 && NT * NB > 8 ? (K8 ? 7 : 8) : NT * NB;
+  // and with a key's factors and the operands that its codes become so does the second pass
+  constexpr int STAY = K8 && NL == 4 && NT * NB > 8 ? 8 : NT * NB;
 #pragma unroll
-  for (int b = 0; b < HELD; ++b) load_q(q[b], b);
+  for (int b = 0; b < (HELD < STAY ? HELD : STAY); ++b) load_q(q[b], b);
 
   if constexpr (OWN) {
     // ---- the rows' own statistics: a first pass over all keys, a row's (max, sum) in four lanes --------
@@ -521,10 +619,11 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
 #pragma unroll
       for (int b = 0; b < NT * NB; ++b) { rm[b] = GKV_NO_MAX; rs[b] = 0.f; }
     };
-    auto stats_tile = [&](const Tile<T, D>& kT, int t, auto exact) {
+    auto stats_tile = [&](const Raw<T, D, K8>& raw, int t, auto exact) { opened(raw, [&](const Tile<T, D>& kT, const f32x4& t_hi, const f32x4& t_lo) {
       constexpr bool EXACT = decltype(exact)::value;
 #pragma unroll
       for (int b = 0; b < NT * NB; ++b) {
+        f32x4 s_hi = t_hi, s_lo = t_lo;
         if (b >= HELD) {
           asm volatile("" ::: "memory");                 // read here, not once before the loop
           load_q(q[b], b);
@@ -535,9 +634,15 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
           const int seen = cc + (pair ? (r & 7) : 16 * (b / NB) + r);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (16 * t + 4 * kb + e > seen) z[e] = -INFINITY;
+            if (16 * t + 4 * kb + e > seen) {
+              z[e] = -INFINITY;
+              if constexpr (K8) { s_hi[e] = dm.scale_l2_hi; s_lo[e] = dm.scale_l2_lo; }   // (a scale behind the last row may be anything)
+            }
         }
-        const float tm = rounded_product(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), s_hi);
+        // (one product where the keys share their factor)
+        const float tm = K8 ? fmaxf(fmaxf(rounded_product(z[0], s_hi[0]), rounded_product(z[1], s_hi[1])),
+                                    fmaxf(rounded_product(z[2], s_hi[2]), rounded_product(z[3], s_hi[3])))
+                            : rounded_product(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), s_hi[0]);
         if (__any(tm > rm[b])) {
           const float mnew = fmaxf(rm[b], tm);
           rs[b] *= __builtin_amdgcn_exp2f(rm[b] - mnew);
@@ -545,24 +650,24 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          rs[b] += __builtin_amdgcn_exp2f(EXACT ? log2_weight(z[e], s_hi, s_lo, rm[b])
-                                                : fmaf(z[e], s_lo, fmaf(z[e], s_hi, -rm[b])));
+          rs[b] += __builtin_amdgcn_exp2f(EXACT ? log2_weight(z[e], s_hi[e], s_lo[e], rm[b])
+                                                : fmaf(z[e], s_lo[e], fmaf(z[e], s_hi[e], -rm[b])));
       }
-    };
+    }); };
     const int n_tiles = (l + 15) >> 4;
     auto exact_tiles = [&](int t0) {
       for (int t = t0; t < n_tiles; t += NW) {
-        Tile<T, D> kT;
-        load_k_tile<T, D>(kT, Kh, t, seq.n_tiled, lane, r, kb);
+        Raw<T, D, K8> kT;
+        load_tile(kT, t, std::false_type{});
         stats_tile(kT, t, std::true_type{});
       }
     };
     reset();
     for (int t = wave; t < n_full; t += 2 * NW) {
-      load_k_tile<T, D>(kN, Kh, min(t + NW, n_full - 1), seq.n_tiled, lane, r, kb);
+      load_tile(kN, min(t + NW, n_full - 1), std::false_type{});
       stats_tile(kA, t, std::false_type{});
       if (t + NW >= n_full) break;
-      load_k_tile<T, D>(kA, Kh, min(t + 2 * NW, n_full - 1), seq.n_tiled, lane, r, kb);
+      load_tile(kA, min(t + 2 * NW, n_full - 1), std::false_type{});
       stats_tile(kN, t + NW, std::false_type{});
     }
     bool again = false;
@@ -570,7 +675,7 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
     for (int b = 0; b < NT * NB; ++b) again |= stats_in_doubt(rm[b], rs[b]);
     if (__any(again)) reset();
     exact_tiles(__any(again) ? wave : n_full + (wave + NW - n_full % NW) % NW);
-    if (g0 + wave < g1) load_k_tile<T, D>(kA, Kh, g0 + wave, seq.n_tiled, lane, r, kb);
+    if (g0 + wave < g1) load_tile(kA, g0 + wave, std::false_type{});
     float2* red_ms = row_c + NT * NB * 16;               // [NW][rows]
 #pragma unroll
     for (int b = 0; b < NT * NB; ++b) {
@@ -594,7 +699,7 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
       row_c[tid] = row_offset(row_valid, M, Z);
     }
 #pragma unroll
-    for (int b = HELD; b < NT * NB; ++b) load_q(q[b], b);
+    for (int b = HELD; b < STAY; ++b) load_q(q[b], b);
     __syncthreads();
   }
   const float mean = 0x1p-3f / (float)w;
@@ -622,7 +727,7 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
     const float2 c = row_c[16 * b + r];
     c_hi[b] = c.x; c_lo[b] = c.y;
   }
-  auto tile = [&](const Tile<T, D>& kT, int t) {
+  auto tile = [&](const Raw<T, D, K8>& raw, int t) { opened(raw, [&](const Tile<T, D>& kT, const f32x4& s_hi, const f32x4& s_lo) {
     f32x4 tot = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -630,10 +735,14 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         const int b = nt * NB + i;
+        if (b >= STAY) {
+          asm volatile("" ::: "memory");                   // read here, not once before the loop
+          load_q(q[b], b);
+        }
         const f32x4 z = logits<T, NL>(kT, q[b]);           // lane (row r, kb): keys 4 kb + e
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          ymax[e] = fmaxf(ymax[e], log2_score<false>(z[e], s_hi, s_lo, c_hi[b], c_lo[b]));
+          ymax[e] = fmaxf(ymax[e], log2_score<false>(z[e], s_hi[e], s_lo[e], c_hi[b], c_lo[b]));
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -643,10 +752,10 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
       }
     }
     finish(tot, t);
-  };
+  }); };
   // the tiles in turn: the next ones are always requested before one is worked on, and stay where they land
   // (copied over at the end of each round instead: 121 -> 117 us at 1792 units of b = 1024)
-  auto request = [&](Tile<T, D>& kT, int t) { load_k_tile<T, D, ONCE>(kT, Kh, min(t, g1 - 1), seq.n_tiled, lane, r, kb); };
+  auto request = [&](Raw<T, D, K8>& kT, int t) { load_tile(kT, min(t, g1 - 1), std::bool_constant<ONCE>{}); };
   if constexpr (OWN) {
     for (int t = g0 + wave; t < g1; t += 2 * NW) {
       request(kN, t + NW);
@@ -673,9 +782,10 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
   if (__any(huge)) {
     // seldom: block by block from LDS, a tile at a time, over what the loop above stored
     for (int t = g0 + wave; t < g1; t += NW) {
-      Tile<T, D> kT;
-      load_k_tile<T, D>(kT, Kh, t, seq.n_tiled, lane, r, kb);
+      Raw<T, D, K8> raw;
+      load_tile(raw, t, std::false_type{});
       f32x4 tot = {0.f, 0.f, 0.f, 0.f};
+      opened(raw, [&](const Tile<T, D>& kT, const f32x4& s_hi, const f32x4& s_lo) {
 #pragma unroll 1
       for (int nt = 0; nt < NT; ++nt) {
         f32x4 ymax = {-1e30f, -1e30f, -1e30f, -1e30f};
@@ -686,12 +796,13 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
           const float2 c = row_c[16 * b + r];
           const f32x4 z = logits<T, NL>(kT, qb);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) ymax[e] = fmaxf(ymax[e], log2_score<true>(z[e], s_hi, s_lo, c.x, c.y));
+          for (int e = 0; e < 4; ++e) ymax[e] = fmaxf(ymax[e], log2_score<true>(z[e], s_hi[e], s_lo[e], c.x, c.y));
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           tot[e] += __builtin_amdgcn_exp2f(pair ? fmaxf(ymax[e], GKV_DPP_F(ymax[e], 0x128)) : ymax[e]);
       }
+      });
       finish(tot, t);
     }
   }
@@ -703,20 +814,20 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
 // 2176 rows, g = 8 91 -> 32; 256 of 1088, g = 5, w = 32 127 -> 38; 896 of 640, g = 7, w = 16 122 -> 73; 18432 of 1088,
 // g = 5, w = 32 4670 -> 2480.  Bound: the arithmetic of two passes (the second alone, with recorded statistics:
 // 38 us at 896 units).
-template <int D, int NB, int NT>
+template <int D, int NB, int NT, bool K8>
 hipError_t launch_regs_own(const GkvLaunch& ln, const GkvDims& dm, const ScoreArgs& a, int len_max, bool pair) {
   constexpr int NW = 8, ROWS = NT * NB * 16;
   const int units = dm.L * dm.B * dm.Hkv;
   const int tiles = (len_max + 15) / 16, most = (tiles + NW - 1) / NW;
   int ksplit = 256 / units;
   ksplit = ksplit < 1 ? 1 : (ksplit > most ? (most < 1 ? 1 : most) : ksplit);
-  return gkv_launch(ln, score_regs_kernel<D, NW, NB, NT, false, true>, dim3(units * ksplit), dim3(NW * 64),
+  return gkv_launch(ln, score_regs_kernel<D, NW, NB, NT, false, true, K8>, dim3(units * ksplit), dim3(NW * 64),
                     (size_t)ROWS * (Geo<uint16_t, D>::ROW_BYTES + 8 + 8 * NW), dm, a, (int)pair, ksplit, gkv_divisor(ksplit));
 }
 
-template <int D, int NB, int NT>
+template <int D, int NB, int NT, bool K8>
 hipError_t launch_regs(const GkvLaunch& ln, const GkvDims& dm, const ScoreArgs& a, int len_max, bool pair) {
-  if (!a.stats) return launch_regs_own<D, NB, NT>(ln, dm, a, len_max, pair);
+  if (!a.stats) return launch_regs_own<D, NB, NT, K8>(ln, dm, a, len_max, pair);
   constexpr int NW = 4;
   const int units = dm.L * dm.B * dm.Hkv;
   // Two workgroups of 4 wavefronts fit a CU at these register counts: fewer than 512 units are cut into
@@ -728,25 +839,25 @@ hipError_t launch_regs(const GkvLaunch& ln, const GkvDims& dm, const ScoreArgs& 
   // K beyond the 256 MiB memory-side cache is read with non-temporal loads: right after a decode step
   // 80 -> 67 us at 280 MB of K (1792 units), 134 -> 113 us at 504 MB, 305 -> 285 us at 1.2 GB; at 70 and
   // 140 MB there is no difference then, and a second reader of the same K finds it cached.
-  const bool once = (size_t)units * len_max * Geo<uint16_t, D>::ROW_BYTES > (size_t)256 << 20;
-  auto kern = once ? score_regs_kernel<D, NW, NB, NT, true, false> : score_regs_kernel<D, NW, NB, NT, false, false>;
+  const bool once = (size_t)units * len_max * (K8 ? D : Geo<uint16_t, D>::ROW_BYTES) > (size_t)256 << 20;
+  auto kern = once ? score_regs_kernel<D, NW, NB, NT, true, false, K8> : score_regs_kernel<D, NW, NB, NT, false, false, K8>;
   return gkv_launch(ln, kern, dim3(units * ksplit), dim3(NW * 64),
                     (size_t)NT * NB * (Geo<uint16_t, D>::TILE_BYTES + 128), dm, a, (int)pair, ksplit, gkv_divisor(ksplit));
 }
 
 // false: no such instantiation
-template <int D>
+template <int D, bool K8>
 bool try_launch_regs(const GkvLaunch& ln, const GkvDims& dm, const ScoreArgs& a, int len_max, hipError_t* e) {
   const bool pair = dm.w <= 8;
   const int nb = pair ? (dm.g + 1) / 2 : dm.g, nt = pair ? 1 : (dm.w + 15) / 16;
-#define GKV_CASE(NB_, NT_) if (nb == NB_ && nt == NT_) { *e = launch_regs<D, NB_, NT_>(ln, dm, a, len_max, pair); return true; }
+#define GKV_CASE(NB_, NT_) if (nb == NB_ && nt == NT_) { *e = launch_regs<D, NB_, NT_, K8>(ln, dm, a, len_max, pair); return true; }
   GKV_CASE(1, 1) GKV_CASE(2, 1) GKV_CASE(3, 1) GKV_CASE(4, 1) GKV_CASE(5, 1) GKV_CASE(6, 1) GKV_CASE(7, 1) GKV_CASE(8, 1)
   GKV_CASE(1, 2) GKV_CASE(2, 2) GKV_CASE(3, 2) GKV_CASE(4, 2) GKV_CASE(5, 2)
 #undef GKV_CASE
   return false;
 }
 
-template <typename T, int D, int NW, int KT>
+template <typename T, int D, int NW, int KT, bool K8>
 hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const ScoreArgs& a, int len_max) {
   using G = Geo<T, D>;
   const int units = dm.L * dm.B * dm.Hkv;
@@ -765,7 +876,7 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const ScoreArgs& a, in
   const size_t rows = (size_t)pl.nt_pass * pl.n_blk * 16;
   const size_t shmem = rows * G::ROW_BYTES + rows * 8 + (pl.use_sbuf ? 4 * (size_t)dm.cap : 0) +
                        (a.stats ? 0 : NW * rows * 8);
-  auto kern = a.stats ? score_mfma_kernel<T, D, NW, KT, true> : score_mfma_kernel<T, D, NW, KT, false>;
+  auto kern = a.stats ? score_mfma_kernel<T, D, NW, KT, true, K8> : score_mfma_kernel<T, D, NW, KT, false, K8>;
   if (shmem > GKV_LDS_LIMIT) {                             // beyond the default per-workgroup limit: opt in (a CU holds 160 KiB)
     const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
     if (e != hipSuccess) return e;
@@ -773,12 +884,17 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const ScoreArgs& a, in
   return gkv_launch(ln, kern, dim3(units * pl.ksplit), dim3(NW * 64), shmem, dm, a, pl);
 }
 
+template <bool K8>
+hipError_t launch_for(const GkvLaunch& ln, const GkvDims& dm, int dtype, const ScoreArgs& a, int len_max) {
+  if (dtype == GKV_F32)
+    return dm.d == 64 ? launch<float, 64, 4, 2, K8>(ln, dm, a, len_max) : launch<float, 128, 4, 1, K8>(ln, dm, a, len_max);
+  hipError_t e;
+  if (dm.d == 64 ? try_launch_regs<64, K8>(ln, dm, a, len_max, &e) : try_launch_regs<128, K8>(ln, dm, a, len_max, &e)) return e;
+  return dm.d == 64 ? launch<uint16_t, 64, 4, 2, K8>(ln, dm, a, len_max) : launch<uint16_t, 128, 4, 2, K8>(ln, dm, a, len_max);
+}
+
 }  // namespace
 
 hipError_t gkv_launch_score_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const ScoreArgs& a, int len_max) {
-  if (dtype == GKV_F32)
-    return dm.d == 64 ? launch<float, 64, 4, 2>(ln, dm, a, len_max) : launch<float, 128, 4, 1>(ln, dm, a, len_max);
-  hipError_t e;
-  if (dm.d == 64 ? try_launch_regs<64>(ln, dm, a, len_max, &e) : try_launch_regs<128>(ln, dm, a, len_max, &e)) return e;
-  return dm.d == 64 ? launch<uint16_t, 64, 4, 2>(ln, dm, a, len_max) : launch<uint16_t, 128, 4, 2>(ln, dm, a, len_max);
+  return a.scales ? launch_for<true>(ln, dm, dtype, a, len_max) : launch_for<false>(ln, dm, dtype, a, len_max);
 }
