@@ -366,8 +366,8 @@ gkv_status gkv_q8_evict(gkv_ctx* ctx, const void* qwin, void* K8, void* V8, void
  * The prefix is not part of the sequences' caches: it has no positions there, does not count to the budget, is never
  * evicted, and the local score stays a softmax over the sequence's own rows.
  * part: device memory of at least gkv_prefix_bytes(rows) bytes, 16-byte aligned, zeroed once by the caller.  gkv_prefix_attend
- * leaves there, for each query head of its sequences, sum, maximum and weighted values, in 32 bits; those of other sequences stay as
- * they are, so a batch of several prompts takes one call for each of them (on one stream, or ordered by events), and a sequence
+ * leaves there, for each query head of its sequences, maximum, sum and weighted values of up to 64 pieces of the prefix, in 32 bits;
+ * those of other sequences stay as they are, so a batch of several prompts takes one call for each of them (on one stream, or ordered by events), and a sequence
  * that has none a part that still is zero.  Results stay until they are written again: call it in every step.
  * rows may be 0 (Kp and Vp are not looked at then).  A call with more rows than the context's gkv_prefix_bytes calls were asked for
  * returns GKV_ERR_WORKSPACE.  Both calls can be recorded; the rows are frozen then.  head_dim has to be a multiple of 4.

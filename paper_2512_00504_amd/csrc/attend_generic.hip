@@ -68,16 +68,20 @@ __global__ __launch_bounds__(NWG * 64) void attend_generic_kernel(GkvDims dm, At
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
     const size_t row = (size_t)lb * dm.Hq + head;
-    PrefixWeight pw{sm > 0.f ? 1.f / sm : 0.f, 0.f};
-    if constexpr (PREFIX) pw = prefix_weight(a.prefix, row, mx, sm, n_tot > 0);
+    float own = sm > 0.f ? 1.f / sm : 0.f;
+    PrefixTotal all{};
+    if constexpr (PREFIX) {
+      all = prefix_total(a.prefix, row, mx, sm, n_tot > 0);
+      own = __builtin_amdgcn_exp2f(mx - all.max) * all.inverse;
+    }
     // output: a lane per channel, keys in order
     T* oh = (T*)a.out + ((size_t)lb * dm.Hq + head) * d;
     for (int c = lane; c < d; c += 64) {
       float acc = 0.f;
       for (int n = 0; n < len0; ++n) acc = fmaf(prob[n], Elem<T>::ld(Vh + (size_t)n * d + c), acc);
       if (has_new) acc = fmaf(prob[len0], Elem<T>::ld(vn + c), acc);
-      acc *= pw.own;
-      if (PREFIX && pw.prefix != 0.f) acc = fmaf(a.prefix.o[row * d + c], pw.prefix, acc);
+      acc *= own;
+      if constexpr (PREFIX) acc = fmaf(prefix_channel(a.prefix, row, d, c, all.max), all.inverse, acc);
       Elem<T>::st(oh + c, acc);
     }
     __builtin_amdgcn_wave_barrier();           // prob / qs are reused by this wavefront's next head

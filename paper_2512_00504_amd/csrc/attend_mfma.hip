@@ -649,12 +649,16 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
   const int slot = step - quotient(step, a.by_w) * a.w;
   float2* stats = a.stats + (size_t)slot * a.LB * a.Hq + head0;
   // the unit's result, from its own sum of weighted values
-  auto finish = [&](int x, int h, int c4, float M, float L, const f32x4& o, bool fast) {
+  auto finish = [&](int x, int h, int c4, float M, float L, f32x4 o, bool fast) {
     if constexpr (PREFIX) {
-      const PrefixWeight pw = prefix_weight(a.prefix, head0 + h, M, L, n_tot > 0);
-      f32x4 y = o * pw.own;
-      if (pw.prefix != 0.f) y += *(const f32x4*)(a.prefix.o + (head0 + h) * D + c4) * pw.prefix;
-      store_row4(out + (uint32_t)(x * 4), y);
+      const int n = a.prefix.n[head0];                       // uniform, the same for all heads of a sequence
+      bool any_key = n_tot > 0;
+      PrefixPieces pre;
+      for (int s0 = 0; s0 < n; s0 += PrefixPieces::AT_ONCE) {
+        pre.request(a.prefix, head0 + h, D, c4, s0, n);
+        pre.join(s0, n, M, L, o, any_key);
+      }
+      store_row4(out + (uint32_t)(x * 4), o * inverse_total(L, any_key));
     } else {
       store_row4(out + (uint32_t)(x * 4), o * inv_sum(L, n_tot > 0, fast));
     }

@@ -456,13 +456,15 @@ static int32_t copies_q(const gkv_ctx* ctx, const void* q, const void* qwin, int
   return (const char*)q != (const char*)qwin + (size_t)(step % ctx->dims.w) * slot_bytes;
 }
 
-// What gkv_prefix_attend leaves at the start of its buffer.
-static size_t prefix_o_bytes(const gkv_ctx* ctx) {
-  return gkv_align256((size_t)ctx->dims.L * ctx->dims.B * ctx->dims.Hq * ctx->dims.d * sizeof(float));
-}
+// What gkv_prefix_attend leaves in its buffer: n [heads], maxima and sums [GKV_PREFIX_PIECES][heads], outputs [pieces][heads][d], for
+// the L * B * h_q heads of the context.
+static size_t prefix_heads(const gkv_ctx* ctx) { return (size_t)ctx->dims.L * ctx->dims.B * ctx->dims.Hq; }
 static PrefixPart prefix_part(const gkv_ctx* ctx, const void* part) {
-  if (!part) return PrefixPart{nullptr, nullptr};
-  return PrefixPart{(const float*)part, (const float2*)((const char*)part + prefix_o_bytes(ctx))};
+  if (!part) return PrefixPart{nullptr, nullptr, nullptr, 0};
+  const size_t heads = prefix_heads(ctx);
+  const char* ms = (const char*)part + gkv_align256(heads * sizeof(int32_t));
+  return PrefixPart{(const float*)(ms + gkv_align256(GKV_PREFIX_PIECES * heads * sizeof(float2))), (const float2*)ms,
+                    (const int32_t*)part, (int64_t)heads};
 }
 static bool aligned16(std::initializer_list<const void*> ptrs) {
   uintptr_t bits = 0;
@@ -773,7 +775,7 @@ static PrefixPlan prefix_plan(const gkv_ctx* ctx, bool mfma, int rows, int count
     const int64_t blocks = ((int64_t)count * d.g + 31) / 32;
     p.tiles = (int)((blocks + 3) / 4);
     p.blocks = (int)((blocks + p.tiles - 1) / p.tiles);
-    want = 512 / ((int64_t)d.L * d.Hkv * p.tiles);
+    want = 768 / ((int64_t)d.L * d.Hkv * p.tiles);
     least = 128;
   } else {
     want = 2048 / ((int64_t)d.L * count * d.Hkv);
@@ -781,22 +783,22 @@ static PrefixPlan prefix_plan(const gkv_ctx* ctx, bool mfma, int rows, int count
   }
   const int64_t most = ((int64_t)rows + least - 1) / least;
   const int64_t n = want < most ? want : most;
-  p.splits = (int)(n < 1 ? 1 : n > 128 ? 128 : n);
+  p.splits = (int)(n < 1 ? 1 : n > GKV_PREFIX_PIECES ? GKV_PREFIX_PIECES : n);
   return p;
 }
 
 extern "C" gkv_status gkv_prefix_bytes(gkv_ctx* ctx, int32_t rows_max, size_t* out_bytes) {
   if (!ctx || !out_bytes || rows_max < 0) return GKV_ERR_INVALID_ARG;
-  size_t pieces = 0;                                              // of one query head of every sequence of a call
+  size_t pieces = 1;
   for (int count = 1; count <= ctx->dims.B; ++count)
     for (int mfma = 0; mfma <= (int)ctx->mfma_shape; ++mfma) {
-      const int n = prefix_plan(ctx, mfma, rows_max, count).splits;
-      if (n > 1 && (size_t)n * count > pieces) pieces = (size_t)n * count;
+      const size_t n = (size_t)prefix_plan(ctx, mfma, rows_max, count).splits;
+      if (n > pieces) pieces = n;
     }
-  const size_t heads = (size_t)ctx->dims.L * ctx->dims.Hq;
   if (rows_max > ctx->prefix_rows) ctx->prefix_rows = rows_max;
-  *out_bytes = prefix_o_bytes(ctx) + gkv_align256(heads * ctx->dims.B * sizeof(float2)) +
-               gkv_align256(pieces * heads * ctx->dims.d * sizeof(float)) + gkv_align256(pieces * heads * sizeof(float2));
+  const size_t heads = prefix_heads(ctx);
+  *out_bytes = gkv_align256(heads * sizeof(int32_t)) + gkv_align256(GKV_PREFIX_PIECES * heads * sizeof(float2)) +
+               gkv_align256(pieces * heads * ctx->dims.d * sizeof(float));
   return GKV_OK;
 }
 
@@ -808,23 +810,16 @@ extern "C" gkv_status gkv_prefix_attend(gkv_ctx* ctx, const void* q, const void*
   if (ctx->dims.d % 4 != 0) return GKV_ERR_SHAPE;
   if (rows > ctx->prefix_rows) return GKV_ERR_WORKSPACE;          // the buffer was not sized for them
   const GkvDims& d = ctx->dims;
-  const size_t heads = (size_t)d.L * d.Hq;
-  PrefixArgs a{q, Kp, Vp, rows, capacity, first, count, 1, 0, nullptr, nullptr, nullptr, nullptr};
-  char* p = (char*)part;
-  a.o = (float*)p; p += prefix_o_bytes(ctx);
-  a.ms = (float2*)p; p += gkv_align256(heads * d.B * sizeof(float2));
+  const PrefixPart to = prefix_part(ctx, part);
+  PrefixArgs a{q, Kp, Vp, rows, capacity, first, count, 1, 0, (float*)to.o, (float2*)to.ms, (int32_t*)to.n, to.heads};
   const bool mfma = use_mfma(ctx, {q, Kp, Vp});
   const PrefixPlan plan = prefix_plan(ctx, mfma, rows, count);
   a.split_rows = (int)((((int64_t)rows + plan.splits - 1) / plan.splits + 63) / 64 * 64);
   if (a.split_rows < 64) a.split_rows = 64;
   a.splits = rows > 0 ? (int)(((int64_t)rows + a.split_rows - 1) / a.split_rows) : 1;
-  a.part_o = (float*)p; p += gkv_align256((size_t)a.splits * heads * count * d.d * sizeof(float));
-  a.part_ms = (float2*)p;
   GkvLaunch ln{ctx, -1, (hipStream_t)stream};
-  gkv_status st = hip_status(mfma ? gkv_launch_prefix_mfma(ln, d, ctx->cfg.dtype, a, plan)
-                                  : gkv_launch_prefix_generic(ln, d, ctx->cfg.dtype, a));
-  if (st != GKV_OK || a.splits == 1) return st;
-  return hip_status(gkv_launch_prefix_join(ln, d, a));
+  return hip_status(mfma ? gkv_launch_prefix_mfma(ln, d, ctx->cfg.dtype, a, plan)
+                         : gkv_launch_prefix_generic(ln, d, ctx->cfg.dtype, a));
 }
 
 // ---- profiling API ------------------------------------------------------------------------------

@@ -41,6 +41,7 @@ struct GkvProfile;   // event pools, defined in gkv_api.hip
 // now, so each capture counts as a stream of its own.
 constexpr int GKV_SPLIT_SETS = 8;
 constexpr int GKV_TICKETS = 8;   // tickets per unit and set: one for each wavefront that has outputs (g * d / 256, at most 8)
+constexpr int GKV_PREFIX_PIECES = 64;   // that a shared prefix is cut into at most
 struct GkvStreamKey { const void* stream; unsigned long long capture; };
 
 struct gkv_ctx {
@@ -102,9 +103,9 @@ struct GkvLaunch {
   bool continued = false;   // a further launch of the same call: its time counts, the call does not count again
 };
 
-// The results over a shared prefix of every (layer, sequence, query head): unnormalised outputs, and maximum (log2 units) and
-// sum.  A sum of zero: nothing there.  o == nullptr: no prefix.
-struct PrefixPart { const float* o; const float2* ms; };
+// The results over a shared prefix: n[head] pieces for each (layer, sequence, query head), `heads` of them in all, and of each
+// piece [piece][head] the unnormalised outputs and the maximum (log2 units) and sum.  o == nullptr: no prefix.
+struct PrefixPart { const float* o; const float2* ms; const int32_t* n; int64_t heads; };
 
 // ---- launch wrappers implemented in the kernel files -------------------------------------
 struct AttendArgs {
@@ -178,15 +179,13 @@ hipError_t gkv_launch_q8_compact(const GkvLaunch& ln, const GkvDims& dm, const i
 struct PrefixArgs {
   const void* q; const void* K; const void* V;
   int32_t rows, capacity, first, count;
-  int32_t splits, split_rows;   // pieces, rows of each; with one piece the results go to o and ms
-  float* o; float2* ms;         // [L,B,h_q,d], [L,B,h_q]
-  float* part_o; float2* part_ms;   // [splits][L,count,h_q] of each
+  int32_t splits, split_rows;   // pieces, rows of each
+  float* o; float2* ms; int32_t* n; int64_t heads;   // as PrefixPart has them
 };
 // How the matrix-core kernel's rows are dealt out: `tiles` workgroups of up to `blocks` wavefronts of 32 rows per piece.
 struct PrefixPlan { int32_t splits, tiles, blocks; };
 hipError_t gkv_launch_prefix_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a, const PrefixPlan& plan);
 hipError_t gkv_launch_prefix_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a);
-hipError_t gkv_launch_prefix_join(const GkvLaunch& ln, const GkvDims& dm, const PrefixArgs& a);
 hipError_t gkv_launch_fill_zero(hipStream_t stream, int32_t* p, size_t n);
 hipError_t gkv_launch_add_int(hipStream_t stream, int32_t* p, int32_t delta);
 
@@ -297,22 +296,76 @@ __device__ __forceinline__ float log2_weight(float z, float hi, float lo, float 
   return fmaf(fmaxf(z, -3.402823466e38f), lo, fmaf(z, hi, -m));
 }
 
-// The maximum as a prefix result holds it: -inf where there were keys, all of weight zero.
+// The maximum as a piece of a prefix holds it: -inf where there were keys, all of weight zero.
 __device__ __forceinline__ float prefix_max(float m, float sum, bool any_key) {
   return sum == 0.f ? (any_key ? -INFINITY : GKV_NO_MAX) : m;
 }
-// Factors of the sequence's own sum of weighted values (maximum m, sum l) and of the prefix's in the joint result.  Nothing
-// attended to: 0; keys whose logits are all -inf: NaN, as softmax gives.
-struct PrefixWeight { float own, prefix; };
-__device__ __forceinline__ PrefixWeight prefix_weight(const PrefixPart& p, size_t head, float m, float l, bool any_key) {
-  float2 ms = make_float2(GKV_NO_MAX, 0.f);
-  if (p.o) ms = p.ms[head];
-  const bool there = !(ms.y == 0.f);
-  const float both = there ? fmaxf(m, ms.x) : m;
-  const float own = there ? __builtin_amdgcn_exp2f(m - both) : 1.f, prefix = there ? __builtin_amdgcn_exp2f(ms.x - both) : 0.f;
-  const float total = l * own + ms.y * prefix;
-  if (total == 0.f) return PrefixWeight{any_key || ms.x == -INFINITY ? __builtin_nanf("") : 0.f, 0.f};
-  return PrefixWeight{own / total, there ? prefix / total : 0.f};   // (0 where there is none, whatever the total: p.o may be null)
+// 1 / total of a softmax's weights.  Nothing attended to: 0; keys whose logits are all -inf: NaN, as softmax gives.
+__device__ __forceinline__ float inverse_total(float total, bool any_key) {
+  return total == 0.f ? (any_key ? __builtin_nanf("") : 0.f) : 1.f / total;
+}
+// Joins a prefix's pieces of one head with the sequence's own sum o of weighted values (channels c .. c + 3; maximum m, sum l).
+typedef float gkv_f32x4 __attribute__((ext_vector_type(4)));
+struct PrefixPieces {
+  static constexpr int AT_ONCE = 4;
+  float2 ms[AT_ONCE];
+  gkv_f32x4 o[AT_ONCE];
+  __device__ __forceinline__ void request(const PrefixPart& p, size_t head, int d, int c, int s0, int n) {
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+      if (s0 + i < n) {
+        const size_t at = (size_t)(s0 + i) * p.heads + head;
+        ms[i] = p.ms[at];
+        o[i] = *(const gkv_f32x4*)(p.o + at * d + c);
+      }
+  }
+  __device__ __forceinline__ void join(int s0, int n, float& m, float& l, gkv_f32x4& sum, bool& any_key) {
+    float mn = m;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+      if (s0 + i < n) {
+        any_key |= ms[i].x == -INFINITY;
+        if (ms[i].y != 0.f) mn = fmaxf(mn, ms[i].x);
+      }
+    const float f0 = __builtin_amdgcn_exp2f(m - mn);
+    m = mn;
+    l *= f0;
+    sum *= f0;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+      if (s0 + i < n) {
+        const float f = ms[i].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[i].x - mn);
+        l += ms[i].y * f;
+        sum += o[i] * f;
+      }
+  }
+};
+// The same for the plain kernels, one channel a lane: maximum and inverse of the joint total, and the pieces' share of a channel.
+struct PrefixTotal { float max, inverse; };
+__device__ __forceinline__ PrefixTotal prefix_total(const PrefixPart& p, size_t head, float m, float l, bool any_key) {
+  const int n = p.o ? p.n[head] : 0;
+  float mx = m, total = 0.f;
+  for (int s = 0; s < n; ++s) {
+    const float2 ms = p.ms[s * p.heads + head];
+    any_key |= ms.x == -INFINITY;
+    if (ms.y != 0.f) mx = fmaxf(mx, ms.x);
+  }
+  total = l * __builtin_amdgcn_exp2f(m - mx);
+  for (int s = 0; s < n; ++s) {
+    const float2 ms = p.ms[s * p.heads + head];
+    if (ms.y != 0.f) total += ms.y * __builtin_amdgcn_exp2f(ms.x - mx);
+  }
+  return PrefixTotal{mx, inverse_total(total, any_key)};
+}
+__device__ __forceinline__ float prefix_channel(const PrefixPart& p, size_t head, int d, int c, float mx) {
+  const int n = p.o ? p.n[head] : 0;
+  float x = 0.f;
+  for (int s = 0; s < n; ++s) {
+    const size_t at = s * p.heads + head;
+    const float2 ms = p.ms[at];
+    if (ms.y != 0.f) x = fmaf(p.o[at * d + c], __builtin_amdgcn_exp2f(ms.x - mx), x);
+  }
+  return x;
 }
 
 __device__ __forceinline__ float wave_max(float v) {

@@ -1,10 +1,10 @@
-// Attention over a prefix that sequences share: the plain kernel, and the joining of pieces.
+// Attention over a prefix that sequences share: the plain kernel.
 //
 // K and V of the prefix are there once per (layer, KV head), and the newest queries of all sequences that share it are
 // the rows of one product with them.  What is left of it for each query head is o = sum 2^(y_n - m) v_n with y_n the logit in log2
-// units, the largest of them m and the sum l = sum 2^(y_n - m), all in 32 bits; the decode kernels join (o, m, l) with
-// what they have of the sequence's own cache (prefix_weight), so the result is one softmax over both.
-// Long prefixes are cut over workgroups, each piece with an (o, m, l) of its own.
+// units, the largest of them m and the sum l = sum 2^(y_n - m), all in 32 bits.  Long prefixes are cut over
+// workgroups, each piece with an (o, m, l) of its own, and the decode kernels join the pieces with what they have of the
+// sequence's own cache (PrefixPieces), so the result is one softmax over all.
 #include "gkv_internal.h"
 
 namespace {
@@ -58,42 +58,15 @@ __global__ __launch_bounds__(NWG * 64) void prefix_generic_kernel(GkvDims dm, Pr
           acc[x] = o;
         }
     }
-    const size_t piece = ((size_t)layer * a.count + i) * dm.Hq + j * g + hi;
-    const size_t to = a.splits > 1 ? (size_t)blockIdx.y * ((size_t)dm.L * a.count * dm.Hq) + piece : head0 + hi;
+    const size_t to = (size_t)blockIdx.y * a.heads + head0 + hi;
 #pragma unroll
     for (int x = 0; x < MOST; ++x)
-      if (lane + 64 * x < d) (a.splits > 1 ? a.part_o : a.o)[to * d + lane + 64 * x] = acc[x];
-    if (lane == 0) (a.splits > 1 ? a.part_ms : a.ms)[to] = make_float2(prefix_max(m, sum, n1 > n0), sum);
+      if (lane + 64 * x < d) a.o[to * d + lane + 64 * x] = acc[x];
+    if (lane == 0) {
+      a.ms[to] = make_float2(prefix_max(m, sum, n1 > n0), sum);
+      if (blockIdx.y == 0) a.n[to] = a.splits;
+    }
   }
-}
-
-// Joins the pieces of each query head: d / 4 threads a head.
-__global__ __launch_bounds__(256) void prefix_join_kernel(GkvDims dm, PrefixArgs a) {
-  const int per = dm.d / 4;
-  const size_t heads = (size_t)dm.L * a.count * dm.Hq;
-  const size_t x = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (x >= heads * per) return;
-  const size_t head = x / per;
-  const int c = (int)(x - head * per) * 4;
-  float m = GKV_NO_MAX;
-  bool nothing = false;
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ms = a.part_ms[s * heads + head];
-    if (ms.y == 0.f) nothing |= ms.x == -INFINITY;
-    else m = fmaxf(m, ms.x);
-  }
-  float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ms = a.part_ms[s * heads + head];
-    const float f = ms.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms.x - m);
-    sum += ms.y * f;
-    const float4 p = *(const float4*)(a.part_o + (s * heads + head) * dm.d + c);
-    o[0] = fmaf(p.x, f, o[0]); o[1] = fmaf(p.y, f, o[1]); o[2] = fmaf(p.z, f, o[2]); o[3] = fmaf(p.w, f, o[3]);
-  }
-  const size_t lb = head / dm.Hq, layer = lb / a.count;
-  const size_t to = (layer * dm.B + a.first + (lb - layer * a.count)) * dm.Hq + (head - lb * dm.Hq);
-  *(float4*)(a.o + to * dm.d + c) = make_float4(o[0], o[1], o[2], o[3]);
-  if (c == 0) a.ms[to] = make_float2(prefix_max(m, sum, nothing), sum);
 }
 
 }  // namespace
@@ -103,9 +76,4 @@ hipError_t gkv_launch_prefix_generic(const GkvLaunch& ln, const GkvDims& dm, int
   const size_t shmem = sizeof(float) * NWG * (dm.d + 64);
   if (dtype == GKV_F32) return gkv_launch(ln, prefix_generic_kernel<float>, grid, dim3(NWG * 64), shmem, dm, a);
   return gkv_launch(ln, prefix_generic_kernel<uint16_t>, grid, dim3(NWG * 64), shmem, dm, a);
-}
-
-hipError_t gkv_launch_prefix_join(const GkvLaunch& ln, const GkvDims& dm, const PrefixArgs& a) {
-  const size_t threads = (size_t)dm.L * a.count * dm.Hq * (dm.d / 4);
-  return gkv_launch(ln, prefix_join_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, dm, a);
 }

@@ -14,6 +14,8 @@
 // 16 x (maximum, fma, exponential, sum, conversion).
 #include "gkv_internal.h"
 
+#include <type_traits>
+
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -38,7 +40,7 @@ __device__ __forceinline__ float over_halves(float x, bool max) {
 template <typename T, int D>
 struct Geo {
   static constexpr bool F32 = sizeof(T) == 4;
-  static constexpr int TK = F32 ? 32 : 64;                   // keys of a tile
+  static constexpr int TK = 32;                   // keys of a tile
   static constexpr int ROW = D * (int)sizeof(T);             // bytes
   static constexpr int CHUNKS = ROW / 16;
   static constexpr int TILE = TK * ROW;                      // bytes of K, and of V
@@ -55,8 +57,12 @@ struct Geo {
 // A 1 KiB piece from memory to LDS, 16 bytes a lane; `lds` is uniform.  (Written out, because the compiler makes every later read of LDS
 // wait for every such request; the wait is the one before the barrier below.  Nothing else in this file uses m0.)
 __device__ __forceinline__ void to_lds(const char* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
 }
+
+// What lies at an address of LDS.
+template <typename V>
+__device__ __forceinline__ V in_lds(uint32_t at) { return *(const __attribute__((address_space(3))) V*)(uintptr_t)at; }
 
 struct KernelArgs {
   PrefixArgs p;
@@ -66,7 +72,7 @@ struct KernelArgs {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void prefix_mfma_kernel(KernelArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void prefix_mfma_kernel(KernelArgs a) {
   using G = Geo<T, D>;
   constexpr int SUB = G::TK / 32, CB = D / 32;
   extern __shared__ __attribute__((aligned(1024))) char smem[];     // [2][K, V][TILE]
@@ -112,27 +118,36 @@ __global__ __launch_bounds__(256, 2) void prefix_mfma_kernel(KernelArgs a) {
   f32x16 o[CB];
 #pragma unroll
   for (int i = 0; i < CB; ++i) o[i] = f32x16{};
-  if (n_tiles > 0) bring(0, 0);
-  for (int t = 0; t < n_tiles; ++t) {
-    const int buf = t & 1;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wavefront's share of the tile is there
-    __syncthreads();                                         // everybody's is, and nobody reads the other buffer any more
-    if (t + 1 < n_tiles) bring(t + 1, buf ^ 1);
-    const char* Kt = smem + buf * 2 * G::TILE;
-    char* Vt = smem + buf * 2 * G::TILE + G::TILE;
-    const int there = n1 - n0 - t * G::TK;                   // keys of this tile that count
-    if (there < G::TK) {                                     // the last one: V behind the end is zero
-      for (int x = tid; x < (G::TK - there) * G::CHUNKS; x += nw * 64) *(u32x4*)(Vt + there * G::ROW + x * 16) = u32x4{0u, 0u, 0u, 0u};
+  // This lane's places in a tile: a chunk of K (two of them with h) and a block of channels of V each; the rest of an address is an
+  // immediate.
+  uint32_t k_at[G::ROW / 32], v_at[CB];
+#pragma unroll
+  for (int c = 0; c < G::ROW / 32; ++c) k_at[c] = lds0 + lr * G::ROW + ((2 * c + h) ^ G::k_swap(lr)) * 16;
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    if constexpr (G::F32) {
+      v_at[cb] = lds0 + G::TILE + 4 * h * G::ROW + lr * 4 + cb * 128;
+    } else {
+      // row 4 h + (lane % 16) / 4 of eight, piece lane % 4 of the 16 channels that its 16 lanes share
+      const int at = 4 * h + ((lane & 15) >> 2), chunk = 4 * cb + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      v_at[cb] = lds0 + G::TILE + at * G::ROW + (chunk ^ G::v_swap(at)) * 16 + (lane & 1) * 8;
+    }
+  }
+  // One tile of `there` keys, in the buffer that begins at `buf`; last: it may have fewer than TK.
+  auto work = [&](uint32_t buf, int there, auto last) {
+    constexpr bool LAST = decltype(last)::value;
+    if constexpr (LAST) {                                    // V behind the end is zero
+      char* end = smem + buf + G::TILE + there * G::ROW;
+      for (int x = tid; x < (G::TK - there) * G::CHUNKS; x += nw * 64) *(u32x4*)(end + x * 16) = u32x4{0u, 0u, 0u, 0u};
       __syncthreads();
     }
     f32x16 s[SUB];
 #pragma unroll
     for (int i = 0; i < SUB; ++i) {
       s[i] = f32x16{};
-      const char* kr = Kt + (32 * i + lr) * G::ROW;
 #pragma unroll
       for (int c = 0; c < G::ROW / 32; ++c) {
-        const u32x4 k = ld16(kr + ((2 * c + h) ^ G::k_swap(lr)) * 16);
+        const u32x4 k = in_lds<u32x4>(k_at[c] + buf + 32 * i * G::ROW);
         if constexpr (G::F32) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -142,7 +157,7 @@ __global__ __launch_bounds__(256, 2) void prefix_mfma_kernel(KernelArgs a) {
         }
       }
     }
-    if (there < G::TK) {
+    if constexpr (LAST) {
 #pragma unroll
       for (int i = 0; i < SUB; ++i)
 #pragma unroll
@@ -154,10 +169,10 @@ __global__ __launch_bounds__(256, 2) void prefix_mfma_kernel(KernelArgs a) {
     for (int i = 0; i < SUB; ++i)
 #pragma unroll
       for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[i][e]);
-    mx = over_halves(mx, true);
-    const float mn = fmaxf(m, rounded_product(mx, a.scale_hi));
-    if (__any(mn > m)) {
-      const float f = __builtin_amdgcn_exp2f(m - mn);
+    mx = rounded_product(over_halves(mx, true), a.scale_hi);
+    // m follows the largest logit at a distance of up to 8 (weights up to 256): moving it takes a product for every accumulator
+    if (__any(mx > m + 8.f)) {
+      const float mn = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - mn);
       l *= f;
 #pragma unroll
       for (int i = 0; i < CB; ++i) o[i] *= f;
@@ -191,10 +206,11 @@ __global__ __launch_bounds__(256, 2) void prefix_mfma_kernel(KernelArgs a) {
       if constexpr (G::F32) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const char* vr = Vt + (32 * i + 8 * (e >> 2) + 4 * h + (e & 3)) * G::ROW + lr * 4;
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb)
-            o[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float*)(vr + cb * 128), s[i][e], o[cb], 0, 0, 0);
+          for (int cb = 0; cb < CB; ++cb) {
+            const float v = in_lds<float>(v_at[cb] + buf + (32 * i + 8 * (e >> 2) + (e & 3)) * G::ROW);
+            o[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i][e], o[cb], 0, 0, 0);
+          }
         }
       } else {
 #pragma unroll
@@ -207,13 +223,8 @@ __global__ __launch_bounds__(256, 2) void prefix_mfma_kernel(KernelArgs a) {
           for (int cb = 0; cb < CB; ++cb) {
             s16x4 v[2];
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              // lane: row 4 h + (lane % 16) / 4 of eight, piece lane % 4 of the 16 channels that its 16 lanes share
-              const int at = 32 * i + 16 * k + 8 * y + 4 * h + ((lane & 15) >> 2);
-              const int chunk = 4 * cb + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-              const char* vp = Vt + at * G::ROW + (chunk ^ G::v_swap(at)) * 16 + (lane & 1) * 8;
-              v[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)vp);
-            }
+            for (int y = 0; y < 2; ++y)
+              v[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)(v_at[cb] + buf + (32 * i + 16 * k + 8 * y) * G::ROW));
             const u32x2 v0 = __builtin_bit_cast(u32x2, v[0]), v1 = __builtin_bit_cast(u32x2, v[1]);
             o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, (u32x4{v0[0], v0[1], v1[0], v1[1]})),
                                                             __builtin_bit_cast(bf16x8, p), o[cb], 0, 0, 0);
@@ -221,18 +232,42 @@ __global__ __launch_bounds__(256, 2) void prefix_mfma_kernel(KernelArgs a) {
         }
       }
     }
+  };
+  // The next tile's buffer is the one that everybody is through with at the barrier.
+  auto there_now = [] {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wavefront's share of the tile
+    __syncthreads();                                         // and everybody's
+  };
+  if (n_tiles > 0) {
+    bring(0, 0);
+    uint32_t buf = 0;
+    for (int t = 0;; t += 2) {
+      there_now();
+      if (t == n_tiles - 1) break;
+      bring(t + 1, 1);
+      work(0, G::TK, std::false_type{});
+      there_now();
+      buf = 2 * G::TILE;
+      if (t + 1 == n_tiles - 1) break;
+      buf = 0;
+      bring(t + 2, 0);
+      work(2 * G::TILE, G::TK, std::false_type{});
+    }
+    work(buf, n1 - n0 - (n_tiles - 1) * G::TK, std::true_type{});
   }
   if (row >= n_rows) return;
   l = over_halves(l, false);
-  const bool pieces = a.p.splits > 1;
-  const size_t piece = (((size_t)split * a.L + layer) * a.p.count + seq) * a.Hq + j * a.g + (row - seq * a.g);
-  float* to = pieces ? a.p.part_o + piece * D : a.p.o + head * D;
+  const size_t piece = (size_t)split * a.p.heads + head;
+  float* to = a.p.o + piece * D;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       *(f32x4*)(to + 32 * cb + 8 * i + 4 * h) = f32x4{o[cb][4 * i], o[cb][4 * i + 1], o[cb][4 * i + 2], o[cb][4 * i + 3]};
-  if (h == 0) (pieces ? a.p.part_ms[piece] : a.p.ms[head]) = make_float2(prefix_max(m, l, n1 > n0), l);
+  if (h == 0) {
+    a.p.ms[piece] = make_float2(prefix_max(m, l, n1 > n0), l);
+    if (split == 0) a.p.n[head] = a.p.splits;
+  }
 }
 
 template <typename T, int D>

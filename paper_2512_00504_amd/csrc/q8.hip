@@ -218,13 +218,13 @@ __global__ __launch_bounds__(NWG * 64) void q8_attend_generic_kernel(GkvDims dm,
     }
     sm = wave_sum(sm);
     wave_sync();
-    const PrefixWeight pw = prefix_weight(a.prefix, row, mx, sm, n_tot > 0);
+    const PrefixTotal all = prefix_total(a.prefix, row, mx, sm, n_tot > 0);
+    const float own = __builtin_amdgcn_exp2f(mx - all.max) * all.inverse;
     T* oh = (T*)a.out + row * d;
     for (int c = lane; c < d; c += 64) {
       float acc = 0.f;
       for (int n = 0; n < n_tot; ++n) acc = fmaf(prob[n], __builtin_amdgcn_cvt_f32_fp8(Vh[(size_t)n * d + c], 0), acc);
-      acc *= pw.own;
-      if (pw.prefix != 0.f) acc = fmaf(a.prefix.o[row * d + c], pw.prefix, acc);
+      acc = fmaf(prefix_channel(a.prefix, row, d, c, all.max), all.inverse, acc * own);
       Elem<T>::st(oh + c, acc);
     }
     wave_sync();                                           // prob / qs are reused by this wavefront's next head

@@ -429,20 +429,26 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
         *(f32x4*)(row + G::NC * (4 * kb + e) + 4 * q4) = f32x4{st.o[4 * q4][e], st.o[4 * q4 + 1][e], st.o[4 * q4 + 2][e], st.o[4 * q4 + 3][e]};
     if (kb == 0) { sm[r * NW + wave] = st.m; sl[r * NW + wave] = l_tot; }
   }
-  __syncthreads();
 
   constexpr int TPH = D / 4;                                 // threads per head
   T* out = (T*)a.out + head0 * D;
   float* part = a.partials + (size_t)(unit * splits) * g * PSTR;
   const int slot = step - quotient(step, a.by_w) * a.w;
   float2* stats = a.stats + (size_t)slot * a.LB * a.Hq + head0;
-  auto finish = [&](int x, int h, int c4, float M, float L, const f32x4& o) {
-    const PrefixWeight pw = prefix_weight(a.prefix, head0 + h, M, L, n_tot > 0);
-    f32x4 y = o * pw.own;
-    if (pw.prefix != 0.f) y += *(const f32x4*)(a.prefix.o + (head0 + h) * D + c4) * pw.prefix;
-    store_row4(out + (uint32_t)(x * 4), y);
+  const int n_pre = a.prefix.o ? a.prefix.n[head0] : 0;      // uniform, the same for all heads of a sequence
+  PrefixPieces pre;
+  // the unit's result; ready: the first pieces of the prefix are in `pre`
+  auto finish = [&](int x, int h, int c4, float M, float L, f32x4 o, bool ready) {
     if (c4 == 0 && a.write_stats) stats[h] = make_float2(M, L);
+    bool any_key = n_tot > 0;
+    for (int s0 = 0; s0 < n_pre; s0 += PrefixPieces::AT_ONCE) {
+      if (s0 > 0 || !ready) pre.request(a.prefix, head0 + h, D, c4, s0, n_pre);
+      pre.join(s0, n_pre, M, L, o, any_key);
+    }
+    store_row4(out + (uint32_t)(x * 4), o * inverse_total(L, any_key));
   };
+  if (ns == 1 && n_pre > 0 && tid < g * TPH) pre.request(a.prefix, head0 + tid / TPH, D, (tid % TPH) * 4, 0, n_pre);
+  __syncthreads();
   for (int x = tid; x < g * TPH; x += NW * 64) {
     const int h = x / TPH, c4 = (x % TPH) * 4;
     float mw[NW], M = GKV_NO_MAX;
@@ -457,7 +463,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
       o += *(const f32x4*)(so + (i * g + h) * OSTR + c4) * f;
     }
     if (ns == 1) {
-      finish(x, h, c4, M, L, o);
+      finish(x, h, c4, M, L, o, x == tid);
     } else {
       float* ph = part + (uint32_t)((sp * g + h) * PSTR);
       store_agent(ph + c4, o[0], o[1]);
@@ -520,7 +526,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
             o += f32x4{got[i][1].x, got[i][1].y, got[i][2].x, got[i][2].y} * f;
           }
       }
-      finish(x, h, c4, M, L, o);
+      finish(x, h, c4, M, L, o, false);
     }
   }
 }
