@@ -471,6 +471,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
   // holds chunks 4c+kb of q[r]) and the rows stored at the end of the workgroup.
   int4 rec = *(const int4*)(a.d_state + 4 * (size_t)lb);
   const int32_t base = *a.step_base;
+  const int n_pre = PREFIX ? a.prefix.n[head0] : 0;       // pieces of the prefix, the same for all heads of a sequence
   __builtin_amdgcn_sched_barrier(0);
   u32x4 qB[G::NL];
   {
@@ -640,10 +641,12 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
     }
     if (kb == 0) { sm[r * NW + wave] = st.m_run; sl[r * NW + wave] = l_tot; }
   }
+  constexpr int TPH = D / 4;                // threads per head
+  constexpr int PRE = 4;                    // pieces of the prefix at once (with 8 or 16 it takes no less)
+  PrefixPieces<PRE> pre;
   __syncthreads();
 
   // one thread per (head, 4 channels): a single round for g <= 8 with 256 threads
-  constexpr int TPH = D / 4;                // threads per head
   T* out = (T*)a.out + head0 * D;
   float* part = a.partials + (size_t)(unit * splits) * g * PSTR;      // [ns][g][PSTR]
   const int slot = step - quotient(step, a.by_w) * a.w;
@@ -651,12 +654,10 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
   // the unit's result, from its own sum of weighted values
   auto finish = [&](int x, int h, int c4, float M, float L, f32x4 o, bool fast) {
     if constexpr (PREFIX) {
-      const int n = a.prefix.n[head0];                       // uniform, the same for all heads of a sequence
       bool any_key = n_tot > 0;
-      PrefixPieces pre;
-      for (int s0 = 0; s0 < n; s0 += PrefixPieces::AT_ONCE) {
-        pre.request(a.prefix, head0 + h, D, c4, s0, n);
-        pre.join(s0, n, M, L, o, any_key);
+      for (int s0 = 0; s0 < n_pre; s0 += PRE) {
+        if (s0 > 0 || ns == 1 || x != tid) pre.request(a.prefix, head0 + h, D, c4, s0, n_pre);
+        pre.join(s0, n_pre, M, L, o, any_key);
       }
       store_row4(out + (uint32_t)(x * 4), o * inverse_total(L, any_key));
     } else {
@@ -710,6 +711,10 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // (counts to ns - 1 and starts over; an addition would be made into one over the active lanes and waited for at once)
     if (lane == 0) arrived = __builtin_amdgcn_atomic_inc32((uint32_t*)a.ticket + (size_t)unit * GKV_TICKETS + wave, (uint32_t)ns - 1u, __ATOMIC_RELAXED, "agent");
+  }
+
+  if constexpr (PREFIX) {                   // the prefix's first pieces, on their way while the ticket is
+    if (merges && tid < g * TPH) pre.request(a.prefix, head0 + tid / TPH, D, (tid % TPH) * 4, 0, n_pre);
   }
 
   // ---- append the new row (row-major, one contiguous row each for K and V), push q into the

@@ -764,19 +764,26 @@ extern "C" gkv_status gkv_q8_evict(gkv_ctx* ctx, const void* qwin, void* K8, voi
 // ---- shared prefix ---------------------------------------------------------------------------------
 // Pieces of a prefix of `rows` rows for `count` sequences.  More rows never make fewer pieces, so a buffer for more rows holds
 // those of fewer.
-//   Matrix cores: rows of queries in blocks of 32, at most 4 to a workgroup, and as many pieces as make about two workgroups a CU,
-//   of 128 keys at least.
+//   Matrix cores: rows of queries in blocks of 32, a wavefront each and at most 4 to a workgroup.  One or two blocks: the workgroup's
+//   wavefronts are groups that take the keys in turn, two workgroups a CU and up to 32 pieces of 256 keys at least.  A piece costs
+//   the decode kernel 0.2 us, so (us, the prefix's kernel + the decode kernel, 16 / 32 / 64 pieces, bf16, d = 128, g = 7) 8 sequences x 8000 rows,
+//   one layer 12.9 + 9.8 / 10.4 + 12.9 / 9.8 + 12.3, 4 x 32000 25.4 + 9.6 / 17.6 + 12.4 / 15.7 + 18.2; in one group instead of two or
+//   four 8 x 8000 27.8 in all where this takes 22; 28 layers, 8 x 4000 one workgroup a CU 84.5 in all, two 77.8.
+//   More blocks: three workgroups a CU (two: 136 us where three take 117, 64 sequences x 16384 rows, g = 5, 4 layers), 128 keys at least.
 //   Plain kernel: about two thousand workgroups, one a (sequence, KV head, piece), of 256 keys at least.
 static PrefixPlan prefix_plan(const gkv_ctx* ctx, bool mfma, int rows, int count) {
   const GkvDims& d = ctx->dims;
-  PrefixPlan p{1, 1, 1};
+  PrefixPlan p{1, 1, 1, 1};
   int64_t want, least;
   if (mfma) {
     const int64_t blocks = ((int64_t)count * d.g + 31) / 32;
     p.tiles = (int)((blocks + 3) / 4);
     p.blocks = (int)((blocks + p.tiles - 1) / p.tiles);
-    want = 768 / ((int64_t)d.L * d.Hkv * p.tiles);
-    least = 128;
+    const bool wide = d.d * ctx->esz >= 512;                    // rows of which LDS holds two groups' tiles
+    p.key_groups = p.blocks == 1 ? (wide ? 2 : 4) : p.blocks == 2 ? 2 : 1;
+    want = (p.key_groups > 1 ? 512 : 768) / ((int64_t)d.L * d.Hkv * p.tiles);
+    if (p.key_groups > 1 && want > 32) want = 32;
+    least = p.key_groups > 1 ? 256 : 128;
   } else {
     want = 2048 / ((int64_t)d.L * count * d.Hkv);
     least = 256;

@@ -183,7 +183,8 @@ struct PrefixArgs {
   float* o; float2* ms; int32_t* n; int64_t heads;   // as PrefixPart has them
 };
 // How the matrix-core kernel's rows are dealt out: `tiles` workgroups of up to `blocks` wavefronts of 32 rows per piece.
-struct PrefixPlan { int32_t splits, tiles, blocks; };
+// key_groups: groups of so many wavefronts in a workgroup, which take its keys in turn.
+struct PrefixPlan { int32_t splits, tiles, blocks, key_groups; };
 hipError_t gkv_launch_prefix_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a, const PrefixPlan& plan);
 hipError_t gkv_launch_prefix_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a);
 hipError_t gkv_launch_fill_zero(hipStream_t stream, int32_t* p, size_t n);
@@ -306,8 +307,9 @@ __device__ __forceinline__ float inverse_total(float total, bool any_key) {
 }
 // Joins a prefix's pieces of one head with the sequence's own sum o of weighted values (channels c .. c + 3; maximum m, sum l).
 typedef float gkv_f32x4 __attribute__((ext_vector_type(4)));
+// AT_ONCE pieces are on their way together.
+template <int AT_ONCE>
 struct PrefixPieces {
-  static constexpr int AT_ONCE = 4;
   float2 ms[AT_ONCE];
   gkv_f32x4 o[AT_ONCE];
   __device__ __forceinline__ void request(const PrefixPart& p, size_t head, int d, int c, int s0, int n) {

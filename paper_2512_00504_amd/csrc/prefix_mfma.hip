@@ -10,8 +10,10 @@
 //   bf16 rounds P to bf16 (to the nearest; 2^-9 of the value, and the sum is of the unrounded weights).
 // LDS holds a tile's rows as they are, their 16-byte pieces exchanged within the row so that neither kind of read finds two
 // rows in the same banks.
-// Bound: HBM with few rows; with several hundred the vector unit: 32 keys of 32 rows take 16 products (512 cycles) and about
-// 16 x (maximum, fma, exponential, sum, conversion).
+// Bound: HBM with few rows.  With several hundred the products and the vector unit in turn: 32 keys of 32 rows are 16 products (512
+// cycles) and 16 x (maximum, fma, exponential, sum, half a conversion), about as many; what a wavefront does of one does not overlap
+// with the other, and three of them on a SIMD overlap little (counters, 64 sequences x 16384 rows: products 48% of the time, vector
+// instructions 51%).  Two tiles' logits in turn within a wavefront, which takes the registers of the third: 117 -> 138 us.
 #include "gkv_internal.h"
 
 #include <type_traits>
@@ -67,17 +69,21 @@ __device__ __forceinline__ V in_lds(uint32_t at) { return *(const __attribute__(
 struct KernelArgs {
   PrefixArgs p;
   int32_t L, B, Hq, Hkv, g, tiles, blocks, groups;          // row tiles; blocks of 32 rows per tile at most; (layer, KV head, piece)s
-  GkvDivisor by_tiles, by_splits, by_hkv, by_g;
+  GkvDivisor by_tiles, by_splits, by_hkv, by_g, by_blocks;
   float scale_hi, scale_lo;
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void prefix_mfma_kernel(KernelArgs a) {
+// NK: groups of a.blocks wavefronts that share the rows and take the tiles in turn (joined through LDS at the end): with one or two
+// blocks of rows they make a workgroup of four wavefronts, and the prefix is cut into fewer pieces for the decode kernel to join.
+template <typename T, int D, int NK>
+__global__ __launch_bounds__(256, sizeof(T) * D >= 512 && NK > 1 ? 1 : NK > 1 || sizeof(T) == 4 ? 2 : 3) void prefix_mfma_kernel(KernelArgs a) {
   using G = Geo<T, D>;
   constexpr int SUB = G::TK / 32, CB = D / 32;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];     // [2][K, V][TILE]
-  const int tid = threadIdx.x, lane = tid & 63, nw = blockDim.x >> 6;
+  constexpr uint32_t BUF = NK * 2 * G::TILE;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];     // [2][NK][K, V][TILE]
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ki = NK == 1 ? 0 : quotient(wave, a.by_blocks), mi = wave - ki * a.blocks;      // group, block of rows
   const int lr = lane & 31, h = lane >> 5;
 
   // Workgroups go to the XCDs in turn: the row tiles of one piece of the prefix go to the same one, and find it in its L2.
@@ -88,29 +94,30 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void prefix_mfma_kerne
   const int unit = quotient(group, a.by_splits), split = group - unit * a.p.splits;
   const int layer = quotient(unit, a.by_hkv), j = unit - layer * a.Hkv;
   const int n0 = split * a.p.split_rows, n1 = min(a.p.rows, n0 + a.p.split_rows);
-  const int n_tiles = (n1 - n0 + G::TK - 1) / G::TK;
+  const int n_tiles = (n1 - n0 + G::TK - 1) / G::TK, n_rounds = (n_tiles + NK - 1) / NK;
   const char* Kp = (const char*)a.p.K + (((size_t)layer * a.Hkv + j) * a.p.capacity + n0) * G::ROW;
   const char* Vp = (const char*)a.p.V + (((size_t)layer * a.Hkv + j) * a.p.capacity + n0) * G::ROW;
 
   const int n_rows = a.p.count * a.g;
-  const int row = (tile * a.blocks + wave) * 32 + lr, safe = min(row, n_rows - 1);
+  const int row = (tile * a.blocks + mi) * 32 + lr, safe = min(row, n_rows - 1);
   const int seq = quotient(safe, a.by_g);
   const size_t head = ((size_t)layer * a.B + a.p.first + seq) * a.Hq + j * a.g + (safe - seq * a.g);
   u32x4 q[D * sizeof(T) / 32];                               // chunks 2 c + h
 #pragma unroll
   for (int c = 0; c < D * (int)sizeof(T) / 32; ++c) q[c] = ld16((const char*)a.p.q + head * G::ROW + (2 * c + h) * 16);
 
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-  auto bring = [&](int t, int buf) {
-    const int first = t * G::TK, last = n1 - n0 - 1;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + ki * 2 * G::TILE;
+  auto bring = [&](int r) {                                  // the group's tile of round r
+    const int first = (r * NK + ki) * G::TK, last = n1 - n0 - 1 - first;
+    if (NK > 1 && last < 0) return;
     const char* kt = Kp + (size_t)first * G::ROW;
     const char* vt = Vp + (size_t)first * G::ROW;
-    for (int x = wave; x < G::PIECES; x += nw) {
+    const uint32_t to = lds0 + (r & 1) * BUF;
+    for (int x = mi; x < G::PIECES; x += a.blocks) {
       const int at = x * G::ROWS_PIECE + lane / G::CHUNKS, chunk = lane % G::CHUNKS;
-      const int src = min(at, last - first);                 // rows behind the end repeat its last one
-      const uint32_t ko = src * G::ROW + (chunk ^ G::k_swap(at)) * 16, vo = src * G::ROW + (chunk ^ G::v_swap(at)) * 16;
-      to_lds(kt, ko, lds0 + buf * 2 * G::TILE + x * 1024);
-      to_lds(vt, vo, lds0 + buf * 2 * G::TILE + G::TILE + x * 1024);
+      const int src = min(at, last);                         // rows behind the end repeat its last one
+      to_lds(kt, src * G::ROW + (chunk ^ G::k_swap(at)) * 16, to + x * 1024);
+      to_lds(vt, src * G::ROW + (chunk ^ G::v_swap(at)) * 16, to + G::TILE + x * 1024);
     }
   };
 
@@ -136,11 +143,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void prefix_mfma_kerne
   // One tile of `there` keys, in the buffer that begins at `buf`; last: it may have fewer than TK.
   auto work = [&](uint32_t buf, int there, auto last) {
     constexpr bool LAST = decltype(last)::value;
-    if constexpr (LAST) {                                    // V behind the end is zero
-      char* end = smem + buf + G::TILE + there * G::ROW;
-      for (int x = tid; x < (G::TK - there) * G::CHUNKS; x += nw * 64) *(u32x4*)(end + x * 16) = u32x4{0u, 0u, 0u, 0u};
-      __syncthreads();
-    }
     f32x16 s[SUB];
 #pragma unroll
     for (int i = 0; i < SUB; ++i) {
@@ -208,7 +210,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void prefix_mfma_kerne
         for (int e = 0; e < 16; ++e) {
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb) {
-            const float v = in_lds<float>(v_at[cb] + buf + (32 * i + 8 * (e >> 2) + (e & 3)) * G::ROW);
+            float v = in_lds<float>(v_at[cb] + buf + (32 * i + 8 * (e >> 2) + (e & 3)) * G::ROW);
+            if (LAST && 32 * i + 8 * (e >> 2) + 4 * h + (e & 3) >= there) v = 0.f;
             o[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i][e], o[cb], 0, 0, 0);
           }
         }
@@ -225,7 +228,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void prefix_mfma_kerne
 #pragma unroll
             for (int y = 0; y < 2; ++y)
               v[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)(v_at[cb] + buf + (32 * i + 16 * k + 8 * y) * G::ROW));
-            const u32x2 v0 = __builtin_bit_cast(u32x2, v[0]), v1 = __builtin_bit_cast(u32x2, v[1]);
+            u32x2 v0 = __builtin_bit_cast(u32x2, v[0]), v1 = __builtin_bit_cast(u32x2, v[1]);
+            if constexpr (LAST) {                            // V behind the end is zero
+              const int left = there - (32 * i + 16 * k + 4 * h);
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                v0[y] &= (left > 2 * y ? 0x0000ffffu : 0u) | (left > 2 * y + 1 ? 0xffff0000u : 0u);
+                v1[y] &= (left > 8 + 2 * y ? 0x0000ffffu : 0u) | (left > 8 + 2 * y + 1 ? 0xffff0000u : 0u);
+              }
+            }
             o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, (u32x4{v0[0], v0[1], v1[0], v1[1]})),
                                                             __builtin_bit_cast(bf16x8, p), o[cb], 0, 0, 0);
           }
@@ -233,27 +244,57 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void prefix_mfma_kerne
       }
     }
   };
-  // The next tile's buffer is the one that everybody is through with at the barrier.
+  // The next round's buffer is the one that everybody is through with at the barrier.
   auto there_now = [] {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wavefront's share of the tile
     __syncthreads();                                         // and everybody's
   };
-  if (n_tiles > 0) {
-    bring(0, 0);
+  if (n_rounds > 0) {
+    bring(0);
     uint32_t buf = 0;
-    for (int t = 0;; t += 2) {
+    for (int r = 0;; r += 2) {
       there_now();
-      if (t == n_tiles - 1) break;
-      bring(t + 1, 1);
+      if (r == n_rounds - 1) break;
+      bring(r + 1);
       work(0, G::TK, std::false_type{});
       there_now();
-      buf = 2 * G::TILE;
-      if (t + 1 == n_tiles - 1) break;
+      buf = BUF;
+      if (r + 1 == n_rounds - 1) break;
       buf = 0;
-      bring(t + 2, 0);
-      work(2 * G::TILE, G::TK, std::false_type{});
+      bring(r + 2);
+      work(BUF, G::TK, std::false_type{});
     }
-    work(buf, n1 - n0 - (n_tiles - 1) * G::TK, std::true_type{});
+    const int t = (n_rounds - 1) * NK + ki;
+    if (NK == 1 || t == n_tiles - 1) work(buf, n1 - n0 - t * G::TK, std::true_type{});
+    else if (t < n_tiles - 1) work(buf, G::TK, std::false_type{});
+  }
+  if constexpr (NK > 1) {
+    // the groups' results, lane by lane: 4 x CB pieces of 16 bytes, and (m, l)
+    __syncthreads();
+    constexpr int PER = 64 * (16 * CB + 2);                  // floats of a wavefront
+    float* mine = (float*)smem + (size_t)(wave - a.blocks) * PER;   // (the first group keeps its own)
+    if (ki > 0) {
+#pragma unroll
+      for (int i = 0; i < 4 * CB; ++i)
+        *(f32x4*)(mine + (i * 64 + lane) * 4) = f32x4{o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2], o[i >> 2][4 * (i & 3) + 3]};
+      *(f32x2*)(mine + 64 * 16 * CB + lane * 2) = f32x2{m, l};
+    }
+    __syncthreads();
+    if (ki > 0) return;
+#pragma unroll 1
+    for (int k = 1; k < NK; ++k) {
+      const float* other = (float*)smem + (size_t)((k - 1) * a.blocks + mi) * PER;
+      const f32x2 ml = *(const f32x2*)(other + 64 * 16 * CB + lane * 2);
+      const float mn = fmaxf(m, ml[0]), f = __builtin_amdgcn_exp2f(m - mn), g = __builtin_amdgcn_exp2f(ml[0] - mn);
+      l = l * f + ml[1] * g;
+      m = mn;
+#pragma unroll
+      for (int i = 0; i < 4 * CB; ++i) {
+        const f32x4 x = *(const f32x4*)(other + (i * 64 + lane) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i >> 2][4 * (i & 3) + e] = o[i >> 2][4 * (i & 3) + e] * f + x[e] * g;
+      }
+    }
   }
   if (row >= n_rows) return;
   l = over_halves(l, false);
@@ -270,20 +311,36 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : 3) void prefix_mfma_kerne
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, int NK>
 hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const PrefixArgs& p, const PrefixPlan& plan) {
   KernelArgs a{p, dm.L, dm.B, dm.Hq, dm.Hkv, dm.g, plan.tiles, plan.blocks, dm.L * dm.Hkv * p.splits,
-               gkv_divisor(plan.tiles), gkv_divisor(p.splits), dm.by_hkv, gkv_divisor(dm.g), dm.scale_l2_hi, dm.scale_l2_lo};
+               gkv_divisor(plan.tiles), gkv_divisor(p.splits), dm.by_hkv, gkv_divisor(dm.g), gkv_divisor(plan.blocks),
+               dm.scale_l2_hi, dm.scale_l2_lo};
   const int64_t grid = (int64_t)(a.groups + 7) / 8 * 8 * plan.tiles;
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  constexpr size_t shmem = 4 * Geo<T, D>::TILE;
-  static_assert(shmem <= GKV_LDS_LIMIT, "a workgroup gets 64 KiB");
-  return gkv_launch(ln, prefix_mfma_kernel<T, D>, dim3((unsigned)grid), dim3(plan.blocks * 64), shmem, a);
+  constexpr size_t shmem = NK * 4 * Geo<T, D>::TILE;
+  // the results of all groups but the first: (NK - 1) * blocks wavefronts, four in all at most
+  static_assert(shmem <= 131072 && (NK == 1 || shmem >= (NK == 4 ? 3 : 2) * 64 * (D / 2 + 2) * sizeof(float)), "tiles, or the groups' results");
+  if (plan.blocks * NK > 4) return hipErrorInvalidConfiguration;
+  auto kern = prefix_mfma_kernel<T, D, NK>;
+  if (shmem > GKV_LDS_LIMIT) {                               // beyond the default per-workgroup limit: opt in (a CU holds 160 KiB)
+    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
+    if (e != hipSuccess) return e;
+  }
+  return gkv_launch(ln, kern, dim3((unsigned)grid), dim3(plan.blocks * NK * 64), shmem, a);
+}
+
+template <typename T, int D>
+hipError_t launch_groups(const GkvLaunch& ln, const GkvDims& dm, const PrefixArgs& p, const PrefixPlan& plan) {
+  if constexpr (sizeof(T) * D < 512) {
+    if (plan.key_groups == 4) return launch<T, D, 4>(ln, dm, p, plan);
+  }
+  return plan.key_groups == 2 ? launch<T, D, 2>(ln, dm, p, plan) : launch<T, D, 1>(ln, dm, p, plan);
 }
 
 }  // namespace
 
 hipError_t gkv_launch_prefix_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a, const PrefixPlan& plan) {
-  if (dtype == GKV_F32) return dm.d == 64 ? launch<float, 64>(ln, dm, a, plan) : launch<float, 128>(ln, dm, a, plan);
-  return dm.d == 64 ? launch<uint16_t, 64>(ln, dm, a, plan) : launch<uint16_t, 128>(ln, dm, a, plan);
+  if (dtype == GKV_F32) return dm.d == 64 ? launch_groups<float, 64>(ln, dm, a, plan) : launch_groups<float, 128>(ln, dm, a, plan);
+  return dm.d == 64 ? launch_groups<uint16_t, 64>(ln, dm, a, plan) : launch_groups<uint16_t, 128>(ln, dm, a, plan);
 }

@@ -310,6 +310,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   // requested at once: the record, the step counter, the group's queries, the new row
   int4 rec = *(const int4*)(a.d_state + 4 * (size_t)lb);
   const int32_t base = *a.step_base;
+  const int32_t prefix_n = *(a.prefix.o ? a.prefix.n + head0 : a.d_state);   // pieces of the prefix, the same for all heads of a sequence
   u32x4 qraw[G::NL][2][G::F32 ? 2 : 1];
 #pragma unroll
   for (int c = 0; c < G::NL; ++c)
@@ -323,6 +324,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   load4<T>((may_grow ? (which ? a.v_new : a.k_new) + (size_t)unit * ROW_BYTES : q_g) + min(nr, D / 4 - 1) * 4 * sizeof(T), fresh4);
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("" : "+s"(rec.x), "+s"(rec.y), "+s"(rec.w));
+  const int n_pre = a.prefix.o ? prefix_n : 0;
 
   const SeqState seq = state_record(rec);
   const int step = a.step + (a.has_base ? base : 0);
@@ -435,19 +437,18 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   float* part = a.partials + (size_t)(unit * splits) * g * PSTR;
   const int slot = step - quotient(step, a.by_w) * a.w;
   float2* stats = a.stats + (size_t)slot * a.LB * a.Hq + head0;
-  const int n_pre = a.prefix.o ? a.prefix.n[head0] : 0;      // uniform, the same for all heads of a sequence
-  PrefixPieces pre;
+  constexpr int PRE = 4;                    // pieces of the prefix at once (with 8 or 16 it takes no less)
+  PrefixPieces<PRE> pre;
   // the unit's result; ready: the first pieces of the prefix are in `pre`
   auto finish = [&](int x, int h, int c4, float M, float L, f32x4 o, bool ready) {
     if (c4 == 0 && a.write_stats) stats[h] = make_float2(M, L);
     bool any_key = n_tot > 0;
-    for (int s0 = 0; s0 < n_pre; s0 += PrefixPieces::AT_ONCE) {
+    for (int s0 = 0; s0 < n_pre; s0 += PRE) {
       if (s0 > 0 || !ready) pre.request(a.prefix, head0 + h, D, c4, s0, n_pre);
       pre.join(s0, n_pre, M, L, o, any_key);
     }
     store_row4(out + (uint32_t)(x * 4), o * inverse_total(L, any_key));
   };
-  if (ns == 1 && n_pre > 0 && tid < g * TPH) pre.request(a.prefix, head0 + tid / TPH, D, (tid % TPH) * 4, 0, n_pre);
   __syncthreads();
   for (int x = tid; x < g * TPH; x += NW * 64) {
     const int h = x / TPH, c4 = (x % TPH) * 4;
@@ -463,7 +464,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
       o += *(const f32x4*)(so + (i * g + h) * OSTR + c4) * f;
     }
     if (ns == 1) {
-      finish(x, h, c4, M, L, o, x == tid);
+      finish(x, h, c4, M, L, o, false);
     } else {
       float* ph = part + (uint32_t)((sp * g + h) * PSTR);
       store_agent(ph + c4, o[0], o[1]);
@@ -480,6 +481,9 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (lane == 0) arrived = __builtin_amdgcn_atomic_inc32((uint32_t*)a.ticket + (size_t)unit * GKV_TICKETS + wave, (uint32_t)ns - 1u, __ATOMIC_RELAXED, "agent");
   }
+
+  // (the prefix's first pieces, on their way while the ticket is)
+  if (joins && n_pre > 0 && tid < g * TPH) pre.request(a.prefix, head0 + tid / TPH, D, (tid % TPH) * 4, 0, n_pre);
 
   // ---- the new row, its scales and position, and q into the ring -----------------------------------
   if (sp == 0) {
@@ -526,7 +530,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
             o += f32x4{got[i][1].x, got[i][1].y, got[i][2].x, got[i][2].y} * f;
           }
       }
-      finish(x, h, c4, M, L, o, false);
+      finish(x, h, c4, M, L, o, x == tid);
     }
   }
 }
