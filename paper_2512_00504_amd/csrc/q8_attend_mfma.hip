@@ -71,7 +71,7 @@ struct Geo {
   static constexpr int NC = D / 16;                          // channels per lane, accumulators
   static constexpr int VW = D / 64;                          // words of V per lane and key
   static constexpr int QP = F32 ? 3 : 1;                     // bf16 parts of a query
-  static constexpr int PP = F32 ? 3 : 2;                     // of a probability
+  static constexpr int PP = F32 ? 3 : 1;                     // of a probability
   static constexpr int ROW_BYTES = D * (int)sizeof(T);       // of q, out and the new rows
   static constexpr int OSTR = D + 4, PSTR = D + 2;           // LDS rows of partial outputs; pieces in memory: o[D], m, l
 };
@@ -94,7 +94,7 @@ struct Rows {
 };
 
 template <typename T, int D>
-__device__ __forceinline__ void request(Slice<T, D>& x, const Rows<T, D>& at, int it) {
+__device__ __forceinline__ void request_k(Slice<T, D>& x, const Rows<T, D>& at, int it) {
   using G = Geo<T, D>;
 #pragma unroll
   for (int tt = 0; tt < G::KT; ++tt) {
@@ -105,23 +105,34 @@ __device__ __forceinline__ void request(Slice<T, D>& x, const Rows<T, D>& at, in
     const uint32_t step = tiled ? 1024 : 64;
 #pragma unroll
     for (int c = 0; c < G::NL; ++c) x.k[tt][c] = ld16(p + c * step);
-    x.scale[tt] = ld16((const char*)at.scales + (uint32_t)(t * 64) + at.s);
   }
+}
+template <typename T, int D, bool ONCE>
+__device__ __forceinline__ void request_v(Slice<T, D>& x, const Rows<T, D>& at, int it) {
+  using G = Geo<T, D>;
 #pragma unroll
   for (int tt = 0; tt < G::KT; ++tt) {
     const int t = G::KT > 2 ? min(it * G::KT + tt, at.last_tile) : it * G::KT + tt;
+    x.scale[tt] = ld16((const char*)at.scales + (uint32_t)(t * 64) + at.s);
     const uint8_t* p = at.V + (uint32_t)(t * 16 * D) + at.v;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if constexpr (G::VW == 2) {
-        const u32x2 a = __builtin_nontemporal_load((const u32x2*)(p + e * D));
+        const u32x2 a = ONCE ? __builtin_nontemporal_load((const u32x2*)(p + e * D)) : *(const u32x2*)(p + e * D);
         x.v[4 * tt + e].w[0] = a[0]; x.v[4 * tt + e].w[1] = a[1];
       } else {
-        x.v[4 * tt + e].w[0] = __builtin_nontemporal_load((const uint32_t*)(p + e * D));
+        x.v[4 * tt + e].w[0] = ONCE ? __builtin_nontemporal_load((const uint32_t*)(p + e * D)) : *(const uint32_t*)(p + e * D);
       }
     }
   }
 }
+
+template <typename T, int D, bool ONCE>
+__device__ __forceinline__ void request(Slice<T, D>& x, const Rows<T, D>& at, int it) {
+  request_k<T, D>(x, at, it);
+  request_v<T, D, ONCE>(x, at, it);
+}
+struct Nothing { __device__ void operator()() const {} };
 
 template <int NC>
 struct Running {
@@ -148,9 +159,10 @@ struct NewRow { const uint8_t *k, *v; uint32_t word; int row; };
 // edge: the slice holds the unit's end: rows behind it are zeros of scale zero, masked, and the new row is taken from its place in
 // LDS.  EXACT: right for every logit (see log2_weight); without it a logit of -inf may give NaN and a huge maximum any
 // weight, which shows at the end.
-template <typename T, int D, bool EXACT>
+// between: what to do once the products with K are under way, whose registers are free then.
+template <typename T, int D, bool EXACT, typename Between>
 __device__ __forceinline__ void process(Slice<T, D>& x, Running<D / 16>& st, const u32x4 (&q)[Geo<T, D>::NL][2][Geo<T, D>::QP], int it,
-                                        bool edge, float hi, float lo, int r, int kb, int n_tot, const NewRow& fresh) {
+                                        bool edge, float hi, float lo, int r, int kb, int n_tot, const NewRow& fresh, Between between) {
   using G = Geo<T, D>;
   constexpr int NS = 4 * G::KT;
   const int key0 = it * G::KEYS;
@@ -181,20 +193,29 @@ __device__ __forceinline__ void process(Slice<T, D>& x, Running<D / 16>& st, con
     }
   }
   float z[NS];
+  f32x4 acc[G::KT];
 #pragma unroll
   for (int tt = 0; tt < G::KT; ++tt) {
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    acc[tt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < G::NL; ++c)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const bf16x8 a = as_bf16x8(eight(x.k[tt][c][2 * h], x.k[tt][c][2 * h + 1]));
 #pragma unroll
-        for (int p = 0; p < G::QP; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, as_bf16x8(q[c][h][p]), acc, 0, 0, 0);
+        for (int p = 0; p < G::QP; ++p) acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, as_bf16x8(q[c][h][p]), acc[tt], 0, 0, 0);
       }
+  }
+  if constexpr (!std::is_same_v<Between, Nothing>) {
+    __builtin_amdgcn_sched_barrier(0);
+    between();
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int tt = 0; tt < G::KT; ++tt) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      z[4 * tt + e] = acc[e] * q8_k_scale(x.scale[tt][e]);
+      z[4 * tt + e] = acc[tt][e] * q8_k_scale(x.scale[tt][e]);
       if (edge && key0 + 16 * tt + 4 * kb + e >= n_tot) z[4 * tt + e] = EXACT ? -INFINITY : -1e30f;
     }
   }
@@ -202,8 +223,10 @@ __device__ __forceinline__ void process(Slice<T, D>& x, Running<D / 16>& st, con
 #pragma unroll
   for (int i = 1; i < NS; ++i) mx = fmaxf(mx, z[i]);
   mx = over_head(mx, true);
-  const float m_new = fmaxf(st.m, rounded_product(mx, hi));
-  if (__any(m_new > st.m)) {
+  // m follows the largest logit at a distance of up to 8 (weights up to 256): moving it takes a product for every accumulator
+  const float top = rounded_product(mx, hi);
+  if (__any(top > st.m + 8.f)) {
+    const float m_new = fmaxf(st.m, top);
     const float f = __builtin_amdgcn_exp2f(st.m - m_new);
     st.l *= f;
 #pragma unroll
@@ -292,7 +315,7 @@ __device__ __forceinline__ void load4(const char* p, float (&x)[4]) {
 
 // Dynamic LDS: float so[NW][g][OSTR], sm[16][NW], sl[16][NW]; the new row's codes, K then V, per wavefront.
 // DEPTH: slices in flight.
-template <typename T, int D, int NW, int OCC, int DEPTH>
+template <typename T, int D, int NW, int OCC, int DEPTH, bool ONCE>
 __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs a) {
   using G = Geo<T, D>;
   constexpr int ROW_BYTES = G::ROW_BYTES, OSTR = G::OSTR, PSTR = G::PSTR;
@@ -344,8 +367,8 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   at.k_tiled = lane * 16; at.k_rows = r * D + kb * 16; at.v = kb * 4 * D + r * G::NC; at.s = kb * 16;
 
   Slice<T, D> s[DEPTH];
-  request(s[0], at, min(it0, max(n_iter - 1, 0)));           // (wavefronts beyond the end ask for its last slice and do not use it)
-  if constexpr (DEPTH > 1) request(s[1], at, min(it0 + stride, max(n_iter - 1, 0)));
+  request<T, D, ONCE>(s[0], at, min(it0, max(n_iter - 1, 0)));           // (wavefronts beyond the end ask for its last slice and do not use it)
+  if constexpr (DEPTH > 1) request<T, D, ONCE>(s[1], at, min(it0 + stride, max(n_iter - 1, 0)));
 
   // while that is on its way: the queries' parts, and the new row's codes
   u32x4 q[G::NL][2][G::QP];
@@ -388,30 +411,31 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   };
   reset();
   auto work = [&](Slice<T, D>& x, int it, auto exact) {
-    process<T, D, decltype(exact)::value>(x, st, q, it, it == n_iter - 1, a.scale_hi, a.scale_lo, r, kb, n_tot, fresh);
+    process<T, D, decltype(exact)::value>(x, st, q, it, it == n_iter - 1, a.scale_hi, a.scale_lo, r, kb, n_tot, fresh, Nothing{});
   };
   if (it0 < n_iter) {
     if constexpr (DEPTH == 1) {
-      for (int it = it0;;) {
-        work(s[0], it, std::false_type{});
-        if ((it += stride) >= n_iter) break;
-        request(s[0], at, it);
+      int it = it0;
+      for (; it + stride < n_iter; it += stride) {
+        process<T, D, false>(s[0], st, q, it, false, a.scale_hi, a.scale_lo, r, kb, n_tot, fresh, [&] { request_k<T, D>(s[0], at, it + stride); });
+        request_v<T, D, ONCE>(s[0], at, it + stride);
       }
+      work(s[0], it, std::false_type{});
     } else {
       for (int it = it0;;) {
         work(s[0], it, std::false_type{});
         if (it + stride >= n_iter) break;
-        request(s[0], at, min(it + 2 * stride, n_iter - 1));
+        request<T, D, ONCE>(s[0], at, min(it + 2 * stride, n_iter - 1));
         work(s[1], it + stride, std::false_type{});
         if ((it += 2 * stride) >= n_iter) break;
-        request(s[1], at, min(it + stride, n_iter - 1));
+        request<T, D, ONCE>(s[1], at, min(it + stride, n_iter - 1));
       }
     }
     // seldom: a maximum that the short form of the weights is not right for, or a NaN that may be its doing
     if (__any(fabsf(st.m) >= GKV_HUGE_LOG2 || st.l != st.l)) {
       reset();
       for (int it = it0; it < n_iter; it += stride) {
-        request(s[0], at, it);
+        request<T, D, ONCE>(s[0], at, it);
         work(s[0], it, std::true_type{});
       }
     }
@@ -535,7 +559,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   }
 }
 
-template <typename T, int D, int NW, int OCC, int DEPTH>
+template <typename T, int D, int NW, int OCC, int DEPTH, bool ONCE = false>
 hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const Q8AttendArgs& a) {
   KernelArgs k;
   k.d_state = a.d_state; k.step_base = dm.step_base ? dm.step_base : a.d_state;
@@ -548,7 +572,7 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const Q8AttendArgs& a)
   k.Hq = dm.Hq; k.Hkv = dm.Hkv; k.g = dm.g; k.cap = dm.cap; k.LB = dm.L * dm.B; k.w = dm.w; k.step = a.step;
   k.has_base = dm.step_base != nullptr; k.copy_q = a.copy_q; k.write_stats = a.write_stats;
   k.scale_hi = dm.scale_l2_hi; k.scale_lo = dm.scale_l2_lo; k.prefix = a.prefix;
-  return gkv_launch(ln, q8_attend_mfma_kernel<T, D, NW, OCC, DEPTH>, dim3(dm.L * dm.B * dm.Hkv * a.splits), dim3(NW * 64),
+  return gkv_launch(ln, q8_attend_mfma_kernel<T, D, NW, OCC, DEPTH, ONCE>, dim3(dm.L * dm.B * dm.Hkv * a.splits), dim3(NW * 64),
                     gkv_q8_attend_mfma_lds(D, dm.g, NW), k);
 }
 
@@ -558,7 +582,9 @@ hipError_t launch_waves(const GkvLaunch& ln, const GkvDims& dm, const Q8AttendAr
   constexpr int OCC = sizeof(T) == 4 ? 2 : 3;                // wavefronts per SIMD that the registers of one slice leave room for
   if (a.waves == 8) return launch<T, D, 8, 2, 1>(ln, dm, a);
   if (workgroups <= 256) return launch<T, D, 4, 2, 2>(ln, dm, a);
-  return launch<T, D, 4, OCC, 1>(ln, dm, a);
+  // V of caches beyond the 256 MiB memory-side cache is read with non-temporal loads, beside K's ordinary ones
+  const bool once = (int64_t)dm.L * dm.B * dm.Hkv * (dm.b + dm.s / 2) * 2 * D > (int64_t)256 << 20;
+  return once ? launch<T, D, 4, OCC, 1, true>(ln, dm, a) : launch<T, D, 4, OCC, 1>(ln, dm, a);
 }
 
 }  // namespace
