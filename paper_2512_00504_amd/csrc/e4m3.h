@@ -46,6 +46,23 @@ __device__ __forceinline__ void q8_values(uint32_t w, float (&x)[4]) {
   const q8_f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
   x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
 }
+// The maximum of numbers that are not negative over groups of 2^log lanes (up to 32), in each of them; through registers, an exchange
+// through LDS takes 60 ns.
+template <int LOG>
+__device__ __forceinline__ float q8_group_max(float v) {
+#define GKV_Q8_DPP(ctrl) v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, 0xF, 0xF, false)))
+  if constexpr (LOG > 0) GKV_Q8_DPP(0xB1);                   // quad_perm [1,0,3,2]
+  if constexpr (LOG > 1) GKV_Q8_DPP(0x4E);                   // quad_perm [2,3,0,1]
+  if constexpr (LOG > 2) GKV_Q8_DPP(LOG > 3 ? 0x124 : 0x141);   // row_ror:4, or the other quad of eight lanes (row_half_mirror)
+  if constexpr (LOG > 3) GKV_Q8_DPP(0x128);                  // row_ror:8
+#undef GKV_Q8_DPP
+  if constexpr (LOG > 4) {
+    const uint32_t u = __float_as_uint(v);
+    const auto y = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+  }
+  return v;
+}
 // Byte offset of (row, 16-byte piece) in one KV head's K block whose first n_tiled rows are in tiled format.
 __device__ __forceinline__ size_t q8_k_offset(int row, int piece, int d, int n_tiled) {
   return row < n_tiled ? (size_t)(row >> 4) * 16 * d + piece * 256 + (row & 15) * 16 : (size_t)row * d + piece * 16;

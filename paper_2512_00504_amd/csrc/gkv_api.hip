@@ -676,7 +676,7 @@ extern "C" gkv_status gkv_q8_store_prompt(gkv_ctx* ctx, const void* k, const voi
     return GKV_ERR_INVALID_ARG;
   const gkv_status st = check_q8(ctx, {k, v, K8, V8, scales});
   if (st != GKV_OK) return st;
-  Q8StoreArgs a{k, v, n, t_first, t0, d_prompt_len, (uint8_t*)K8, (uint8_t*)V8, (uint32_t*)scales, pos, 0, 0};
+  Q8StoreArgs a{k, v, n, t_first, t0, d_prompt_len, (uint8_t*)K8, (uint8_t*)V8, (uint32_t*)scales, pos, 0};
   GkvLaunch ln{ctx, -1, (hipStream_t)stream};
   return hip_status(gkv_launch_q8_store(ln, ctx->dims, ctx->cfg.dtype, a));
 }

@@ -152,7 +152,7 @@ hipError_t gkv_launch_evicted_positions(const GkvLaunch& ln, const GkvDims& dm, 
 struct Q8StoreArgs {
   const void* k; const void* v; int32_t n, t_first, t0; const int32_t* prompt_len;
   uint8_t* K8; uint8_t* V8; uint32_t* scales; int32_t* pos;
-  int32_t rows, lanes_log;      // of a workgroup; lanes a row (set by the launch)
+  int32_t rows;                 // of a workgroup (set by the launch)
 };
 struct Q8ReadArgs {
   const uint8_t* K8; const uint8_t* V8; const uint32_t* scales; const int32_t* d_state; int32_t step;
@@ -165,8 +165,8 @@ struct Q8AttendArgs {
   PrefixPart prefix;
   GkvWorkspace ws; int32_t splits, split_iters, waves, copy_q, write_stats;   // as in AttendArgs
 };
-hipError_t gkv_launch_q8_store(const GkvLaunch& ln, const GkvDims& dm, int dtype, Q8StoreArgs a);
-hipError_t gkv_launch_q8_read(const GkvLaunch& ln, const GkvDims& dm, int dtype, Q8ReadArgs a);
+hipError_t gkv_launch_q8_store(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8StoreArgs& a);
+hipError_t gkv_launch_q8_read(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8ReadArgs& a);
 hipError_t gkv_launch_q8_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8AttendArgs& a);
 size_t gkv_q8_attend_mfma_lds(int d, int g, int waves);   // LDS of a workgroup of that kernel (bytes)
 hipError_t gkv_launch_q8_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8AttendArgs& a);

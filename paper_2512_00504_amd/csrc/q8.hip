@@ -5,7 +5,11 @@
 namespace {
 
 __device__ __forceinline__ q8_u32x4 ld16(const void* p) { return *(const q8_u32x4*)p; }
-__device__ __forceinline__ void st16(void* p, q8_u32x4 v) { *(q8_u32x4*)p = v; }
+template <bool ONCE = false>
+__device__ __forceinline__ void st16(void* p, q8_u32x4 v) {
+  if constexpr (ONCE) __builtin_nontemporal_store(v, (q8_u32x4*)p);
+  else *(q8_u32x4*)p = v;
+}
 
 // Sixteen elements of a row, as floats.
 template <typename T>
@@ -29,13 +33,13 @@ __device__ __forceinline__ void load16(const T* p, float (&x)[16]) {
     }
   }
 }
-// A row's scale, from the pieces of the `lanes` lanes that share it (a power of two).
-__device__ __forceinline__ uint32_t row_scale(const float (&x)[16], int lanes) {
+// A row's scale, from the pieces of the 2^LANES_LOG lanes that share it.
+template <int LANES_LOG>
+__device__ __forceinline__ uint32_t row_scale(const float (&x)[16]) {
   float m = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) m = fmaxf(m, q8_finite_magnitude(x[i]));
-  for (int o = 1; o < lanes; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-  return q8_scale_field(m);
+  return q8_scale_field(q8_group_max<LANES_LOG>(m));
 }
 __device__ __forceinline__ q8_u32x4 codes16(const float (&x)[16], uint32_t field) {
   const float inv = q8_inverse(field);
@@ -46,32 +50,45 @@ __device__ __forceinline__ q8_u32x4 codes16(const float (&x)[16], uint32_t field
 }
 
 // ---- prompt rows -----------------------------------------------------------------------------
-// A workgroup takes `rows` tokens of one unit; 2^lanes_log lanes a row of K and the same row of V, 16 elements each.
-template <typename T>
+// A workgroup takes `rows` tokens of one unit; 2^LANES_LOG lanes a row of K and the same row of V, 16 elements each, and a lane
+// has ROWS rows on their way.  The source's rows of a unit lie L * B * h_kv rows apart: neighbouring workgroups take neighbouring
+// units.  Bound: HBM.
+template <typename T, int LANES_LOG>
 __global__ __launch_bounds__(256) void q8_store_kernel(GkvDims dm, Q8StoreArgs a) {
+  constexpr int LANES = 1 << LANES_LOG, STRIDE = 256 >> LANES_LOG, ROWS = sizeof(T) == 4 ? 1 : 2;
   const int unit = blockIdx.x, lb = quotient(unit, dm.by_hkv), tid = threadIdx.x;
-  const int lanes = 1 << a.lanes_log, pieces = dm.d >> 4;
+  const int pieces = dm.d >> 4;
   const int64_t units = (int64_t)dm.L * dm.B * dm.Hkv;
   // sequence i's prompt is the positions [t0 - P, t0), its rows 0 .. P - 1
   const int64_t start = (int64_t)a.t0 - a.prompt_len[lb % dm.B];
-  const int piece = tid & (lanes - 1);
+  const int piece = tid & (LANES - 1);
   const bool idle = piece >= pieces;
-  for (int r = (int)blockIdx.y * a.rows + (tid >> a.lanes_log); r < min(a.n, ((int)blockIdx.y + 1) * a.rows); r += 256 >> a.lanes_log) {
-    const int64_t t = (int64_t)a.t_first + r, row = t - start;
-    if (row < 0 || row >= dm.cap || t >= a.t0) continue;             // the same for all lanes of a row
-    const size_t src = ((size_t)r * units + unit) * dm.d + (idle ? 0 : piece * 16);
-    float k[16], v[16];
-    load16((const T*)a.k + src, k);
-    load16((const T*)a.v + src, v);
-    const uint32_t ks = row_scale(k, lanes), vs = row_scale(v, lanes);
-    if (!idle) {
-      const size_t dst = ((size_t)unit * dm.cap + row) * dm.d + piece * 16;
-      st16(a.K8 + dst, codes16(k, ks));
-      st16(a.V8 + dst, codes16(v, vs));
+  const int64_t skip = start - a.t_first;                            // tokens of this call before the prompt's first
+  const int end = (int)max((int64_t)0, min((int64_t)min(a.n, ((int)blockIdx.y + 1) * a.rows), min((int64_t)a.t0 - a.t_first, skip + dm.cap)));
+  int first = (int)blockIdx.y * a.rows;
+  if (skip > first) first = (int)min(skip, (int64_t)end);
+  for (int r0 = first + (tid >> LANES_LOG); r0 < end; r0 += ROWS * STRIDE) {   // the same for all lanes of a row
+    float k[ROWS][16], v[ROWS][16];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const size_t src = ((size_t)min(r0 + i * STRIDE, end - 1) * units + unit) * dm.d + (idle ? 0 : piece * 16);
+      load16((const T*)a.k + src, k[i]);
+      load16((const T*)a.v + src, v[i]);
     }
-    if (piece == 0) {
-      a.scales[(size_t)unit * dm.cap + row] = q8_scale_word(ks, vs);
-      a.pos[(size_t)unit * dm.cap + row] = (int32_t)t;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int r = r0 + i * STRIDE;
+      const uint32_t ks = row_scale<LANES_LOG>(k[i]), vs = row_scale<LANES_LOG>(v[i]);
+      if (r >= end) break;
+      const size_t row = (size_t)unit * dm.cap + (size_t)(r - skip);
+      if (!idle) {
+        st16<true>(a.K8 + row * dm.d + piece * 16, codes16(k[i], ks));
+        st16<true>(a.V8 + row * dm.d + piece * 16, codes16(v[i], vs));
+      }
+      if (piece == 0) {
+        a.scales[row] = q8_scale_word(ks, vs);
+        a.pos[row] = (int32_t)((int64_t)a.t_first + r);
+      }
     }
   }
 }
@@ -99,7 +116,8 @@ __device__ __forceinline__ void store16(uint16_t* p, size_t stride, const float 
 
 // A workgroup takes 16-row tiles of one unit's K (blockIdx.y even) or V, a 16-byte piece of codes a thread; what it
 // writes has the format of the cache that d_state describes.
-template <typename T>
+// ONCE: the codes are read with non-temporal loads (32 x 4 units of 1090 rows 26.4 -> 23.9 us; 1792 of 1151 325 -> 328, so up to 256 MiB of output).
+template <typename T, bool ONCE>
 __global__ __launch_bounds__(256) void q8_read_kernel(GkvDims dm, Q8ReadArgs a) {
   constexpr int EPC = Elem<T>::EPC;
   const int step = resolve_step(dm, a.step);
@@ -116,7 +134,8 @@ __global__ __launch_bounds__(256) void q8_read_kernel(GkvDims dm, Q8ReadArgs a) 
     const bool tiled = isK && first + 16 * tile < st.n_tiled;
     const int row = first + 16 * tile + (tiled ? in & 15 : in / pieces), piece = tiled ? in >> 4 : in % pieces;
     if (row >= end) continue;
-    const q8_u32x4 c = ld16(src + (isK ? q8_k_offset(row, piece, d, st.n_tiled) : (size_t)row * d + piece * 16));
+    const q8_u32x4* from = (const q8_u32x4*)(src + (isK ? q8_k_offset(row, piece, d, st.n_tiled) : (size_t)row * d + piece * 16));
+    const q8_u32x4 c = ONCE ? __builtin_nontemporal_load(from) : *from;
     const uint32_t word = scales[row];
     const float scale = isK ? q8_k_scale(word) : q8_v_scale(word);
     float y[16];
@@ -299,23 +318,34 @@ __global__ void q8_score_generic_kernel(GkvDims dm, ScoreArgs a) {
 
 }  // namespace
 
-hipError_t gkv_launch_q8_store(const GkvLaunch& ln, const GkvDims& dm, int dtype, Q8StoreArgs a) {
-  const int units = dm.L * dm.B * dm.Hkv, pieces = dm.d / 16;
-  a.lanes_log = 0;
-  while (1 << a.lanes_log < pieces) ++a.lanes_log;
-  a.rows = 256 >> a.lanes_log;
+template <typename T, int LANES_LOG>
+static hipError_t launch_store(const GkvLaunch& ln, const GkvDims& dm, Q8StoreArgs a) {
+  // one round of a workgroup: 896 units, prompts of up to 509 rows, bf16, d = 128, cold: 49 us, four of them 54 (non-temporal stores: 49.5
+  // where ordinary ones take 53.7; non-temporal loads 63)
+  a.rows = (256 >> LANES_LOG) * (sizeof(T) == 4 ? 1 : 2);
   while ((a.n + a.rows - 1) / a.rows > 65535) a.rows *= 2;
-  const dim3 grid(units, (a.n + a.rows - 1) / a.rows);
-  if (dtype == GKV_F32) return gkv_launch(ln, q8_store_kernel<float>, grid, dim3(256), 0, dm, a);
-  return gkv_launch(ln, q8_store_kernel<uint16_t>, grid, dim3(256), 0, dm, a);
+  return gkv_launch(ln, q8_store_kernel<T, LANES_LOG>, dim3(dm.L * dm.B * dm.Hkv, (a.n + a.rows - 1) / a.rows), dim3(256), 0, dm, a);
+}
+template <typename T>
+static hipError_t launch_store(const GkvLaunch& ln, const GkvDims& dm, const Q8StoreArgs& a) {
+  const int pieces = dm.d / 16;                                      // at most 32, a row being at most 1024 bytes
+  return pieces <= 1 ? launch_store<T, 0>(ln, dm, a) : pieces <= 2 ? launch_store<T, 1>(ln, dm, a) : pieces <= 4 ? launch_store<T, 2>(ln, dm, a)
+       : pieces <= 8 ? launch_store<T, 3>(ln, dm, a) : pieces <= 16 ? launch_store<T, 4>(ln, dm, a) : launch_store<T, 5>(ln, dm, a);
+}
+hipError_t gkv_launch_q8_store(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8StoreArgs& a) {
+  return dtype == GKV_F32 ? launch_store<float>(ln, dm, a) : launch_store<uint16_t>(ln, dm, a);
 }
 
-hipError_t gkv_launch_q8_read(const GkvLaunch& ln, const GkvDims& dm, int dtype, Q8ReadArgs a) {
-  const int units = dm.L * dm.B * dm.Hkv;
+template <typename T>
+static hipError_t launch_read(const GkvLaunch& ln, const GkvDims& dm, Q8ReadArgs a) {
+  const int units = dm.L * dm.B * dm.Hkv, caches = a.which == 2 ? 2 : 1;
   a.rows = 128;
-  const dim3 grid(units, (dm.cap + a.rows - 1) / a.rows, a.which == 2 ? 2 : 1);
-  if (dtype == GKV_F32) return gkv_launch(ln, q8_read_kernel<float>, grid, dim3(256), 0, dm, a);
-  return gkv_launch(ln, q8_read_kernel<uint16_t>, grid, dim3(256), 0, dm, a);
+  const bool once = (size_t)units * dm.cap * dm.d * sizeof(T) * caches <= (size_t)256 << 20;
+  return gkv_launch(ln, once ? q8_read_kernel<T, true> : q8_read_kernel<T, false>, dim3(units, (dm.cap + a.rows - 1) / a.rows, caches),
+                    dim3(256), 0, dm, a);
+}
+hipError_t gkv_launch_q8_read(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8ReadArgs& a) {
+  return dtype == GKV_F32 ? launch_read<float>(ln, dm, a) : launch_read<uint16_t>(ln, dm, a);
 }
 
 hipError_t gkv_launch_q8_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const Q8AttendArgs& a) {

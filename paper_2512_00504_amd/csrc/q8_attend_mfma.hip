@@ -391,8 +391,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   if (may_grow) {                                            // uniform
     float top = fmaxf(fmaxf(q8_finite_magnitude(fresh4[0]), q8_finite_magnitude(fresh4[1])),
                       fmaxf(q8_finite_magnitude(fresh4[2]), q8_finite_magnitude(fresh4[3])));
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));    // (lanes beyond the row repeat its end)
+    top = q8_group_max<5>(top);                              // (lanes beyond the row repeat its end)
     const uint32_t field = q8_scale_field(top);
     my_codes = q8_codes(fresh4[0], fresh4[1], fresh4[2], fresh4[3], q8_inverse(field));
     if (nr < D / 4) *(uint32_t*)(codes + which * D + nr * 4) = my_codes;
