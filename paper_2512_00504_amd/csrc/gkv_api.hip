@@ -204,6 +204,9 @@ static int explicit_splits(const gkv_ctx* ctx) {
 // more than 512 units of 64 slices (896 x 2113 159.5 -> 157, ragged to 3900 174 -> 170); in between 4 do (512 x 1100 45.2 against 45.7, 270 x
 // 2000 55.3 / 59.5).  fp32 at D = 128 has 16 KiB slices and stays at 4 (256 x 577 25.6 / 26.9).  With "attend_splits" pieces of 48 slices and more
 // have 8 (2 x 64 units of 2000 fp32 rows, D = 64 18.8 -> 17.8).
+// A cache in 8 bits (q8): slices of 32 keys whatever the head_dim, half the bytes of bf16's.  8 wavefronts where each has a slice (bf16, d = 128 8
+// units of 300 rows 6.4 -> 6.1, 128 of 577 7.8 -> 7.5), and two pieces of a unit only from 100 slices on (128 units of 2113 rows uncut with 8
+// wavefronts 15.1, in two pieces 16.3).
 struct AttendPlan { int waves, splits, iters; };
 
 static AttendPlan attend_plan(const gkv_ctx* ctx, int asked, bool q8 = false) {
@@ -214,7 +217,7 @@ static AttendPlan attend_plan(const gkv_ctx* ctx, int asked, bool q8 = false) {
   const int64_t units = (int64_t)d.L * d.B * d.Hkv;
   const int row_bytes = q8 ? d.d : d.d * ctx->esz;
   const bool wide = row_bytes > 256;                                  // 16 KiB slices
-  const int keys = q8 ? 4096 / d.d : row_bytes == 128 ? 32 : 16;      // per slice
+  const int keys = q8 || row_bytes == 128 ? 32 : 16;                  // per slice
   const int typical = (d.b + d.s / 2 + keys - 1) / keys, full = d.cap / keys;   // slices of a unit
   const bool long_slices = !q8 && ctx->attend_tile == 32 && ctx->cfg.dtype == GKV_BF16 && d.d == 128;   // 4 wavefronts only
   const bool may_have_8 = !wide && fits(8) && !long_slices;
@@ -225,8 +228,8 @@ static AttendPlan attend_plan(const gkv_ctx* ctx, int asked, bool q8 = false) {
     const int most = (int)(256 / units) < 16 ? (int)(256 / units) : 16;
     const int aim = typical > 24 * 7 ? (typical + 23) / 24 : 7, n = aim < most ? aim : most;
     const bool bf16 = q8 || ctx->cfg.dtype == GKV_BF16;
-    const int enough = n == 2 ? (wide ? 12 : bf16 ? 40 : 30) : wide ? 9 : keys >= 32 ? 10 : 18;
-    const int prompt = n == 2 && !wide ? (bf16 ? 64 : 48) : 2 * enough;
+    const int enough = n == 2 ? (wide ? 12 : q8 ? 100 : bf16 ? 40 : 30) : wide ? 9 : keys == 32 ? 10 : 18;
+    const int prompt = n == 2 && !wide && !q8 ? (bf16 ? 64 : 48) : 2 * enough;
     if (n == most && typical >= enough && typical >= 20 * n && may_have_8) {
       p = AttendPlan{8, most, 8};
     } else if (typical >= enough || full >= prompt) {
@@ -237,7 +240,7 @@ static AttendPlan attend_plan(const gkv_ctx* ctx, int asked, bool q8 = false) {
     if (p.splits < 2) p = AttendPlan{4, 1, 0};
   }
   const int slices = (int)((int64_t)d.cap * 2 * row_bytes / 8192);    // in units of 8 KiB, at full capacity
-  const bool more = p.splits == 1 ? (units <= 256 && slices >= (keys >= 32 ? 12 : 16)) || (units > 512 && slices >= 64)
+  const bool more = p.splits == 1 ? (units <= 256 && (q8 ? full >= 8 : slices >= (keys == 32 ? 12 : 16))) || (units > 512 && slices >= 64)
                                   : asked > 0 && slices / p.splits >= 48;
   if (more && may_have_8) p.waves = 8;
   if (ctx->attend_waves > 0) p.waves = fits(ctx->attend_waves) ? ctx->attend_waves : 4;

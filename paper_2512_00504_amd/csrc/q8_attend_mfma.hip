@@ -1,7 +1,7 @@
 // Decode attention over a cache in 8 bits on the matrix cores: head_dim 64 or 128, group size g <= 16, queries in bf16 or fp32.
 //
-// One workgroup of NW wavefronts per (unit, piece).  A wavefront owns slices of KEYS keys (32 at D = 128, 64 at D = 64: 8 KiB of
-// codes) and keeps running maxima, sums and accumulators of all g query heads, so every code is read once per KV head.
+// One workgroup of NW wavefronts per (unit, piece).  A wavefront owns slices of 32 keys and keeps running maxima, sums and accumulators
+// of all g query heads, so every code is read once per KV head.
 //   A row is its codes c_n times 2^e_n, so  q . k_n = 2^ek_n (q . c_n)  and  sum p_n v_n = sum (p_n 2^ev_n) c_n:  the scales
 //   meet the logits and the probabilities, one multiplication per (head, key) each, and never the elements.  A code has 4
 //   significant bits and is exact as a bf16 number, so the products are those of the bf16 matrix cores, 16x16x32.
@@ -10,10 +10,15 @@
 //      result lane (head r, block kb) holds keys 4 kb + e of its head per tile, whose scales are 16 bytes of `scales`.
 //   V: a lane loads D/16 channels of keys 4 kb + e (a quarter-wave reads a row).  O^T[channel, head] += V^T P^T wants two
 //      keys' codes of one channel side by side: one byte permutation for two channels, then the conversion.
-//   fp32 queries and their probabilities enter as the sum of three bf16 numbers, which hold all of their 24 bits; bf16's
-//   probabilities as the sum of two (16 bits).
-// Bound: HBM in launches of some hundred units and more; a slice is about 200 vector instructions and 24 matrix instructions
-// (16 cycles each), a quarter of the time its bytes take at the memory's rate.
+//   fp32 queries and their probabilities enter as the sum of three bf16 numbers, which hold all of their 24 bits.  bf16's
+//   probabilities are rounded to bf16 under the running maximum: 4e-4 of the result beside the 1.7e-3 of its own rounding (as two
+//   numbers: 16 steps and the score of 896 units 469 -> 457 us without the second).
+// Bound: HBM in launches of some hundred units and more (18432 units of 1056 rows 850 us, 6.05 TB/s); a slice is about 170 vector
+// instructions and 16 matrix instructions (16 cycles each), a fifth of the time its bytes take at the memory's rate.  Below, the chain of
+// trips to memory and instructions: us in a graph, this / the kernel of bf16 or fp32 caches, 4 units of 577 rows 6.4 / 5.6, 128 of 577 7.5 / 8.6, 128
+// of 1100 10.2 / 13.8, 512 of 577 16.0 / 25.1; fp32, D = 64 2 of 72 4.7 / 4.2.  One slice in flight, K of the next asked for as soon as the
+// products with this one are under way (behind them: 861 / 854 us for 18432 units; two slices: 891, 4 of 577 7.0); 4 wavefronts (6: 935, 8: 915);
+// slices of 64 keys at D = 64: 2 of 72 6.25, 128 of 528 8.05 -> 6.3, 25088 of 600 56.6 -> 49.5.
 // The newest token's row is quantised by every wavefront for itself while its first slice is on the way (a step's call is
 // one launch), and replaces what the cache holds in its place in the unit's last slice; the workgroup of the first piece stores it.
 #include "e4m3.h"
@@ -66,7 +71,7 @@ __device__ __forceinline__ void parts_of(const f32x8& x, u32x4 (&p)[P]) {
 template <typename T, int D>
 struct Geo {
   static constexpr bool F32 = sizeof(T) == 4;
-  static constexpr int KEYS = 4096 / D, KT = KEYS / 16;      // of a slice: 4 KiB of K and as much of V
+  static constexpr int KEYS = 32, KT = 2;                    // of a slice, tiles of 16
   static constexpr int NL = D / 64;                          // K loads per tile
   static constexpr int NC = D / 16;                          // channels per lane, accumulators
   static constexpr int VW = D / 64;                          // words of V per lane and key
@@ -89,7 +94,7 @@ template <typename T, int D>
 struct Rows {
   const uint8_t *K, *V;
   const uint32_t* scales;
-  int n_tiled, last_tile;
+  int n_tiled;
   uint32_t k_tiled, k_rows, v, s;
 };
 
@@ -98,8 +103,7 @@ __device__ __forceinline__ void request_k(Slice<T, D>& x, const Rows<T, D>& at, 
   using G = Geo<T, D>;
 #pragma unroll
   for (int tt = 0; tt < G::KT; ++tt) {
-    // (the capacity is whole 32 rows: at D = 64 a unit's last slice may be half beyond it)
-    const int t = G::KT > 2 ? min(it * G::KT + tt, at.last_tile) : it * G::KT + tt;
+    const int t = it * G::KT + tt;                           // (the capacity is whole slices)
     const bool tiled = 16 * t < at.n_tiled;                  // uniform
     const uint8_t* p = at.K + (uint32_t)(t * 16 * D) + (tiled ? at.k_tiled : at.k_rows);
     const uint32_t step = tiled ? 1024 : 64;
@@ -112,7 +116,7 @@ __device__ __forceinline__ void request_v(Slice<T, D>& x, const Rows<T, D>& at, 
   using G = Geo<T, D>;
 #pragma unroll
   for (int tt = 0; tt < G::KT; ++tt) {
-    const int t = G::KT > 2 ? min(it * G::KT + tt, at.last_tile) : it * G::KT + tt;
+    const int t = it * G::KT + tt;
     x.scale[tt] = ld16((const char*)at.scales + (uint32_t)(t * 64) + at.s);
     const uint8_t* p = at.V + (uint32_t)(t * 16 * D) + at.v;
 #pragma unroll
@@ -314,8 +318,7 @@ __device__ __forceinline__ void load4(const char* p, float (&x)[4]) {
 }
 
 // Dynamic LDS: float so[NW][g][OSTR], sm[16][NW], sl[16][NW]; the new row's codes, K then V, per wavefront.
-// DEPTH: slices in flight.
-template <typename T, int D, int NW, int OCC, int DEPTH, bool ONCE>
+template <typename T, int D, int NW, int OCC, bool ONCE>
 __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs a) {
   using G = Geo<T, D>;
   constexpr int ROW_BYTES = G::ROW_BYTES, OSTR = G::OSTR, PSTR = G::PSTR;
@@ -363,12 +366,11 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   const int stride = ns * NW, it0 = sp * NW + wave;
   Rows<T, D> at;
   at.K = a.K + (size_t)unit * cap * D; at.V = a.V + (size_t)unit * cap * D; at.scales = a.scales + (size_t)unit * cap;
-  at.n_tiled = seq.n_tiled; at.last_tile = (cap >> 4) - 1;
+  at.n_tiled = seq.n_tiled;
   at.k_tiled = lane * 16; at.k_rows = r * D + kb * 16; at.v = kb * 4 * D + r * G::NC; at.s = kb * 16;
 
-  Slice<T, D> s[DEPTH];
-  request<T, D, ONCE>(s[0], at, min(it0, max(n_iter - 1, 0)));           // (wavefronts beyond the end ask for its last slice and do not use it)
-  if constexpr (DEPTH > 1) request<T, D, ONCE>(s[1], at, min(it0 + stride, max(n_iter - 1, 0)));
+  Slice<T, D> s;
+  request<T, D, ONCE>(s, at, min(it0, max(n_iter - 1, 0)));  // (wavefronts beyond the end ask for its last slice and do not use it)
 
   // while that is on its way: the queries' parts, and the new row's codes
   u32x4 q[G::NL][2][G::QP];
@@ -413,29 +415,18 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
     process<T, D, decltype(exact)::value>(x, st, q, it, it == n_iter - 1, a.scale_hi, a.scale_lo, r, kb, n_tot, fresh, Nothing{});
   };
   if (it0 < n_iter) {
-    if constexpr (DEPTH == 1) {
-      int it = it0;
-      for (; it + stride < n_iter; it += stride) {
-        process<T, D, false>(s[0], st, q, it, false, a.scale_hi, a.scale_lo, r, kb, n_tot, fresh, [&] { request_k<T, D>(s[0], at, it + stride); });
-        request_v<T, D, ONCE>(s[0], at, it + stride);
-      }
-      work(s[0], it, std::false_type{});
-    } else {
-      for (int it = it0;;) {
-        work(s[0], it, std::false_type{});
-        if (it + stride >= n_iter) break;
-        request<T, D, ONCE>(s[0], at, min(it + 2 * stride, n_iter - 1));
-        work(s[1], it + stride, std::false_type{});
-        if ((it += 2 * stride) >= n_iter) break;
-        request<T, D, ONCE>(s[1], at, min(it + stride, n_iter - 1));
-      }
+    int it = it0;
+    for (; it + stride < n_iter; it += stride) {
+      process<T, D, false>(s, st, q, it, false, a.scale_hi, a.scale_lo, r, kb, n_tot, fresh, [&] { request_k<T, D>(s, at, it + stride); });
+      request_v<T, D, ONCE>(s, at, it + stride);
     }
+    work(s, it, std::false_type{});
     // seldom: a maximum that the short form of the weights is not right for, or a NaN that may be its doing
     if (__any(fabsf(st.m) >= GKV_HUGE_LOG2 || st.l != st.l)) {
       reset();
       for (int it = it0; it < n_iter; it += stride) {
-        request<T, D, ONCE>(s[0], at, it);
-        work(s[0], it, std::true_type{});
+        request<T, D, ONCE>(s, at, it);
+        work(s, it, std::true_type{});
       }
     }
   }
@@ -558,7 +549,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   }
 }
 
-template <typename T, int D, int NW, int OCC, int DEPTH, bool ONCE = false>
+template <typename T, int D, int NW, int OCC, bool ONCE = false>
 hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const Q8AttendArgs& a) {
   KernelArgs k;
   k.d_state = a.d_state; k.step_base = dm.step_base ? dm.step_base : a.d_state;
@@ -571,19 +562,18 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const Q8AttendArgs& a)
   k.Hq = dm.Hq; k.Hkv = dm.Hkv; k.g = dm.g; k.cap = dm.cap; k.LB = dm.L * dm.B; k.w = dm.w; k.step = a.step;
   k.has_base = dm.step_base != nullptr; k.copy_q = a.copy_q; k.write_stats = a.write_stats;
   k.scale_hi = dm.scale_l2_hi; k.scale_lo = dm.scale_l2_lo; k.prefix = a.prefix;
-  return gkv_launch(ln, q8_attend_mfma_kernel<T, D, NW, OCC, DEPTH, ONCE>, dim3(dm.L * dm.B * dm.Hkv * a.splits), dim3(NW * 64),
+  return gkv_launch(ln, q8_attend_mfma_kernel<T, D, NW, OCC, ONCE>, dim3(dm.L * dm.B * dm.Hkv * a.splits), dim3(NW * 64),
                     gkv_q8_attend_mfma_lds(D, dm.g, NW), k);
 }
 
 template <typename T, int D>
 hipError_t launch_waves(const GkvLaunch& ln, const GkvDims& dm, const Q8AttendArgs& a) {
-  const int64_t workgroups = (int64_t)dm.L * dm.B * dm.Hkv * a.splits;
-  constexpr int OCC = sizeof(T) == 4 ? 2 : 3;                // wavefronts per SIMD that the registers of one slice leave room for
-  if (a.waves == 8) return launch<T, D, 8, 2, 1>(ln, dm, a);
-  if (workgroups <= 256) return launch<T, D, 4, 2, 2>(ln, dm, a);
-  // V of caches beyond the 256 MiB memory-side cache is read with non-temporal loads, beside K's ordinary ones
+  if (a.waves == 8) return launch<T, D, 8, 2>(ln, dm, a);
+  // V of caches beyond the 256 MiB memory-side cache is read with non-temporal loads beside K's ordinary ones (18432 units of 1056 rows: both
+  // ordinary 939 us, this 861; 896 of 640, which that cache holds: both ordinary 462 for 16 steps and the score, this 473)
+  constexpr int OCC = sizeof(T) == 4 ? 2 : 3;                // wavefronts per SIMD that the registers leave room for
   const bool once = (int64_t)dm.L * dm.B * dm.Hkv * (dm.b + dm.s / 2) * 2 * D > (int64_t)256 << 20;
-  return once ? launch<T, D, 4, OCC, 1, true>(ln, dm, a) : launch<T, D, 4, OCC, 1>(ln, dm, a);
+  return once ? launch<T, D, 4, OCC, true>(ln, dm, a) : launch<T, D, 4, OCC>(ln, dm, a);
 }
 
 }  // namespace
