@@ -171,7 +171,7 @@ class DecodeState:
             self.ctx.attend_decode(q, k_new, v_new, self.K, self.V, self.pos, step, self.qwin, self.d_state,
                                    self.len_host, self.out, self.workspace)
         else:
-            prefix.attend(q)
+            prefix.attend(q, self)
             self.ctx.attend_decode_prefix(q, k_new, v_new, self.K, self.V, self.pos, step, self.qwin, self.d_state,
                                           self.len_host, prefix.part, self.out, self.workspace)
         return self._stepped_on(k_new)
@@ -233,11 +233,18 @@ class Q8DecodeState(DecodeState):
         self.K = self.V = None
 
     def load_prompt_rows(self, t_first, k, v, t0, prompt_lens):
-        """As DecodeState's, quantised on the way."""
-        dt = self.qwin.dtype
-        lens = torch.tensor(prompt_lens, dtype=torch.int32).to(self.device)
-        self.ctx.q8_store_prompt(k.to(dt).contiguous(), v.to(dt).contiguous(), k.shape[0], t_first, t0, lens, self.K8, self.V8,
-                                 self.scales, self.pos)
+        """As DecodeState's, quantised on the way.  Rows that would lie at or beyond the capacity are left out."""
+        cfg, n, lens = self.cfg, k.shape[0], [int(P) for P in prompt_lens]
+        row = (cfg.n_layers, cfg.batch, cfg.n_kv_heads, cfg.head_dim)
+        if k.shape[1:] != row or v.shape != k.shape:
+            raise ValueError(f"gkv: k and v have to be [n, {', '.join(map(str, row))}]")
+        if len(lens) > cfg.batch:
+            raise ValueError("gkv: more prompts than sequences")
+        if n == 0:
+            return
+        k, v = (x.to(self.device, self.qwin.dtype).contiguous() for x in (k, v))
+        lens = torch.tensor(lens + [0] * (cfg.batch - len(lens)), dtype=torch.int32).to(self.device)
+        self.ctx.q8_store_prompt(k, v, n, t_first, t0, lens, self.K8, self.V8, self.scales, self.pos)
 
     def load_prefix(self, k, v, t0=0):
         """As DecodeState's, quantised on the way."""
@@ -252,12 +259,15 @@ class Q8DecodeState(DecodeState):
         K and V, or into new buffers (rows that are not held are zero then)."""
         if K is None and V is None:
             K, V = (torch.zeros(self.K8.shape, dtype=self.qwin.dtype, device=self.device) for _ in range(2))
+        for x in (K, V):
+            if x is not None and (x.shape != self.K8.shape or x.dtype != self.qwin.dtype or x.device != self.K8.device):
+                raise ValueError(f"gkv: K and V have to be {tuple(self.K8.shape)} of {self.qwin.dtype} on {self.K8.device}")
         self.ctx.q8_read(self.K8, self.V8, self.scales, self.d_state, step, K, V)
         return K, V
 
     def attend_decode(self, q, k_new, v_new, step, prefix=None):
         if prefix is not None:
-            prefix.attend(q)
+            prefix.attend(q, self)
         self.ctx.q8_attend_decode(q, k_new, v_new, self.K8, self.V8, self.scales, self.pos, step, self.qwin, self.d_state,
                                   self.len_host, None if prefix is None else prefix.part, self.out, self.workspace)
         return self._stepped_on(k_new)
@@ -289,7 +299,11 @@ class SharedPrefix:
     def __init__(self, state: DecodeState, k, v, first=0, count=None, part=None):
         """part: another SharedPrefix of the same state whose sequences are others: one step then joins both, through
         attend() of this one and attend_decode(..., prefix=the other)."""
-        dt = state.qwin.dtype
+        dt, cfg = state.qwin.dtype, state.cfg
+        if k.dim() != 4 or (k.shape[0], k.shape[1], k.shape[3]) != (cfg.n_layers, cfg.n_kv_heads, cfg.head_dim) or v.shape != k.shape:
+            raise ValueError(f"gkv: a prefix's k and v have to be [{cfg.n_layers}, {cfg.n_kv_heads}, rows, {cfg.head_dim}]")
+        if part is not None and part.ctx is not state.ctx:
+            raise ValueError("gkv: the other prefix is of another state")
         self.ctx = state.ctx
         self.K, self.V = k.to(state.device, dt).contiguous(), v.to(state.device, dt).contiguous()
         self.rows, self.first = k.shape[2], first
@@ -299,6 +313,8 @@ class SharedPrefix:
         if self.part.numel() < need:
             raise ValueError("gkv: make the longer prefix first, its buffer holds the shorter one's pieces too")
 
-    def attend(self, q):
+    def attend(self, q, state=None):
         """The newest queries over the prefix; attend_decode() with a prefix does it by itself."""
+        if state is not None and state.ctx is not self.ctx:
+            raise ValueError("gkv: the prefix is of another state")
         self.ctx.prefix_attend(q, self.K, self.V, self.rows, self.rows, self.first, self.count, self.part)

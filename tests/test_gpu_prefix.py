@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+import paper_2512_00504_amd as P
 from paper_2512_00504_amd import make_config
 from paper_2512_00504_amd.state import DecodeState, Q8DecodeState, SharedPrefix, k_rows_to_cache
 
@@ -250,3 +251,22 @@ def test_recorded_steps_replay_as_eager_ones(cls, dtype, d, g, B, rows):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(st.out.view(torch.uint8), want[i].view(torch.uint8)), i
+
+
+@pytest.mark.parametrize("cls", [DecodeState, Q8DecodeState])
+def test_prefix_of_another_shape_or_state_is_refused(cls):
+    st, other = (cls(make_config(1, 2, 4, 2, 64, 16, 4, 8, 64, "bf16")) for _ in range(2))
+    k = torch.zeros(1, 2, 40, 64)
+    for bad in ((k[0], k[0]), (k[:, :1], k[:, :1]), (k[..., :32], k[..., :32]), (k, k[:, :, :39]), (torch.cat([k, k]), torch.cat([k, k]))):
+        with pytest.raises(ValueError):
+            SharedPrefix(st, *bad)
+    short, long = SharedPrefix(st, k[:, :, :1], k[:, :, :1], count=1), torch.zeros(1, 2, 9000, 64)
+    with pytest.raises(ValueError):
+        SharedPrefix(st, long, long, first=1, part=short)
+    with pytest.raises(ValueError):
+        SharedPrefix(other, k, k, part=short)
+    q, kn, vn = (torch.zeros(1, 2, n, 64, dtype=torch.bfloat16, device="cuda") for n in (4, 2, 2))
+    with pytest.raises(ValueError):
+        other.attend_decode(q, kn, vn, 0, prefix=short)
+    with pytest.raises(P.GkvError):
+        SharedPrefix(st, k, k, first=1, count=2).attend(q)

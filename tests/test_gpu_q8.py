@@ -71,6 +71,27 @@ def test_store_prompts_of_all_lengths_in_chunks(dtype, d, hkv):
             assert (cache.view(torch.uint8)[:, i, :, m:] == mark).all() and (scales[:, i, :, m:] == 7).all() and (pos[:, i, :, m:] == -1).all()
 
 
+def test_prompts_as_the_other_state_takes_them():
+    # from host memory, of another type, not contiguous, of no rows, fewer prompts than sequences
+    st, ref = _state(B=3), _state(B=3)
+    gen = torch.Generator().manual_seed(1)
+    k, v = _rows(gen, "f32", 9, 1, 3, 2, 64), _rows(gen, "f32", 1, 9, 3, 2, 64).transpose(0, 1)
+    st.load_prompt_rows(2, k, v, 11, [4, 9])
+    st.load_prompt_rows(11, k[:0], v[:0], 11, [4, 9])
+    ref.load_prompt_rows(2, k.bfloat16().cuda(), v.bfloat16().contiguous().cuda(), 11, [4, 9, 0])
+    for name in ("K8", "V8", "scales", "pos"):
+        assert torch.equal(getattr(st, name).view(torch.uint8), getattr(ref, name).view(torch.uint8)), name
+    st.load_prefix(k[:0], v[:0], t0=5)
+    assert (st.pos == -1).all() and st.d_state[0, :, :2].tolist() == [[0, 5]] * 3
+    for bad in ((k[:, :, :2], v[:, :, :2], [4]), (k, v[:5], [4]), (k, v, [4, 9, 1, 1])):
+        with pytest.raises(ValueError):
+            st.load_prompt_rows(2, *bad[:2], 11, bad[2])
+    whole = torch.zeros(st.K8.shape, dtype=torch.bfloat16, device="cuda")
+    for bad in (whole.float(), whole[:, :2], whole.cpu()):
+        with pytest.raises(ValueError):
+            st.read(11, K=bad)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_store_hard_values(dtype):
     # zeros, subnormals, the largest numbers, largest magnitudes at and next to 448 * 2^e, every tie between codes, infinities and NaN
@@ -430,7 +451,7 @@ def test_decode_and_evict_cycles(dtype, d, g, params):
             src = sorted(order) + list(range(n - w, n))
             r[0], r[1], r[2] = r[0][src], r[1][src], [r[2][x] for x in src]
             r[3] = [got[x].item() for x in src[:b - w]]
-    assert events == 2 * 2 * (5 + 4 + 3) or events > 20
+    assert events == 2 * 2 * (5 + 4 + 3)                 # compressions of the sequences that begin with 60, 20 and 1 rows
     K, V = st.read(t0 + 5 * s)
     for (l, i, j), r in rows.items():
         n = len(r[0])
