@@ -325,7 +325,7 @@ gkv_status gkv_evict_static(gkv_ctx* ctx, const void* qwin, void* K, void* V, fl
  *
  * gkv_q8_store_prompt: prompt rows into the cache.  k, v [n,L,B,h_kv,d] hold the positions t_first .. t_first + n - 1 of
  * every sequence's token stream; sequence i's prompt is the positions [t0 - P_i, t0) with P_i = d_prompt_len[i] (device,
- * int32 [B]) and goes to rows [0, P_i), row-major, with pos their positions.  May be called chunk by chunk.  Rows that
+ * int32 [B]) and goes to rows [0, P_i), row-major, with pos their positions.  May be called chunk by chunk, of up to 2^30 positions.  Rows that
  * would lie at or beyond the capacity are left out; all other rows stay as they are.  The records are the caller's to set, to
  * {P_i, t0, 0, 0}.
  */
@@ -370,7 +370,7 @@ gkv_status gkv_q8_evict(gkv_ctx* ctx, const void* qwin, void* K8, void* V8, void
  * those of other sequences stay as they are, so a batch of several prompts takes one call for each of them (on one stream, or ordered by events), and a sequence
  * that has none a part that still is zero.  Results stay until they are written again: call it in every step.
  * rows may be 0 (Kp and Vp are not looked at then).  A call with more rows than the context's gkv_prefix_bytes calls were asked for
- * returns GKV_ERR_WORKSPACE.  Both calls can be recorded; the rows are frozen then.  head_dim has to be a multiple of 4.
+ * returns GKV_ERR_WORKSPACE.  Both calls can be recorded; the rows are frozen then.  More than 2^30 rows: GKV_ERR_SHAPE.
  * The result is the same to the last bit for the same rows, first, count and alignment of the arguments.
  */
 gkv_status gkv_prefix_bytes(gkv_ctx* ctx, int32_t rows, size_t* out_bytes);

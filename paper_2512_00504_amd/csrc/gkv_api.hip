@@ -469,6 +469,7 @@ static PrefixPart prefix_part(const gkv_ctx* ctx, const void* part) {
   return PrefixPart{(const float*)(ms + gkv_align256(GKV_PREFIX_PIECES * heads * sizeof(float2))), (const float2*)ms,
                     (const int32_t*)part, (int64_t)heads};
 }
+constexpr int32_t GKV_MOST_ROWS = 1 << 30;                        // of a prompt chunk or a prefix: what the kernels' indices leave room for
 static bool aligned16(std::initializer_list<const void*> ptrs) {
   uintptr_t bits = 0;
   for (const void* p : ptrs) bits |= (uintptr_t)p;
@@ -677,6 +678,7 @@ extern "C" gkv_status gkv_q8_store_prompt(gkv_ctx* ctx, const void* k, const voi
                                           void* stream) {
   if (!ctx || !k || !v || !d_prompt_len || !K8 || !V8 || !scales || !pos || n < 1 || t_first < 0 || t0 < 0)
     return GKV_ERR_INVALID_ARG;
+  if (n > GKV_MOST_ROWS) return GKV_ERR_SHAPE;
   const gkv_status st = check_q8(ctx, {k, v, K8, V8, scales});
   if (st != GKV_OK) return st;
   Q8StoreArgs a{k, v, n, t_first, t0, d_prompt_len, (uint8_t*)K8, (uint8_t*)V8, (uint32_t*)scales, pos, 0};
@@ -817,7 +819,7 @@ extern "C" gkv_status gkv_prefix_attend(gkv_ctx* ctx, const void* q, const void*
   if (!ctx || !q || !part || rows < 0 || rows > capacity || (rows > 0 && (!Kp || !Vp))) return GKV_ERR_INVALID_ARG;
   if (first < 0 || count < 1 || first > ctx->dims.B - count) return GKV_ERR_INVALID_ARG;
   if (!aligned16({part})) return GKV_ERR_INVALID_ARG;
-  if (ctx->dims.d % 4 != 0) return GKV_ERR_SHAPE;
+  if (rows > GKV_MOST_ROWS) return GKV_ERR_SHAPE;
   if (rows > ctx->prefix_rows) return GKV_ERR_WORKSPACE;          // the buffer was not sized for them
   const GkvDims& d = ctx->dims;
   const PrefixPart to = prefix_part(ctx, part);

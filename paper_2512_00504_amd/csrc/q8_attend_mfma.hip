@@ -46,22 +46,12 @@ __device__ __forceinline__ uint32_t upper(uint32_t w) {
 }
 __device__ __forceinline__ u32x4 eight(uint32_t a, uint32_t b) { return u32x4{lower(a), upper(a), lower(b), upper(b)}; }
 
-// x = sum of P bf16 numbers: two hold 16 bits, three all 24.
+// x as bf16 (P = 1), or as the sum of P bf16 numbers: three hold all of its bits.
 template <int P>
 __device__ __forceinline__ void parts_of(const f32x8& x, u32x4 (&p)[P]) {
   f32x8 rest = x;
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    if (P == 2 && i == 0) {                                   // the upper half as it is
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        const uint32_t a = __float_as_uint(x[2 * y]), b = __float_as_uint(x[2 * y + 1]);
-        p[0][y] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-        rest[2 * y] = x[2 * y] - __uint_as_float(a & 0xffff0000u);
-        rest[2 * y + 1] = x[2 * y + 1] - __uint_as_float(b & 0xffff0000u);
-      }
-      continue;
-    }
     const bf16x8 h = __builtin_convertvector(rest, bf16x8);
     p[i] = __builtin_bit_cast(u32x4, h);
     if (i < P - 1) rest -= __builtin_convertvector(h, f32x8);

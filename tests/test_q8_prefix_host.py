@@ -79,6 +79,18 @@ def test_a_prefix_longer_than_the_buffer_was_sized_for_is_refused():
     ctx.close()
 
 
+def test_more_rows_than_indices_have_room_for_are_refused():
+    ctx = _ctx()
+    ctx.prefix_bytes(2 ** 31 - 1)
+    args = list(GOOD["gkv_prefix_attend"])
+    args[3] = args[4] = 2 ** 30 + 1
+    assert LIB.gkv_prefix_attend(ctx.h, *args, None) == SHAPE
+    args = list(GOOD["gkv_q8_store_prompt"])
+    args[2] = 2 ** 30 + 1
+    assert LIB.gkv_q8_store_prompt(ctx.h, *args, None) == SHAPE
+    ctx.close()
+
+
 @pytest.mark.parametrize("batch", [1, 3, 64])
 def test_prefix_buffer_never_shrinks_with_more_rows(batch):
     ctx = _ctx(batch=batch)
