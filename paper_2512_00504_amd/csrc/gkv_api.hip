@@ -784,8 +784,7 @@ static PrefixPlan prefix_plan(const gkv_ctx* ctx, bool mfma, int rows, int count
     const int64_t blocks = ((int64_t)count * d.g + 31) / 32;
     p.tiles = (int)((blocks + 3) / 4);
     p.blocks = (int)((blocks + p.tiles - 1) / p.tiles);
-    const bool wide = d.d * ctx->esz >= 512;                    // rows of which LDS holds two groups' tiles
-    p.key_groups = p.blocks == 1 ? (wide ? 2 : 4) : p.blocks == 2 ? 2 : 1;
+    p.key_groups = p.blocks == 1 ? 4 : p.blocks == 2 ? 2 : 1;
     want = (p.key_groups > 1 ? 512 : 768) / ((int64_t)d.L * d.Hkv * p.tiles);
     if (p.key_groups > 1 && want > 32) want = 32;
     least = p.key_groups > 1 ? 256 : 128;

@@ -10,7 +10,7 @@
 //   bf16 rounds P to bf16 (to the nearest; 2^-9 of the value, and the sum is of the unrounded weights).
 // LDS holds a tile's rows as they are, their 16-byte pieces exchanged within the row so that neither kind of read finds two
 // rows in the same banks.
-// Bound: HBM with few rows.  With several hundred the products and the vector unit in turn: 32 keys of 32 rows are 16 products (512
+// Bound: HBM with few rows (28 layers, 4 KV heads, 32000 rows of d = 128, g = 7: 289 us, 6.3 TB/s).  With several hundred the products and the vector unit in turn: 32 keys of 32 rows are 16 products (512
 // cycles) and 16 x (maximum, fma, exponential, sum, half a conversion), about as many; what a wavefront does of one does not overlap
 // with the other, and three of them on a SIMD overlap little (counters, 64 sequences x 16384 rows: products 48% of the time, vector
 // instructions 51%).  Two tiles' logits in turn within a wavefront, which takes the registers of the third: 117 -> 138 us.
@@ -58,8 +58,12 @@ struct Geo {
 
 // A 1 KiB piece from memory to LDS, 16 bytes a lane; `lds` is uniform.  (Written out, because the compiler makes every later read of LDS
 // wait for every such request; the wait is the one before the barrier below.  Nothing else in this file uses m0.)
+// ONCE: non-temporal.
+template <bool ONCE>
 __device__ __forceinline__ void to_lds(const char* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(base) : "memory");
+  const uint32_t at = __builtin_amdgcn_readfirstlane(lds);
+  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" :: "s"(at), "v"(offset), "s"(base) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(at), "v"(offset), "s"(base) : "memory");
 }
 
 // What lies at an address of LDS.
@@ -73,11 +77,17 @@ struct KernelArgs {
   float scale_hi, scale_lo;
 };
 
+// Tiles in turn.  Groups of one wavefront wait for nobody: where LDS has no room for two tiles each (fp32, D = 128: with two groups and a barrier
+// 260 us, 14 layers, 2 KV heads, 24000 rows; this 166), or the products are as long as the wait (D = 64: 159 / 146), one has them overlap with the others' loads.
+template <typename T, int D, int NK> struct Buffers { static constexpr int N = NK == 4 && Geo<T, D>::F32 ? 1 : 2; };
+
 // NK: groups of a.blocks wavefronts that share the rows and take the tiles in turn (joined through LDS at the end): with one or two
 // blocks of rows they make a workgroup of four wavefronts, and the prefix is cut into fewer pieces for the decode kernel to join.
-template <typename T, int D, int NK>
+template <typename T, int D, int NK, bool ONCE>
 __global__ __launch_bounds__(256, sizeof(T) * D >= 512 && NK > 1 ? 1 : NK > 1 || sizeof(T) == 4 ? 2 : 3) void prefix_mfma_kernel(KernelArgs a) {
   using G = Geo<T, D>;
+  constexpr bool ALONE = NK == 4;                            // a group is one wavefront: no barrier (28 layers, 4 sequences x 8000 78.5 -> 73.7 us)
+  constexpr int BUFS = Buffers<T, D, NK>::N;
   constexpr int SUB = G::TK / 32, CB = D / 32;
   constexpr uint32_t BUF = NK * 2 * G::TILE;
   extern __shared__ __attribute__((aligned(1024))) char smem[];     // [2][NK][K, V][TILE]
@@ -112,12 +122,12 @@ __global__ __launch_bounds__(256, sizeof(T) * D >= 512 && NK > 1 ? 1 : NK > 1 ||
     if (NK > 1 && last < 0) return;
     const char* kt = Kp + (size_t)first * G::ROW;
     const char* vt = Vp + (size_t)first * G::ROW;
-    const uint32_t to = lds0 + (r & 1) * BUF;
+    const uint32_t to = lds0 + (BUFS == 2 ? r & 1 : 0) * BUF;
     for (int x = mi; x < G::PIECES; x += a.blocks) {
       const int at = x * G::ROWS_PIECE + lane / G::CHUNKS, chunk = lane % G::CHUNKS;
       const int src = min(at, last);                         // rows behind the end repeat its last one
-      to_lds(kt, src * G::ROW + (chunk ^ G::k_swap(at)) * 16, to + x * 1024);
-      to_lds(vt, src * G::ROW + (chunk ^ G::v_swap(at)) * 16, to + G::TILE + x * 1024);
+      to_lds<false>(kt, src * G::ROW + (chunk ^ G::k_swap(at)) * 16, to + x * 1024);
+      to_lds<ONCE>(vt, src * G::ROW + (chunk ^ G::v_swap(at)) * 16, to + G::TILE + x * 1024);
     }
   };
 
@@ -246,23 +256,33 @@ __global__ __launch_bounds__(256, sizeof(T) * D >= 512 && NK > 1 ? 1 : NK > 1 ||
   };
   // The next round's buffer is the one that everybody is through with at the barrier.
   auto there_now = [] {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // this wavefront's share of the tile
-    __syncthreads();                                         // and everybody's
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // this wavefront's share of the tile (and it has read the last one)
+    if constexpr (!ALONE) __syncthreads();                   // and everybody's
   };
   if (n_rounds > 0) {
     bring(0);
     uint32_t buf = 0;
-    for (int r = 0;; r += 2) {
-      there_now();
-      if (r == n_rounds - 1) break;
-      bring(r + 1);
-      work(0, G::TK, std::false_type{});
-      there_now();
-      buf = BUF;
-      if (r + 1 == n_rounds - 1) break;
-      buf = 0;
-      bring(r + 2);
-      work(BUF, G::TK, std::false_type{});
+    if constexpr (BUFS == 1) {
+      for (int r = 0;; ++r) {
+        there_now();
+        if (r == n_rounds - 1) break;
+        work(0, G::TK, std::false_type{});
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        bring(r + 1);
+      }
+    } else {
+      for (int r = 0;; r += 2) {
+        there_now();
+        if (r == n_rounds - 1) break;
+        bring(r + 1);
+        work(0, G::TK, std::false_type{});
+        there_now();
+        buf = BUF;
+        if (r + 1 == n_rounds - 1) break;
+        buf = 0;
+        bring(r + 2);
+        work(BUF, G::TK, std::false_type{});
+      }
     }
     const int t = (n_rounds - 1) * NK + ki;
     if (NK == 1 || t == n_tiles - 1) work(buf, n1 - n0 - t * G::TK, std::true_type{});
@@ -311,18 +331,18 @@ __global__ __launch_bounds__(256, sizeof(T) * D >= 512 && NK > 1 ? 1 : NK > 1 ||
   }
 }
 
-template <typename T, int D, int NK>
+template <typename T, int D, int NK, bool ONCE = false>
 hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const PrefixArgs& p, const PrefixPlan& plan) {
   KernelArgs a{p, dm.L, dm.B, dm.Hq, dm.Hkv, dm.g, plan.tiles, plan.blocks, dm.L * dm.Hkv * p.splits,
                gkv_divisor(plan.tiles), gkv_divisor(p.splits), dm.by_hkv, gkv_divisor(dm.g), gkv_divisor(plan.blocks),
                dm.scale_l2_hi, dm.scale_l2_lo};
   const int64_t grid = (int64_t)(a.groups + 7) / 8 * 8 * plan.tiles;
   if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-  constexpr size_t shmem = NK * 4 * Geo<T, D>::TILE;
+  constexpr size_t shmem = NK * 2 * Buffers<T, D, NK>::N * Geo<T, D>::TILE;
   // the results of all groups but the first: (NK - 1) * blocks wavefronts, four in all at most
   static_assert(shmem <= 131072 && (NK == 1 || shmem >= (NK == 4 ? 3 : 2) * 64 * (D / 2 + 2) * sizeof(float)), "tiles, or the groups' results");
   if (plan.blocks * NK > 4) return hipErrorInvalidConfiguration;
-  auto kern = prefix_mfma_kernel<T, D, NK>;
+  auto kern = prefix_mfma_kernel<T, D, NK, ONCE>;
   if (shmem > GKV_LDS_LIMIT) {                               // beyond the default per-workgroup limit: opt in (a CU holds 160 KiB)
     const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);
     if (e != hipSuccess) return e;
@@ -332,10 +352,12 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const PrefixArgs& p, c
 
 template <typename T, int D>
 hipError_t launch_groups(const GkvLaunch& ln, const GkvDims& dm, const PrefixArgs& p, const PrefixPlan& plan) {
-  if constexpr (sizeof(T) * D < 512) {
-    if (plan.key_groups == 4) return launch<T, D, 4>(ln, dm, p, plan);
-  }
-  return plan.key_groups == 2 ? launch<T, D, 2>(ln, dm, p, plan) : launch<T, D, 1>(ln, dm, p, plan);
+  // V of prefixes that are read once and beyond the 256 MiB memory-side cache is read with non-temporal loads beside K's ordinary ones (bf16, d =
+  // 128, 28 layers, 4 KV heads, 8000 rows: 4 sequences 94 us, this 78, K too 86; 16 sequences 107 / 98; 1 layer of 32000 18.8 / 21.0)
+  const bool once = plan.tiles == 1 && (int64_t)dm.L * dm.Hkv * p.rows * 2 * Geo<T, D>::ROW > (int64_t)256 << 20;
+  if (plan.key_groups == 4) return once ? launch<T, D, 4, true>(ln, dm, p, plan) : launch<T, D, 4>(ln, dm, p, plan);
+  if (plan.key_groups == 2) return once ? launch<T, D, 2, true>(ln, dm, p, plan) : launch<T, D, 2>(ln, dm, p, plan);
+  return once ? launch<T, D, 1, true>(ln, dm, p, plan) : launch<T, D, 1>(ln, dm, p, plan);
 }
 
 }  // namespace
