@@ -642,8 +642,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
     if (kb == 0) { sm[r * NW + wave] = st.m_run; sl[r * NW + wave] = l_tot; }
   }
   constexpr int TPH = D / 4;                // threads per head
-  constexpr int PRE = 4;                    // pieces of the prefix at once (with 8 or 16 it takes no less)
-  PrefixPieces<PRE> pre;
+  PrefixPieces<GKV_PREFIX_AT_ONCE> pre;
   __syncthreads();
 
   // one thread per (head, 4 channels): a single round for g <= 8 with 256 threads
@@ -654,12 +653,8 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
   // the unit's result, from its own sum of weighted values
   auto finish = [&](int x, int h, int c4, float M, float L, f32x4 o, bool fast) {
     if constexpr (PREFIX) {
-      bool any_key = n_tot > 0;
-      for (int s0 = 0; s0 < n_pre; s0 += PRE) {
-        if (s0 > 0 || ns == 1 || x != tid) pre.request(a.prefix, head0 + h, D, c4, s0, n_pre);
-        pre.join(s0, n_pre, M, L, o, any_key);
-      }
-      store_row4(out + (uint32_t)(x * 4), o * inverse_total(L, any_key));
+      const float inv = prefix_join(a.prefix, head0, h, D, c4, n_pre, ns > 1 && x == tid, pre, M, L, o, n_tot > 0);
+      store_row4(out + (uint32_t)(x * 4), o * inv);
     } else {
       store_row4(out + (uint32_t)(x * 4), o * inv_sum(L, n_tot > 0, fast));
     }
@@ -714,7 +709,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void attend_mfma_kernel(KernelArgs a)
   }
 
   if constexpr (PREFIX) {                   // the prefix's first pieces, on their way while the ticket is
-    if (merges && tid < g * TPH) pre.request(a.prefix, head0 + tid / TPH, D, (tid % TPH) * 4, 0, n_pre);
+    if (merges && n_pre > 0 && tid < g * TPH) pre.request(a.prefix, head0, tid / TPH, D, (tid % TPH) * 4, 0, n_pre);
   }
 
   // ---- append the new row (row-major, one contiguous row each for K and V), push q into the

@@ -305,43 +305,61 @@ __device__ __forceinline__ float prefix_max(float m, float sum, bool any_key) {
 __device__ __forceinline__ float inverse_total(float total, bool any_key) {
   return total == 0.f ? (any_key ? __builtin_nanf("") : 0.f) : 1.f / total;
 }
-// Joins a prefix's pieces of one head with the sequence's own sum o of weighted values (channels c .. c + 3; maximum m, sum l).
+// Pieces of a prefix on their way: of head head0 + h (head0 uniform), channels c .. c + 3, AT_ONCE of them from piece s0 on.
 typedef float gkv_f32x4 __attribute__((ext_vector_type(4)));
-// AT_ONCE pieces are on their way together.
 template <int AT_ONCE>
 struct PrefixPieces {
   float2 ms[AT_ONCE];
   gkv_f32x4 o[AT_ONCE];
-  __device__ __forceinline__ void request(const PrefixPart& p, size_t head, int d, int c, int s0, int n) {
+  __device__ __forceinline__ void request(const PrefixPart& p, size_t head0, int h, int d, int c, int s0, int n) {
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i)
-      if (s0 + i < n) {
-        const size_t at = (size_t)(s0 + i) * p.heads + head;
-        ms[i] = p.ms[at];
-        o[i] = *(const gkv_f32x4*)(p.o + at * d + c);
-      }
+    for (int i = 0; i < AT_ONCE; ++i) {                      // (without a branch: beyond the last piece that one again)
+      const size_t at = (size_t)min(s0 + i, n - 1) * p.heads + head0;
+      ms[i] = *(const float2*)((const char*)(p.ms + at) + (uint32_t)(h * 8));
+      o[i] = *(const gkv_f32x4*)((const char*)(p.o + at * d) + (uint32_t)((h * d + c) * 4));
+    }
   }
-  __device__ __forceinline__ void join(int s0, int n, float& m, float& l, gkv_f32x4& sum, bool& any_key) {
+  // with a sum o of weighted values, its maximum m (GKV_NO_MAX or more) and sum l.  A piece without weight has an o of 0 and a maximum
+  // that is at most GKV_NO_MAX: its factor multiplies zeros.
+  __device__ __forceinline__ void join(int s0, int n, float& m, float& l, gkv_f32x4& sum) const {
     float mn = m;
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i)
-      if (s0 + i < n) {
-        any_key |= ms[i].x == -INFINITY;
-        if (ms[i].y != 0.f) mn = fmaxf(mn, ms[i].x);
-      }
+    for (int i = 0; i < AT_ONCE; ++i) mn = fmaxf(mn, ms[i].x);
     const float f0 = __builtin_amdgcn_exp2f(m - mn);
     m = mn;
     l *= f0;
     sum *= f0;
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i)
-      if (s0 + i < n) {
-        const float f = ms[i].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[i].x - mn);
+      if (s0 + i < n) {                                      // uniform
+        const float f = __builtin_amdgcn_exp2f(ms[i].x - mn);
         l += ms[i].y * f;
         sum += o[i] * f;
       }
   }
 };
+constexpr int GKV_PREFIX_AT_ONCE = 4;
+// All n pieces joined with m, l, sum, `first` the first of them if `ready`, the next on their way while some are added up.
+// Returns 1 / total.  any_key: the sequence has rows of its own.
+__device__ __forceinline__ float prefix_join(const PrefixPart& p, size_t head0, int h, int d, int c, int n, bool ready,
+                                             PrefixPieces<GKV_PREFIX_AT_ONCE>& first, float m, float l, gkv_f32x4& sum, bool any_key) {
+  constexpr int N = GKV_PREFIX_AT_ONCE;
+  if (n > 0) {
+    PrefixPieces<N> second;
+    if (!ready) first.request(p, head0, h, d, c, 0, n);
+    for (int s = 0;; s += 2 * N) {
+      if (s + N < n) second.request(p, head0, h, d, c, s + N, n);
+      first.join(s, n, m, l, sum);
+      if (s + N >= n) break;
+      if (s + 2 * N < n) first.request(p, head0, h, d, c, s + 2 * N, n);
+      second.join(s + N, n, m, l, sum);
+      if (s + 2 * N >= n) break;
+    }
+    if (l == 0.f && !any_key)                                // seldom
+      for (int s = 0; s < n; ++s) any_key |= p.ms[(size_t)s * p.heads + head0 + h].x == -INFINITY;
+  }
+  return inverse_total(l, any_key);
+}
 // The same for the plain kernels, one channel a lane: maximum and inverse of the joint total, and the pieces' share of a channel.
 struct PrefixTotal { float max, inverse; };
 __device__ __forceinline__ PrefixTotal prefix_total(const PrefixPart& p, size_t head, float m, float l, bool any_key) {

@@ -441,17 +441,12 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   float* part = a.partials + (size_t)(unit * splits) * g * PSTR;
   const int slot = step - quotient(step, a.by_w) * a.w;
   float2* stats = a.stats + (size_t)slot * a.LB * a.Hq + head0;
-  constexpr int PRE = 4;                    // pieces of the prefix at once (with 8 or 16 it takes no less)
-  PrefixPieces<PRE> pre;
+  PrefixPieces<GKV_PREFIX_AT_ONCE> pre;
   // the unit's result; ready: the first pieces of the prefix are in `pre`
   auto finish = [&](int x, int h, int c4, float M, float L, f32x4 o, bool ready) {
     if (c4 == 0 && a.write_stats) stats[h] = make_float2(M, L);
-    bool any_key = n_tot > 0;
-    for (int s0 = 0; s0 < n_pre; s0 += PRE) {
-      if (s0 > 0 || !ready) pre.request(a.prefix, head0 + h, D, c4, s0, n_pre);
-      pre.join(s0, n_pre, M, L, o, any_key);
-    }
-    store_row4(out + (uint32_t)(x * 4), o * inverse_total(L, any_key));
+    const float inv = prefix_join(a.prefix, head0, h, D, c4, n_pre, ready, pre, M, L, o, n_tot > 0);
+    store_row4(out + (uint32_t)(x * 4), o * inv);
   };
   __syncthreads();
   for (int x = tid; x < g * TPH; x += NW * 64) {
@@ -487,7 +482,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void q8_attend_mfma_kernel(KernelArgs
   }
 
   // (the prefix's first pieces, on their way while the ticket is)
-  if (joins && n_pre > 0 && tid < g * TPH) pre.request(a.prefix, head0 + tid / TPH, D, (tid % TPH) * 4, 0, n_pre);
+  if (joins && n_pre > 0 && tid < g * TPH) pre.request(a.prefix, head0, tid / TPH, D, (tid % TPH) * 4, 0, n_pre);
 
   // ---- the new row, its scales and position, and q into the ring -----------------------------------
   if (sp == 0) {
