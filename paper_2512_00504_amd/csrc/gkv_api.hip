@@ -771,9 +771,8 @@ extern "C" gkv_status gkv_q8_evict(gkv_ctx* ctx, const void* qwin, void* K8, voi
 // those of fewer.
 //   Matrix cores: rows of queries in blocks of 32, a wavefront each and at most 4 to a workgroup.  One or two blocks: the workgroup's
 //   wavefronts are groups that take the keys in turn, two workgroups a CU and up to 32 pieces of 256 keys at least.  A piece costs
-//   the decode kernel 0.2 us, so (us, the prefix's kernel + the decode kernel, 16 / 32 / 64 pieces, bf16, d = 128, g = 7) 8 sequences x 8000 rows,
-//   one layer 12.9 + 9.8 / 10.4 + 12.9 / 9.8 + 12.3, 4 x 32000 25.4 + 9.6 / 17.6 + 12.4 / 15.7 + 18.2; in one group instead of two or
-//   four 8 x 8000 27.8 in all where this takes 22; 28 layers, 8 x 4000 one workgroup a CU 84.5 in all, two 77.8.
+//   the decode kernel 0.1 us, so (us in a graph, both kernels, 16 / 32 / 64 pieces, bf16, d = 128, g = 7) 4 sequences x 32000 rows, one layer
+//   31.2 / 25.7 / 28.0, 8 x 8000 20.2 / 20.0 / 20.0; 28 layers, 8 x 4000 one workgroup a CU 76.4, two 69.6, but 4 x 8000 85.9 / 88.3.
 //   More blocks: three workgroups a CU (two: 136 us where three take 117, 64 sequences x 16384 rows, g = 5, 4 layers), 128 keys at least.
 //   Plain kernel: about two thousand workgroups, one a (sequence, KV head, piece), of 256 keys at least.
 static PrefixPlan prefix_plan(const gkv_ctx* ctx, bool mfma, int rows, int count) {
