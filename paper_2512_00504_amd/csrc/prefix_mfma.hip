@@ -7,13 +7,15 @@
 //   8 i + 4 h + e of its row, so the softmax stays in the lane but for one exchange with the other half, and they are what the
 //   product  O^T[channel, row] += V^T P^T  wants of P in that lane, if V's keys are taken in the same order:
 //     bf16: 16x16-transposing reads of LDS give a lane four keys of one channel;  fp32: a lane reads one channel of one key.
-//   bf16 rounds P to bf16 (to the nearest; 2^-9 of the value, and the sum is of the unrounded weights).
+//   bf16 rounds P to bf16 (to the nearest, at most 2^-8 of a weight; the sum is of the unrounded ones): 2.0e-3 of the result where its own
+//   rounding makes 1.7e-3.
 // LDS holds a tile's rows as they are, their 16-byte pieces exchanged within the row so that neither kind of read finds two
 // rows in the same banks.
-// Bound: HBM with few rows (28 layers, 4 KV heads, 32000 rows of d = 128, g = 7: 289 us, 6.3 TB/s).  With several hundred the products and the vector unit in turn: 32 keys of 32 rows are 16 products (512
-// cycles) and 16 x (maximum, fma, exponential, sum, half a conversion), about as many; what a wavefront does of one does not overlap
-// with the other, and three of them on a SIMD overlap little (counters, 64 sequences x 16384 rows: products 48% of the time, vector
-// instructions 51%).  Two tiles' logits in turn within a wavefront, which takes the registers of the third: 117 -> 138 us.
+// Bound: HBM with few rows (28 layers, 4 KV heads, 32000 rows of d = 128, g = 7: 289 us, 6.3 TB/s).  With several hundred the products
+// and the vector unit in turn: 32 keys of 32 rows are 16 products (512 cycles) and 16 x (maximum, fma, exponential, sum, half a
+// conversion), about as many; what a wavefront does of one does not overlap with the other, and three of them on a SIMD overlap little
+// (64 sequences x 16384 rows, g = 5, 4 layers, 8 KV heads 117 us, 0.73 PFLOP/s; counters: products 48% of the time, vector instructions
+// 51%).  Two tiles' logits in turn within a wavefront, which takes the registers of the third: 117 -> 138 us.
 #include "gkv_internal.h"
 
 #include <type_traits>
