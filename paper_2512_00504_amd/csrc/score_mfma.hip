@@ -141,6 +141,34 @@ __device__ __forceinline__ bool stats_in_doubt(float m, float sum) {
   return sum != sum || (fabsf(m) >= GKV_HUGE_LOG2 && m != GKV_NO_MAX);
 }
 
+// The same for a tile of codes, four keys (factors hi + lo) of one row in a lane, N blocks of rows; logits(b): those of block b.  m is the
+// largest logit of the wavefront's first tile, and stays while the sum has room: 32-bit weights lose nothing by being large.  At 2^64 m is raised by the sum's
+// exponent; a sum that overflows is in doubt.  So a tile has one branch, not one a block, no maxima, and what its blocks do
+// overlaps.  us, the largest logit at once -> this: bf16 128 units of 2112 rows, g = 5, w = 32 58.0 -> 47.3; 896 of 640, g = 7, w = 16 70.6 -> 64.9; 4 of
+// 640 14.0 -> 12.7; in the kernel below d = 64, 696 of 1491, g = 8, w = 32 337 -> 170 (there also the next tile ahead and a lane's keys of one row).
+struct First { static constexpr bool value = false; };     // in place of `exact`: not exact, and a wavefront's first tile
+template <bool FIRST, int N, typename Logits>
+__device__ __forceinline__ void add_keys(float (&m)[N], float (&sum)[N], const f32x4& hi, const f32x4& lo, Logits logits) {
+  float top = 0.f;
+#pragma unroll
+  for (int b = 0; b < N; ++b) {
+    const f32x4 z = logits(b);
+    if constexpr (FIRST)
+      m[b] = fmaxf(m[b], fmaxf(fmaxf(rounded_product(z[0], hi[0]), rounded_product(z[1], hi[1])), fmaxf(rounded_product(z[2], hi[2]), rounded_product(z[3], hi[3]))));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[b] += __builtin_amdgcn_exp2f(fmaf(z[e], lo[e], fmaf(z[e], hi[e], -m[b])));
+    top = fmaxf(top, sum[b]);
+  }
+  if (!FIRST && __any(top >= 0x1p64f)) {
+#pragma unroll
+    for (int b = 0; b < N; ++b) {
+      const int e = max(0, __builtin_amdgcn_frexp_expf(sum[b]));
+      sum[b] = __builtin_amdgcn_ldexpf(sum[b], -e);
+      m[b] += (float)e;
+    }
+  }
+}
+
 // Offset of a window row with maximum m (log2 units) and sum s, as hi + lo; a row that is not there has a
 // huge negative one.  Rows with a huge maximum keep it as it is in hi, for log2_score<true>.
 __device__ __forceinline__ float2 row_offset(bool valid, float m, float s) {
@@ -296,7 +324,84 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
       for (int c = 0; c < NL; ++c) q[c] = *(const u32x4*)(qs + (size_t)blk * G::TILE_BYTES + c * 1024 + lane * 16);
     };
 
-    if constexpr (!HAVE_STATS) {
+    if constexpr (!HAVE_STATS && K8) {
+      // ---- first pass over K, as below: lane (row r of a block, keys 4 kb + e) ------------------
+      constexpr int NB = 4;
+      const int n_tiles = (l + 15) >> 4, n_full = (cc + 1) >> 4, n_blocks = nts * pl.n_blk;
+      for (int b0 = 0; b0 < n_blocks; b0 += NB) {
+        float rm[NB], rs[NB];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) { rm[i] = GKV_NO_MAX; rs[i] = 0.f; }
+        auto request = [&](Raw<T, D, K8>& k, int t) { load_k8_tile<T, D, false, false>(k, Kh, scales, t, seq.n_tiled, lane, r, kb); };
+        auto stats_tile = [&](const Raw<T, D, K8>& raw, int t, auto exact) {
+          Tile<T, D> k;
+          expand<T, D>(k, raw);
+          f32x4 t_hi, t_lo;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float scale = q8_k_scale(raw[D / 64][e]);
+            t_hi[e] = hi * scale; t_lo[e] = lo * scale;
+          }
+          auto of_block = [&](int i) {
+            u32x4 q[NL];
+            load_q(q, min(b0 + i, n_blocks - 1));
+            return logits<T, NL>(k, q);
+          };
+          if constexpr (!decltype(exact)::value) {
+            add_keys<std::is_same_v<decltype(exact), First>>(rm, rs, t_hi, t_lo, of_block);
+          } else {
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+              const f32x4 z = of_block(i);
+              const int seen = cc + k_of(16 * min(b0 + i, n_blocks - 1) + r, nt0);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                // a key the row did not see has the logit -inf (and its scale may be anything behind the last row)
+                const bool unseen = 16 * t + 4 * kb + e > seen;
+                add_to_stats<true>(unseen ? -INFINITY : z[e], unseen ? hi : t_hi[e], unseen ? lo : t_lo[e], rm[i], rs[i]);
+              }
+            }
+          }
+        };
+        auto exact_tiles = [&](int t0) {
+          for (int t = t0; t < n_tiles; t += NW) {
+            Raw<T, D, K8> kT;
+            request(kT, t);
+            stats_tile(kT, t, std::true_type{});
+          }
+        };
+        // (asked for here: the score's own first tiles are not on their way yet)
+        if (wave < n_full) {
+          request(kA[0], wave);
+          request(kN[0], min(wave + NW, n_full - 1));
+          stats_tile(kA[0], wave, First{});
+        }
+        for (int t = wave + NW; t < n_full; t += 2 * NW) {
+          request(kA[0], min(t + NW, n_full - 1));
+          stats_tile(kN[0], t, std::false_type{});
+          if (t + NW >= n_full) break;
+          request(kN[0], min(t + 2 * NW, n_full - 1));
+          stats_tile(kA[0], t + NW, std::false_type{});
+        }
+        bool again = false;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) again |= stats_in_doubt(rm[i], rs[i]) || rs[i] == INFINITY;
+        if (__any(again)) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i) { rm[i] = GKV_NO_MAX; rs[i] = 0.f; }
+        }
+        exact_tiles(__any(again) ? wave : n_full + (wave + NW - n_full % NW) % NW);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          float m = fmaxf(rm[i], __shfl_xor(rm[i], 16));
+          m = fmaxf(m, __shfl_xor(m, 32));
+          float sum = rs[i] * __builtin_amdgcn_exp2f(rm[i] - m);
+          sum += __shfl_xor(sum, 16);
+          sum += __shfl_xor(sum, 32);
+          if (kb == 0 && b0 + i < n_blocks) red_ms[wave * rows_pass + 16 * (b0 + i) + r] = make_float2(m, sum);
+        }
+      }
+    } else if constexpr (!HAVE_STATS) {
       // ---- first pass over K: row max and row sum over the keys visible to each window row -----
       // NB blocks at a time keep their running (max, sum) in registers; only the last tiles (those
       // reaching into the window) need the causal mask.
@@ -371,6 +476,8 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
             if (r == 0 && b0 + i < n_blocks) red_ms[wave * rows_pass + 16 * (b0 + i) + 4 * kb + e] = make_float2(m, sum);
           }
       }
+    }
+    if constexpr (!HAVE_STATS) {
       __syncthreads();
       for (int x = tid; x < rows; x += NW * 64) {
         float M = red_ms[x].x;
@@ -621,6 +728,17 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
     };
     auto stats_tile = [&](const Raw<T, D, K8>& raw, int t, auto exact) { opened(raw, [&](const Tile<T, D>& kT, const f32x4& t_hi, const f32x4& t_lo) {
       constexpr bool EXACT = decltype(exact)::value;
+      if constexpr (K8 && !EXACT) {
+        auto of_block = [&](int b) {
+          if (b >= HELD) {
+            asm volatile("" ::: "memory");
+            load_q(q[b], b);
+          }
+          return logits<T, NL>(kT, q[b]);
+        };
+        add_keys<std::is_same_v<decltype(exact), First>>(rm, rs, t_hi, t_lo, of_block);
+        return;
+      }
 #pragma unroll
       for (int b = 0; b < NT * NB; ++b) {
         f32x4 s_hi = t_hi, s_lo = t_lo;
@@ -663,7 +781,17 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
       }
     };
     reset();
-    for (int t = wave; t < n_full; t += 2 * NW) {
+    int t0 = wave;
+    if constexpr (K8) {
+      if (wave < n_full) {
+        load_tile(kN, min(wave + NW, n_full - 1), std::false_type{});
+        stats_tile(kA, wave, First{});
+#pragma unroll
+        for (int c = 0; c < D / 64 + 1; ++c) kA[c] = kN[c];
+      }
+      t0 += NW;
+    }
+    for (int t = t0; t < n_full; t += 2 * NW) {
       load_tile(kN, min(t + NW, n_full - 1), std::false_type{});
       stats_tile(kA, t, std::false_type{});
       if (t + NW >= n_full) break;
@@ -672,7 +800,7 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
     }
     bool again = false;
 #pragma unroll
-    for (int b = 0; b < NT * NB; ++b) again |= stats_in_doubt(rm[b], rs[b]);
+    for (int b = 0; b < NT * NB; ++b) again |= stats_in_doubt(rm[b], rs[b]) || (K8 && rs[b] == INFINITY);
     if (__any(again)) reset();
     exact_tiles(__any(again) ? wave : n_full + (wave + NW - n_full % NW) % NW);
     if (g0 + wave < g1) load_tile(kA, g0 + wave, std::false_type{});

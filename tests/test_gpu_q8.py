@@ -352,6 +352,28 @@ def test_window_score_of_many_and_of_long_units(decoded):
     _score_case("f32", 64, 3, 8, 1500, 64, [1501], decoded=decoded, hkv=1)
 
 
+@pytest.mark.parametrize("jumps", [{300: 30}, {300: 60}, {300: 60, 430: 110}, {300: 100}, {5: 100, 300: 140, 440: 30}, {300: -90}, {n: -70 for n in range(256)}])
+@pytest.mark.parametrize("dtype,d,g,w", [("bf16", 128, 7, 16), ("bf16", 64, 8, 32), ("f32", 64, 2, 8), ("bf16", 64, 3, 4)])
+def test_window_score_of_logits_that_grow_along_the_cache(dtype, d, g, w, jumps):
+    # sums that reach 2^64 and more, and that overflow, under the first keys' maximum: row n's logit is about jumps[n]
+    b, n = 448, 512
+    st = _state(B=1, hkv=1, g=g, d=d, dtype=dtype, b=b, w=w, s=64, cap=512)
+    gen = torch.Generator().manual_seed(d + g)
+    K, V = (torch.randn(1, 1, 1, 512, d, generator=gen).to(DT[dtype]) for _ in range(2))
+    u = (torch.randint(0, 2, (d,), generator=gen) * 2 - 1).double()
+    for row, z in jumps.items():
+        K[0, 0, 0, row] = (u * z / math.sqrt(d)).to(DT[dtype])
+    q = (u + 0.25 * torch.randn(w, 1, 1, g, d, generator=gen).double()).to(DT[dtype])
+    t = 2 * w + 3
+    _fill(st, K, V, [n], b, since=t - w + 1, decoded=w)
+    for k in range(w):
+        st.qwin[(t - w + 1 + k) % w] = q[k].cuda()
+    st.score_window(t)
+    hK, qw = values(K[0, 0, 0]), q[:, 0, 0].double()
+    ref, tol = local_score(qw, hK, 1 / math.sqrt(d)), logit_error(qw, hK, 1 / math.sqrt(d))
+    assert ((st.S[0, 0, 0, :n - w].cpu().double() - ref).abs() <= tol * ref + 1e-30).all()
+
+
 @pytest.mark.parametrize("decoded", [False, True])
 def test_window_score_in_the_plain_kernels(decoded):
     _score_case("bf16", 128, 3, 8, 64, 16, [65, 80], params={"force_generic": 1}, decoded=decoded)
