@@ -673,6 +673,9 @@ static gkv_status check_q8(const gkv_ctx* ctx, std::initializer_list<const void*
   return aligned16(ptrs) ? GKV_OK : GKV_ERR_INVALID_ARG;
 }
 
+// The cache as the record of softmax statistics knows it: another than one of config.dtype that has or had the same address.
+static const void* q8_record(const void* K8) { return (const char*)K8 + 1; }
+
 extern "C" gkv_status gkv_q8_store_prompt(gkv_ctx* ctx, const void* k, const void* v, int32_t n, int32_t t_first, int32_t t0,
                                           const int32_t* d_prompt_len, void* K8, void* V8, void* scales, int32_t* pos,
                                           void* stream) {
@@ -715,10 +718,10 @@ extern "C" gkv_status gkv_q8_attend_decode(gkv_ctx* ctx, const void* q, const vo
     if (st != GKV_OK) return st;
     a.waves = plan.waves; a.splits = plan.splits; a.split_iters = plan.iters;
     a.write_stats = k_new != nullptr;
-    note_stats(ctx, step, a.write_stats != 0, workspace, K8, qwin, (hipStream_t)stream);
+    note_stats(ctx, step, a.write_stats != 0, workspace, q8_record(K8), qwin, (hipStream_t)stream);
     return hip_status(gkv_launch_q8_attend_mfma(ln, ctx->dims, ctx->cfg.dtype, a));
   }
-  note_stats(ctx, step, false, workspace, K8, qwin, (hipStream_t)stream);
+  note_stats(ctx, step, false, workspace, q8_record(K8), qwin, (hipStream_t)stream);
   return hip_status(gkv_launch_q8_attend_generic(ln, ctx->dims, ctx->cfg.dtype, a));
 }
 
@@ -732,7 +735,7 @@ extern "C" gkv_status gkv_q8_score_window(gkv_ctx* ctx, const void* qwin, const 
   ScoreArgs a{qwin, K8, d_state, step, S, nullptr, (const uint32_t*)scales};
   GkvLaunch ln{ctx, GKV_K_SCORE, (hipStream_t)stream};
   if (use_mfma(ctx, {qwin})) {
-    if (stats_cover_window(ctx, step, workspace, K8, qwin)) a.stats = gkv_carve_workspace(ctx, workspace).stats;
+    if (stats_cover_window(ctx, step, workspace, q8_record(K8), qwin)) a.stats = gkv_carve_workspace(ctx, workspace).stats;
     return hip_status(gkv_launch_score_mfma(ln, ctx->dims, ctx->cfg.dtype, a, len_max_host));
   }
   return hip_status(gkv_launch_q8_score_generic(ln, ctx->dims, ctx->cfg.dtype, a));

@@ -379,6 +379,25 @@ def test_window_score_in_the_plain_kernels(decoded):
     _score_case("bf16", 128, 3, 8, 64, 16, [65, 80], params={"force_generic": 1}, decoded=decoded)
 
 
+def test_statistics_of_a_cache_of_another_type_at_the_same_address_are_not_taken():
+    b, w, s, d, n = 64, 8, 16, 128, 80
+    st, ref = _state(hkv=1, g=4, d=d, b=b, w=w, s=s, cap=96), _state(hkv=1, g=4, d=d, b=b, w=w, s=s, cap=96)
+    gen = torch.Generator().manual_seed(3)
+    K, V = _rows(gen, "bf16", 1, 1, 1, 96, d), _rows(gen, "bf16", 1, 1, 1, 96, d)
+    memory = torch.zeros(1, 1, 1, 96, d, dtype=torch.bfloat16, device="cuda")
+    plain_v = torch.zeros_like(memory)
+    st.d_state.copy_(torch.tensor([[[n - w, 5, 0, 0]]], dtype=torch.int32))
+    for t in range(5, 5 + w):
+        q, kn, vn = _token(gen, "bf16", 1, 1, 1, 4, d)
+        st.ctx.attend_decode(q.cuda(), kn.cuda(), vn.cuda(), memory, plain_v, st.pos, t, st.qwin, st.d_state, n - w + t - 5, st.out, st.workspace)
+    ref.qwin.copy_(st.qwin)
+    st.K8 = memory.view(torch.uint8).flatten()[:96 * d].view(torch.float8_e4m3fn).view(ref.K8.shape)
+    for x in (st, ref):
+        _fill(x, K, V, [n], b, since=5, decoded=w)
+        x.score_window(4 + w)
+    assert st.K8.data_ptr() == memory.data_ptr() and torch.equal(st.S, ref.S)
+
+
 # ---- compaction ------------------------------------------------------------------------------------
 @pytest.mark.parametrize("d,B,b,w,s,n_tiled", [(128, 2, 64, 8, 16, 0), (128, 2, 64, 8, 16, 64), (64, 3, 100, 4, 28, 96), (128, 1, 512, 16, 128, 512),
                                                (16, 2, 40, 4, 8, 32), (48, 2, 64, 8, 16, 64), (512, 1, 64, 8, 16, 64), (128, 70, 64, 8, 16, 64),
