@@ -142,24 +142,31 @@ __device__ __forceinline__ bool stats_in_doubt(float m, float sum) {
 }
 
 // The same for a tile of codes, four keys (factors hi + lo) of one row in a lane, N blocks of rows; logits(b): those of block b.  m is the
-// largest logit of the wavefront's first tile, and stays while the sum has room: 32-bit weights lose nothing by being large.  At 2^64 m is raised by the sum's
-// exponent; a sum that overflows is in doubt.  So a tile has one branch, not one a block, no maxima, and what its blocks do
-// overlaps.  us, the largest logit at once -> this: bf16 128 units of 2112 rows, g = 5, w = 32 58.0 -> 47.3; 896 of 640, g = 7, w = 16 70.6 -> 64.9; 4 of
-// 640 14.0 -> 12.7; in the kernel below d = 64, 696 of 1491, g = 8, w = 32 337 -> 170 (there also the next tile ahead and a lane's keys of one row).
+// largest logit of the wavefront's first tile, rounded up to a whole number, and stays while the sums are below 2^8; then it is raised by a sum's
+// exponent, which is exact (m stays whole, a sum is only scaled).  A sum that overflows is in doubt.  So a tile has one branch, not one a block, and no
+// maxima, and what its blocks do overlaps.  A weight's exponent is rounded at 2^-24 of it: at 2^-21 where a row's logits
+// rise by less than a factor of 2^8 within a tile, at 2^-18 at the very most (a sum below 2^128).  us, the largest logit at once -> this: bf16 128 units of
+// 2112 rows, g = 5, w = 32 58.0 -> 48.0; 896 of 640, g = 7, w = 16 70.6 -> 66.4; 4 of 640 14.0 -> 12.1; in the kernel below d = 64, 696 of 1491, g = 8,
+// w = 32 337 -> 145 (there also the next tile ahead and a lane's keys of one row), heavy-tailed logits 231.  Raised at 2^12, 2^20 or 2^64: the same times
+// (+-2%), errors of a sum up to 1.4e-5.
 struct First { static constexpr bool value = false; };     // in place of `exact`: not exact, and a wavefront's first tile
+constexpr float SUM_ROOM = 0x1p8f;
 template <bool FIRST, int N, typename Logits>
 __device__ __forceinline__ void add_keys(float (&m)[N], float (&sum)[N], const f32x4& hi, const f32x4& lo, Logits logits) {
   float top = 0.f;
 #pragma unroll
   for (int b = 0; b < N; ++b) {
     const f32x4 z = logits(b);
-    if constexpr (FIRST)
-      m[b] = fmaxf(m[b], fmaxf(fmaxf(rounded_product(z[0], hi[0]), rounded_product(z[1], hi[1])), fmaxf(rounded_product(z[2], hi[2]), rounded_product(z[3], hi[3]))));
+    if constexpr (FIRST) {
+      float x = fmaxf(fmaxf(rounded_product(z[0], hi[0]), rounded_product(z[1], hi[1])), fmaxf(rounded_product(z[2], hi[2]), rounded_product(z[3], hi[3])));
+      x = fmaxf(x, __shfl_xor(x, 16));                     // the four lanes of a row
+      m[b] = fmaxf(m[b], ceilf(fmaxf(x, __shfl_xor(x, 32))));
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[b] += __builtin_amdgcn_exp2f(fmaf(z[e], lo[e], fmaf(z[e], hi[e], -m[b])));
     top = fmaxf(top, sum[b]);
   }
-  if (!FIRST && __any(top >= 0x1p64f)) {
+  if (!FIRST && __any(top >= SUM_ROOM)) {
 #pragma unroll
     for (int b = 0; b < N; ++b) {
       const int e = max(0, __builtin_amdgcn_frexp_expf(sum[b]));
