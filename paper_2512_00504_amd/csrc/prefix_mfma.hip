@@ -7,8 +7,10 @@
 //   8 i + 4 h + e of its row, so the softmax stays in the lane but for one exchange with the other half, and they are what the
 //   product  O^T[channel, row] += V^T P^T  wants of P in that lane, if V's keys are taken in the same order:
 //     bf16: 16x16-transposing reads of LDS give a lane four keys of one channel;  fp32: a lane reads one channel of one key.
-//   bf16 rounds P to bf16 (to the nearest, at most 2^-8 of a weight; the sum is of the unrounded ones): 2.0e-3 of the result where its own
-//   rounding makes 1.7e-3.
+//   bf16 rounds P to bf16 (to the nearest, at most 2^-8 of a weight), and l is the sum of the rounded ones: a weight's rounding then moves the result
+//   by a part of how far that value is from the mean, and not at all where one key dominates or the values are equal.  Error of the result, whose own
+//   rounding makes 1.7e-3: 1.7e-3 to 2.0e-3 with peaked weights (sum of the unrounded ones: 1.9e-3 to 2.4e-3), 2.4e-3 with flat ones.  With the maximum
+//   followed at once, not at a distance of up to 8, peaked 1.7e-3 to 1.8e-3, but 5 to 8% more time (28 layers, 64 sequences x 4000 rows 158 -> 169 us).
 // LDS holds a tile's rows as they are, their 16-byte pieces exchanged within the row so that neither kind of read finds two
 // rows in the same banks.
 // Bound: HBM with few rows (28 layers, 4 KV heads, 32000 rows of d = 128, g = 7: 289 us, 6.3 TB/s).  With several hundred the products
@@ -207,13 +209,23 @@ __global__ __launch_bounds__(256, sizeof(T) * D >= 512 && NK > 1 ? 1 : NK > 1 ||
                            : fmaf(s[i][e], a.scale_hi, -m);
     }
     float sum = 0.f;
+    u32x4 p[G::F32 ? 1 : SUB][2];                            // bf16: the weights of 16 keys each, 8 (2 k) + 4 h + e and 8 (2 k + 1) + 4 h + e
 #pragma unroll
-    for (int i = 0; i < SUB; ++i)
+    for (int i = 0; i < SUB; ++i) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[i][e] = __builtin_amdgcn_exp2f(s[i][e]);
-        sum += s[i][e];
+      for (int e = 0; e < 16; ++e) s[i][e] = __builtin_amdgcn_exp2f(s[i][e]);
+      if constexpr (G::F32) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum += s[i][e];
+      } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const bf16x2 pair = __builtin_convertvector((f32x2{s[i][2 * x], s[i][2 * x + 1]}), bf16x2);
+          p[i][x >> 2][x & 3] = __builtin_bit_cast(uint32_t, pair);
+          sum = __builtin_amdgcn_fdot2_f32_bf16(pair, __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
+        }
       }
+    }
     l += sum;
 #pragma unroll
     for (int i = 0; i < SUB; ++i) {
@@ -229,11 +241,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D >= 512 && NK > 1 ? 1 : NK > 1 ||
         }
       } else {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {                        // 16 keys: 8 (2 k) + 4 h + e and 8 (2 k + 1) + 4 h + e
-          u32x4 p;
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
-            p[y] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{s[i][8 * k + 2 * y], s[i][8 * k + 2 * y + 1]}), bf16x2));
+        for (int k = 0; k < 2; ++k) {
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb) {
             s16x4 v[2];
@@ -250,7 +258,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D >= 512 && NK > 1 ? 1 : NK > 1 ||
               }
             }
             o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, (u32x4{v0[0], v0[1], v1[0], v1[1]})),
-                                                            __builtin_bit_cast(bf16x8, p), o[cb], 0, 0, 0);
+                                                            __builtin_bit_cast(bf16x8, p[i][k]), o[cb], 0, 0, 0);
           }
         }
       }
