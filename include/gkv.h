@@ -321,7 +321,8 @@ gkv_status gkv_evict_static(gkv_ctx* ctx, const void* qwin, void* K, void* V, fl
  * so are the rules for steps, lengths and no-ops.  head_dim has to be a multiple of 16 (else GKV_ERR_SHAPE).  K8, V8, scales
  * and the rows of gkv_q8_store_prompt and gkv_q8_read have to be 16-byte aligned (else GKV_ERR_INVALID_ARG).
  * gkv_global_update, gkv_select_topk, gkv_pool_scores and gkv_evicted_positions do not look at K or V and serve such a cache
- * as they are; for gkv_redundancy_combine read K back first.
+ * as they are; for gkv_redundancy_combine read K back first (for some sequences of some layers at a time, a context with n_layers = 1 and
+ * their number as the batch takes the slices of all buffers that begin at the first of them).
  *
  * gkv_q8_store_prompt: prompt rows into the cache.  k, v [n,L,B,h_kv,d] hold the positions t_first .. t_first + n - 1 of
  * every sequence's token stream; sequence i's prompt is the positions [t0 - P_i, t0) with P_i = d_prompt_len[i] (device,

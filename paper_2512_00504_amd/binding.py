@@ -169,6 +169,7 @@ class Context:
         self.h = h
         self._handle = h.value
         self._call = _load_call()
+        self.params, self.step_base = {}, None               # as set, for contexts that go the same way on a part of the batch
 
     def close(self):
         if getattr(self, "h", None):
@@ -187,6 +188,7 @@ class Context:
 
     def set_param(self, name: str, value: int):
         self._check(self.lib.gkv_set_param(self.h, name.encode(), value), "gkv_set_param")
+        self.params[name] = value
 
     def workspace_bytes(self) -> int:
         n = c_size_t()
@@ -196,6 +198,7 @@ class Context:
     def set_step_base(self, d_step_base):
         """d_step_base: int32 device tensor of one element (or None for absolute steps)."""
         self._check(self.lib.gkv_set_step_base(self.h, _ptr(d_step_base)), "gkv_set_step_base")
+        self.step_base = d_step_base
 
     def advance_step_base(self, delta: int):
         self._check(self.lib.gkv_advance_step_base(self.h, delta, _stream()), "gkv_advance_step_base")

@@ -221,8 +221,8 @@ class DecodeState:
 class Q8DecodeState(DecodeState):
     """The same with K and V held in 8 bits: K8, V8 (codes) and scales (of a row of K and of V) in place of K and V.
 
-    The redundancy term needs K in the configuration's type: redundancy_combine() reads it back into a buffer that is
-    made at its first call."""
+    The redundancy term needs K in the configuration's type: redundancy_combine() reads it back part by part, into a buffer
+    for one part that is made at its first call."""
 
     def _allocate_cache(self):
         cfg = self.cfg
@@ -231,6 +231,7 @@ class Q8DecodeState(DecodeState):
                             for _ in range(2))
         self.scales = torch.ones(*shape, 2, dtype=torch.bfloat16, device=self.device)
         self.K = self.V = None
+        self._part_ctx = self._K_part = None
 
     def load_prompt_rows(self, t_first, k, v, t0, prompt_lens):
         """As DecodeState's, quantised on the way.  Rows that would lie at or beyond the capacity are left out."""
@@ -275,11 +276,39 @@ class Q8DecodeState(DecodeState):
     def score_window(self, step):
         self.ctx.q8_score_window(self.qwin, self.K8, self.scales, self.d_state, step, self.len_host, self.S, self.workspace)
 
+    def _parts(self):
+        """The (layer, sequence)s in parts: [(first, context of that many sequences)].  A part is a whole round of the redundancy kernel, a
+        workgroup for each compute unit; the last two share what is left, as launches of up to 128 (sequence, KV head)s go another way.
+        (us, all of K at once / parts twice as large / these: 896 units of 640 rows 166 / 172 / 182, 18432 of 1088 7420 / 7400 / 7770.)"""
+        if self._part_ctx is None:
+            cfg, n = self.cfg, self.cfg.n_layers * self.cfg.batch
+            at_once = max(1, 256 // cfg.n_kv_heads)
+            cuts = list(range(0, n, at_once)) + [n]
+            if len(cuts) > 2 and (n - cuts[-2]) * cfg.n_kv_heads <= 128:
+                cuts[-2] = (cuts[-3] + n) // 2
+            self._part_ctx, of = [], {}
+            for lo, hi in zip(cuts, cuts[1:]):
+                if hi - lo not in of:
+                    part = GkvConfig.from_buffer_copy(cfg)
+                    part.n_layers, part.batch = 1, hi - lo
+                    of[hi - lo] = Context(part)
+                self._part_ctx.append((lo, of[hi - lo]))
+            self._K_part = torch.zeros(max(of), *self.K8.shape[2:], dtype=self.qwin.dtype, device=self.device)
+        return self._part_ctx
+
     def redundancy_combine(self, step, lam, tau, n_recent, eps=1e-8):
-        if self.K is None:
-            self.K = torch.zeros(self.K8.shape, dtype=self.qwin.dtype, device=self.device)
-        self.read(step + 1, K=self.K)
-        super().redundancy_combine(step, lam, tau, n_recent, eps)
+        of = lambda x, lo, n: x.flatten(0, 1)[lo:lo + n]
+        for lo, ctx in self._parts():
+            n = ctx.cfg.batch
+            if ctx.step_base is not self.ctx.step_base:
+                ctx.set_step_base(self.ctx.step_base)
+            for name, value in self.ctx.params.items():
+                if ctx.params.get(name) != value:
+                    ctx.set_param(name, value)
+            K, d_state = self._K_part[:n], of(self.d_state, lo, n)
+            ctx.q8_read(of(self.K8, lo, n), None, of(self.scales, lo, n), d_state, step + 1, K, None)
+            ctx.redundancy_combine(K, d_state, step, self.len_host, of(self.F, lo, n), lam, tau, eps, n_recent,
+                                   of(self.R, lo, n), of(self.F_sel, lo, n), None)
 
     def compact(self, step):
         self.ctx.q8_compact(self.keep_idx, self.F, self.K8, self.V8, self.scales, self.F_hist, self.pos, self.d_state, step,
