@@ -169,9 +169,25 @@ class Context:
         self.h = h
         self._handle = h.value
         self._call = _load_call()
-        self.params, self.step_base = {}, None               # as set, for contexts that go the same way on a part of the batch
+        self._params, self._step_base, self._profiled, self._parts = {}, None, False, {}
+
+    def part(self, sequences: int) -> "Context":
+        """A context of so many (layer, sequence)s, for calls on slices of this one's buffers.  It is set as this one is, now and later, and
+        the time and calls of its kernels count here."""
+        if sequences not in self._parts:
+            cfg = GkvConfig.from_buffer_copy(self.cfg)
+            cfg.n_layers, cfg.batch = 1, sequences
+            part = Context(cfg)
+            for name, value in self._params.items():
+                part.set_param(name, value)
+            part.set_step_base(self._step_base)
+            part.profile_enable(self._profiled)
+            self._parts[sequences] = part
+        return self._parts[sequences]
 
     def close(self):
+        for part in getattr(self, "_parts", {}).values():
+            part.close()
         if getattr(self, "h", None):
             self.lib.gkv_destroy(self.h)
             self.h = self._handle = None
@@ -188,7 +204,9 @@ class Context:
 
     def set_param(self, name: str, value: int):
         self._check(self.lib.gkv_set_param(self.h, name.encode(), value), "gkv_set_param")
-        self.params[name] = value
+        self._params[name] = value
+        for part in self._parts.values():
+            part.set_param(name, value)
 
     def workspace_bytes(self) -> int:
         n = c_size_t()
@@ -198,7 +216,9 @@ class Context:
     def set_step_base(self, d_step_base):
         """d_step_base: int32 device tensor of one element (or None for absolute steps)."""
         self._check(self.lib.gkv_set_step_base(self.h, _ptr(d_step_base)), "gkv_set_step_base")
-        self.step_base = d_step_base
+        self._step_base = d_step_base
+        for part in self._parts.values():
+            part.set_step_base(d_step_base)
 
     def advance_step_base(self, delta: int):
         self._check(self.lib.gkv_advance_step_base(self.h, delta, _stream()), "gkv_advance_step_base")
@@ -350,14 +370,20 @@ class Context:
 
     def profile_enable(self, on: bool):
         self._check(self.lib.gkv_profile_enable(self.h, int(on)), "gkv_profile_enable")
+        self._profiled = bool(on)
+        for part in self._parts.values():
+            part.profile_enable(on)
 
     def profile_reset(self):
         self._check(self.lib.gkv_profile_reset(self.h), "gkv_profile_reset")
+        for part in self._parts.values():
+            part.profile_reset()
 
     def profile_read(self, kernel: str):
         ms, n = c_double(), c_int64()
         self._check(self.lib.gkv_profile_read(self.h, KERNEL_IDS[kernel], byref(ms), byref(n)), "gkv_profile_read")
-        return ms.value, n.value
+        of_parts = [part.profile_read(kernel) for part in self._parts.values()]
+        return ms.value + sum(x for x, _ in of_parts), n.value + sum(x for _, x in of_parts)
 
 
 def probe_attend_read(K, V, rows, sink):

@@ -286,25 +286,15 @@ class Q8DecodeState(DecodeState):
             cuts = list(range(0, n, at_once)) + [n]
             if len(cuts) > 2 and (n - cuts[-2]) * cfg.n_kv_heads <= 128:
                 cuts[-2] = (cuts[-3] + n) // 2
-            self._part_ctx, of = [], {}
-            for lo, hi in zip(cuts, cuts[1:]):
-                if hi - lo not in of:
-                    part = GkvConfig.from_buffer_copy(cfg)
-                    part.n_layers, part.batch = 1, hi - lo
-                    of[hi - lo] = Context(part)
-                self._part_ctx.append((lo, of[hi - lo]))
-            self._K_part = torch.zeros(max(of), *self.K8.shape[2:], dtype=self.qwin.dtype, device=self.device)
+            self._part_ctx = [(lo, self.ctx.part(hi - lo)) for lo, hi in zip(cuts, cuts[1:])]
+            most = max(hi - lo for lo, hi in zip(cuts, cuts[1:]))
+            self._K_part = torch.zeros(most, *self.K8.shape[2:], dtype=self.qwin.dtype, device=self.device)
         return self._part_ctx
 
     def redundancy_combine(self, step, lam, tau, n_recent, eps=1e-8):
         of = lambda x, lo, n: x.flatten(0, 1)[lo:lo + n]
         for lo, ctx in self._parts():
             n = ctx.cfg.batch
-            if ctx.step_base is not self.ctx.step_base:
-                ctx.set_step_base(self.ctx.step_base)
-            for name, value in self.ctx.params.items():
-                if ctx.params.get(name) != value:
-                    ctx.set_param(name, value)
             K, d_state = self._K_part[:n], of(self.d_state, lo, n)
             ctx.q8_read(of(self.K8, lo, n), None, of(self.scales, lo, n), d_state, step + 1, K, None)
             ctx.redundancy_combine(K, d_state, step, self.len_host, of(self.F, lo, n), lam, tau, eps, n_recent,

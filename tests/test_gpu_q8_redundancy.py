@@ -92,3 +92,14 @@ def test_a_recorded_redundancy_term_replays_as_an_eager_one():
         torch.cuda.synchronize()
         assert torch.equal(st.R, ref.R) and torch.equal(st.F_sel, ref.F_sel), k
         st.redundancy_combine(27, 0.7, 0.3, 8)             # an eager call in between
+
+
+def test_profile_counts_the_parts():
+    st, _ = _pair(2, 80, 4, 1, 128, "bf16", 40, 8, 16, 64)
+    st.ctx.profile_enable(True)
+    for _ in range(2):
+        st.redundancy_combine(27, 0.7, 0.3, 8)
+    ms, calls = st.ctx.profile_read("redundancy")
+    assert ms > 0 and calls == 2 * len(st._parts()) == 6
+    st.ctx.profile_reset()
+    assert st.ctx.profile_read("redundancy") == (0.0, 0)
