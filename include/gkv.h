@@ -370,8 +370,9 @@ gkv_status gkv_q8_evict(gkv_ctx* ctx, const void* qwin, void* K8, void* V8, void
  * leaves there, for each query head of its sequences, maximum, sum and weighted values of up to 64 pieces of the prefix, in 32 bits;
  * those of other sequences stay as they are, so a batch of several prompts takes one call for each of them (on one stream, or ordered by events), and a sequence
  * that has none a part that still is zero.  Results stay until they are written again: call it in every step.
- * rows may be 0 (Kp and Vp are not looked at then).  A call with more rows than the context's gkv_prefix_bytes calls were asked for
- * returns GKV_ERR_WORKSPACE.  Both calls can be recorded; the rows are frozen then.  More than 2^30 rows: GKV_ERR_SHAPE.
+ * rows may be 0 (Kp and Vp are not looked at then).  A call with more rows than any of the context's gkv_prefix_bytes calls was asked for
+ * returns GKV_ERR_WORKSPACE; the size of `part` itself is not known here: with buffers of several sizes the caller keeps them apart.
+ * Both calls can be recorded; the rows are frozen then.  More than 2^30 rows: GKV_ERR_SHAPE.
  * The result is the same to the last bit for the same rows, first, count and alignment of the arguments.
  */
 gkv_status gkv_prefix_bytes(gkv_ctx* ctx, int32_t rows, size_t* out_bytes);

@@ -20,6 +20,7 @@ LIB_PATH = os.environ.get("GKV_LIB_PATH") or os.path.join(_HERE, "libgkv.so")
 
 GKV_F32, GKV_BF16 = 0, 1
 GKV_COMBINE = {"max": 0, "avg": 1, "sum": 2}
+GKV_ERR_WORKSPACE = 3
 ST_LEN, ST_LEN_STEP, ST_N_HIST, ST_N_TILED = 0, 1, 2, 3     # fields of a d_state record
 KERNEL_IDS = {"attend": 0, "score": 1, "global": 2, "topk": 3, "compact": 4, "redundancy": 5}
 
@@ -170,6 +171,7 @@ class Context:
         self._handle = h.value
         self._call = _load_call()
         self._params, self._step_base, self._profiled, self._parts = {}, None, False, {}
+        self._prefix_bytes, self._prefix_rows = {}, -1       # rows -> size of a buffer for them; the most rows asked for
 
     def part(self, sequences: int) -> "Context":
         """A context of so many (layer, sequence)s, for calls on slices of this one's buffers.  It is set as this one is, now and later, and
@@ -349,9 +351,15 @@ class Context:
     def prefix_bytes(self, rows: int) -> int:
         n = c_size_t()
         self._check(self.lib.gkv_prefix_bytes(self.h, rows, byref(n)), "gkv_prefix_bytes")
+        self._prefix_bytes[rows], self._prefix_rows = n.value, max(rows, self._prefix_rows)
         return n.value
 
     def prefix_attend(self, q, Kp, Vp, rows, prefix_capacity, first, count, part):
+        """Refuses a part that is too small for rows, which the C call cannot tell; rows beyond all that prefix_bytes() was asked for are its to refuse."""
+        if part is not None and 0 <= rows <= self._prefix_rows:
+            need = self._prefix_bytes.get(rows)
+            if part.numel() * part.element_size() < (self.prefix_bytes(rows) if need is None else need):
+                raise GkvError(GKV_ERR_WORKSPACE, "gkv_prefix_attend")
         st = self._call.gkv_prefix_attend(self._handle, q, Kp, Vp, rows, prefix_capacity, first, count, part)
         if st is None:
             st = self.lib.gkv_prefix_attend(self.h, _ptr(q), _ptr(Kp), _ptr(Vp), rows, prefix_capacity, first, count,
