@@ -234,7 +234,7 @@ class Q8DecodeState(DecodeState):
         self._part_ctx = self._K_part = None
 
     def load_prompt_rows(self, t_first, k, v, t0, prompt_lens):
-        """As DecodeState's, quantised on the way.  Rows that would lie at or beyond the capacity are left out."""
+        """As DecodeState's, quantised on the way.  Rows that would lie at or beyond the capacity are left out; begin_decode() refuses such prompts."""
         cfg, n, lens = self.cfg, k.shape[0], [int(P) for P in prompt_lens]
         row = (cfg.n_layers, cfg.batch, cfg.n_kv_heads, cfg.head_dim)
         if k.shape[1:] != row or v.shape != k.shape:
@@ -246,6 +246,12 @@ class Q8DecodeState(DecodeState):
         k, v = (x.to(self.device, self.qwin.dtype).contiguous() for x in (k, v))
         lens = torch.tensor(lens + [0] * (cfg.batch - len(lens)), dtype=torch.int32).to(self.device)
         self.ctx.q8_store_prompt(k, v, n, t_first, t0, lens, self.K8, self.V8, self.scales, self.pos)
+
+    def begin_decode(self, t0, prompt_lens):
+        """As DecodeState's; refuses a prompt longer than the cache, whose last rows load_prompt_rows() has left out."""
+        if max(prompt_lens) > self.cfg.capacity:
+            raise ValueError(f"gkv: a prompt of {max(prompt_lens)} rows does not fit a capacity of {self.cfg.capacity}")
+        super().begin_decode(t0, prompt_lens)
 
     def load_prefix(self, k, v, t0=0):
         """As DecodeState's, quantised on the way."""
