@@ -426,7 +426,7 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
             rm[i][e] = GKV_NO_MAX; rs[i][e] = 0.f;
             last_vis[i][e] = cc + k_of(16 * min(b0 + i, n_blocks - 1) + 4 * kb + e, nt0);
           }
-        auto stats_tile = [&](const Raw<T, D, K8>& raw, int t, auto exact) { opened(raw, [&](const Tile<T, D>& kA, float s_hi, float s_lo) {
+        auto stats_tile = [&](const Tile<T, D>& kA, int t, auto exact) {
           constexpr bool EXACT = decltype(exact)::value;
           const int key = 16 * t + r;
 #pragma unroll
@@ -437,23 +437,21 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               // a key the row did not see has the logit -inf: it never becomes the maximum and adds 0
-              // (nor does its scale, which may be anything behind the last row)
-              const bool unseen = EXACT && key > last_vis[i][e];
-              if (unseen) z[e] = -INFINITY;
-              add_to_stats<EXACT>(z[e], K8 && unseen ? hi : s_hi, K8 && unseen ? lo : s_lo, rm[i][e], rs[i][e]);
+              if (EXACT && key > last_vis[i][e]) z[e] = -INFINITY;
+              add_to_stats<EXACT>(z[e], hi, lo, rm[i][e], rs[i][e]);
             }
           }
-        }); };
+        };
         auto exact_tiles = [&](int t0) {
           for (int t = t0; t < n_tiles; t += NW) {
-            Raw<T, D, K8> kA;
+            Tile<T, D> kA;
             load_tile(kA, t);
             stats_tile(kA, t, std::true_type{});
           }
         };
         int t = wave;
         for (; t < n_full; t += NW) {
-          Raw<T, D, K8> kA;
+          Tile<T, D> kA;
           load_tile(kA, t);
           stats_tile(kA, t, std::false_type{});
         }
@@ -745,39 +743,39 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
           return logits<T, NL>(kT, q[b]);
         };
         add_keys<std::is_same_v<decltype(exact), First>>(rm, rs, t_hi, t_lo, of_block);
-        return;
-      }
+      } else {
 #pragma unroll
-      for (int b = 0; b < NT * NB; ++b) {
-        f32x4 s_hi = t_hi, s_lo = t_lo;
-        if (b >= HELD) {
-          asm volatile("" ::: "memory");                 // read here, not once before the loop
-          load_q(q[b], b);
-        }
-        f32x4 z = logits<T, NL>(kT, q[b]);
-        if constexpr (EXACT) {
-          // a key the row did not see has the logit -inf: it never becomes the maximum and adds 0
-          const int seen = cc + (pair ? (r & 7) : 16 * (b / NB) + r);
+        for (int b = 0; b < NT * NB; ++b) {
+          f32x4 s_hi = t_hi, s_lo = t_lo;
+          if (b >= HELD) {
+            asm volatile("" ::: "memory");                 // read here, not once before the loop
+            load_q(q[b], b);
+          }
+          f32x4 z = logits<T, NL>(kT, q[b]);
+          if constexpr (EXACT) {
+            // a key the row did not see has the logit -inf: it never becomes the maximum and adds 0
+            const int seen = cc + (pair ? (r & 7) : 16 * (b / NB) + r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (16 * t + 4 * kb + e > seen) {
+                z[e] = -INFINITY;
+                if constexpr (K8) { s_hi[e] = dm.scale_l2_hi; s_lo[e] = dm.scale_l2_lo; }   // (a scale behind the last row may be anything)
+              }
+          }
+          // (one product where the keys share their factor)
+          const float tm = K8 ? fmaxf(fmaxf(rounded_product(z[0], s_hi[0]), rounded_product(z[1], s_hi[1])),
+                                      fmaxf(rounded_product(z[2], s_hi[2]), rounded_product(z[3], s_hi[3])))
+                              : rounded_product(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), s_hi[0]);
+          if (__any(tm > rm[b])) {
+            const float mnew = fmaxf(rm[b], tm);
+            rs[b] *= __builtin_amdgcn_exp2f(rm[b] - mnew);
+            rm[b] = mnew;
+          }
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (16 * t + 4 * kb + e > seen) {
-              z[e] = -INFINITY;
-              if constexpr (K8) { s_hi[e] = dm.scale_l2_hi; s_lo[e] = dm.scale_l2_lo; }   // (a scale behind the last row may be anything)
-            }
+            rs[b] += __builtin_amdgcn_exp2f(EXACT ? log2_weight(z[e], s_hi[e], s_lo[e], rm[b])
+                                                  : fmaf(z[e], s_lo[e], fmaf(z[e], s_hi[e], -rm[b])));
         }
-        // (one product where the keys share their factor)
-        const float tm = K8 ? fmaxf(fmaxf(rounded_product(z[0], s_hi[0]), rounded_product(z[1], s_hi[1])),
-                                    fmaxf(rounded_product(z[2], s_hi[2]), rounded_product(z[3], s_hi[3])))
-                            : rounded_product(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), s_hi[0]);
-        if (__any(tm > rm[b])) {
-          const float mnew = fmaxf(rm[b], tm);
-          rs[b] *= __builtin_amdgcn_exp2f(rm[b] - mnew);
-          rm[b] = mnew;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          rs[b] += __builtin_amdgcn_exp2f(EXACT ? log2_weight(z[e], s_hi[e], s_lo[e], rm[b])
-                                                : fmaf(z[e], s_lo[e], fmaf(z[e], s_hi[e], -rm[b])));
       }
     }); };
     const int n_tiles = (l + 15) >> 4;
