@@ -141,7 +141,8 @@ int64_t gkv_k_offset(const gkv_config* cfg, int32_t row, int32_t channel, int32_
  * the matrix-core attend kernel at bf16, head_dim 128; 32 goes with 4 wavefronts and changes nothing
  * elsewhere), "attend_waves" (4, 8 or 16 wavefronts per workgroup of that kernel; 0 = default: 4 or 8, by
  * the number and length of the units; 16 is taken as 8 at fp32, head_dim 128, and a number whose partial
- * results would not fit 64 KiB of LDS at this dtype, head_dim and group size as 4), "force_generic" (1 = use the plain vector-ALU
+ * results would not fit 64 KiB of LDS at this dtype, head_dim and group size as 4; on 8-bit caches
+ * 16 is taken as 8, and "attend_tile" and "compact_ppt" change nothing), "force_generic" (1 = use the plain vector-ALU
  * kernels even where matrix-core kernels exist), "compact_ppt" (4, 8 or 16: 16-byte pieces
  * a thread of the compaction kernel keeps in flight per round), "score_reuse_stats" (0 = the
  * window score always computes its rows' softmax statistics itself instead of reusing the
@@ -341,6 +342,8 @@ gkv_status gkv_q8_read(gkv_ctx* ctx, const void* K8, const void* V8, const void*
                        int32_t step, void* K, void* V, void* stream);
 
 /* gkv_attend_decode on such a cache.  The new row is attended to as it is held: as its codes.
+ * Logits, weights, sums and outputs are formed in 32 bits; with bf16 queries the matrix-core kernel rounds the weights, the largest being 1, to bf16
+ * for their products with V (4e-4 of the result beside the 1.7e-3 that its own rounding makes).
  * part: as gkv_attend_decode_prefix takes it, or NULL. */
 gkv_status gkv_q8_attend_decode(gkv_ctx* ctx, const void* q, const void* k_new, const void* v_new,
                                 void* K8, void* V8, void* scales, int32_t* pos, int32_t step, void* qwin,
@@ -370,6 +373,7 @@ gkv_status gkv_q8_evict(gkv_ctx* ctx, const void* qwin, void* K8, void* V8, void
  * leaves there, for each query head of its sequences, maximum, sum and weighted values of up to 64 pieces of the prefix, in 32 bits;
  * those of other sequences stay as they are, so a batch of several prompts takes one call for each of them (on one stream, or ordered by events), and a sequence
  * that has none a part that still is zero.  Results stay until they are written again: call it in every step.
+ * bf16: the matrix-core kernel rounds the weights to bf16 for their products with V, and sums the rounded ones.
  * rows may be 0 (Kp and Vp are not looked at then).  A call with more rows than any of the context's gkv_prefix_bytes calls was asked for
  * returns GKV_ERR_WORKSPACE; the size of `part` itself is not known here: with buffers of several sizes the caller keeps them apart.
  * Both calls can be recorded; the rows are frozen then.  More than 2^30 rows: GKV_ERR_SHAPE.

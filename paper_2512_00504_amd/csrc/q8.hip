@@ -114,7 +114,7 @@ __device__ __forceinline__ void store16(uint16_t* p, size_t stride, const float 
   }
 }
 
-// A workgroup takes 16-row tiles of one unit's K (blockIdx.y even) or V, a 16-byte piece of codes a thread; what it
+// A workgroup takes 16-row tiles of one unit's K or V (blockIdx.z, where both are asked for), a 16-byte piece of codes a thread; what it
 // writes has the format of the cache that d_state describes.
 // ONCE: the codes are read with non-temporal loads (32 x 4 units of 1090 rows 26.4 -> 23.9 us; 1792 of 1151 325 -> 328, so up to 256 MiB of output).
 template <typename T, bool ONCE>

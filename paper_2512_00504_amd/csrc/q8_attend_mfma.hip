@@ -18,7 +18,7 @@
 // trips to memory and instructions: us in a graph, this / the kernel of bf16 or fp32 caches, 4 units of 577 rows 6.4 / 5.6, 128 of 577 7.5 / 8.6, 128
 // of 1100 10.2 / 13.8, 512 of 577 16.0 / 25.1; fp32, D = 64 2 of 72 4.7 / 4.2.  One slice in flight, K of the next asked for as soon as the
 // products with this one are under way (behind them: 861 / 854 us for 18432 units; two slices: 891, 4 of 577 7.0); 4 wavefronts (6: 935, 8: 915);
-// slices of 64 keys at D = 64: 2 of 72 6.25, 128 of 528 8.05 -> 6.3, 25088 of 600 56.6 -> 49.5.
+// slices of 64 keys at D = 64: 2 of 72 6.25, 128 of 528 8.05 -> 6.3, 3584 of 600 56.6 -> 49.5.
 // The newest token's row is quantised by every wavefront for itself while its first slice is on the way (a step's call is
 // one launch), and replaces what the cache holds in its place in the unit's last slice; the workgroup of the first piece stores it.
 #include "e4m3.h"
