@@ -41,6 +41,9 @@ __device__ __forceinline__ uint32_t q8_codes(float a, float b, float c, float d,
   w = __builtin_amdgcn_cvt_pk_fp8_f32(q8_scaled(c, inverse), q8_scaled(d, inverse), w, true);
   return (uint32_t)w;
 }
+// Codes of K meet queries as code * 2^-7 (3.5 at most, exact in bf16 too), and the 2^7 goes to the logit behind the row's scale: a query of up to 2^125
+// times a code of 448 would be infinite where the logit is not.
+constexpr float Q8_K_SHRUNK = 0x1p-7f, Q8_K_GROWN = 0x1p7f;
 // The codes' values.
 __device__ __forceinline__ void q8_values(uint32_t w, float (&x)[4]) {
   const q8_f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);

@@ -160,7 +160,7 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// q . codes of a row of K; `row` and `piece` as q8_k_offset takes them.
+// q . codes of a row of K, for queries that are shrunk (Q8_K_SHRUNK) in their place; `row` and `piece` as q8_k_offset takes them.
 __device__ __forceinline__ float dot_codes(const float* qs, const uint8_t* Kh, int row, int d, int n_tiled) {
   float acc = 0.f;
   for (int p = 0; p < d >> 4; ++p) {
@@ -220,11 +220,11 @@ __global__ __launch_bounds__(NWG * 64) void q8_attend_generic_kernel(GkvDims dm,
     const int head = j * g + hi;
     const size_t row = (size_t)lb * dm.Hq + head;
     const T* qh = (const T*)a.q + row * d;
-    for (int c = lane; c < d; c += 64) qs[c] = Elem<T>::ld(qh + c);
+    for (int c = lane; c < d; c += 64) qs[c] = Elem<T>::ld(qh + c) * Q8_K_SHRUNK;
     wave_sync();
     float mx = GKV_NO_MAX;
     for (int n = lane; n < n_tot; n += 64) {
-      const float z = dot_codes(qs, Kh, n, d, st.n_tiled) * q8_k_scale(scales[n]);
+      const float z = dot_codes(qs, Kh, n, d, st.n_tiled) * q8_k_scale(scales[n]) * Q8_K_GROWN;
       prob[n] = z;
       mx = fmaxf(mx, rounded_product(z, dm.scale_l2_hi));
     }
@@ -289,11 +289,11 @@ __global__ void q8_score_generic_kernel(GkvDims dm, ScoreArgs a) {
     for (int hi = 0; hi < g; ++hi) {
       const T* qh = (const T*)a.qwin + (((size_t)slot * dm.L * dm.B + lb) * dm.Hq + j * g + hi) * d;
       wave_sync();
-      for (int ch = lane; ch < d; ch += 64) qs[ch] = Elem<T>::ld(qh + ch);
+      for (int ch = lane; ch < d; ch += 64) qs[ch] = Elem<T>::ld(qh + ch) * Q8_K_SHRUNK;
       wave_sync();
       float mx = GKV_NO_MAX;
       for (int n = lane; n < n_vis; n += 64) {
-        z[n] = dot_codes(qs, Kh, n, d, st.n_tiled) * q8_k_scale(scales[n]);
+        z[n] = dot_codes(qs, Kh, n, d, st.n_tiled) * q8_k_scale(scales[n]) * Q8_K_GROWN;
         mx = fmaxf(mx, rounded_product(z[n], dm.scale_l2_hi));
       }
       mx = wave_max(mx);

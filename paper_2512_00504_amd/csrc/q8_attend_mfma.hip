@@ -37,14 +37,16 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ u32x4 ld16(const void* p) { return *(const u32x4*)p; }
 __device__ __forceinline__ bf16x8 as_bf16x8(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
-// Two codes of a word's lower or upper half as bf16 numbers.
-__device__ __forceinline__ uint32_t lower(uint32_t w) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+// Two codes of a word's lower or upper half as bf16 numbers, times a power of two.
+__device__ __forceinline__ uint32_t lower(uint32_t w, float times = 1.0f) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, times, false));
 }
-__device__ __forceinline__ uint32_t upper(uint32_t w) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
+__device__ __forceinline__ uint32_t upper(uint32_t w, float times = 1.0f) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, times, true));
 }
-__device__ __forceinline__ u32x4 eight(uint32_t a, uint32_t b) { return u32x4{lower(a), upper(a), lower(b), upper(b)}; }
+__device__ __forceinline__ u32x4 eight_of_k(uint32_t a, uint32_t b) {
+  return u32x4{lower(a, Q8_K_SHRUNK), upper(a, Q8_K_SHRUNK), lower(b, Q8_K_SHRUNK), upper(b, Q8_K_SHRUNK)};
+}
 
 // x as bf16 (P = 1), or as the sum of P bf16 numbers: three hold all of its bits.
 template <int P>
@@ -195,7 +197,7 @@ __device__ __forceinline__ void process(Slice<T, D>& x, Running<D / 16>& st, con
     for (int c = 0; c < G::NL; ++c)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const bf16x8 a = as_bf16x8(eight(x.k[tt][c][2 * h], x.k[tt][c][2 * h + 1]));
+        const bf16x8 a = as_bf16x8(eight_of_k(x.k[tt][c][2 * h], x.k[tt][c][2 * h + 1]));
 #pragma unroll
         for (int p = 0; p < G::QP; ++p) acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, as_bf16x8(q[c][h][p]), acc[tt], 0, 0, 0);
       }
@@ -289,7 +291,7 @@ struct KernelArgs {
   GkvDivisor by_splits, by_hkv, by_iters, by_w;
   int32_t splits, split_iters, Hq, Hkv, g, cap, LB, w, step;
   int32_t has_base, copy_q, write_stats;
-  float scale_hi, scale_lo;
+  float scale_hi, scale_lo;                                // (with Q8_K_GROWN)
   PrefixPart prefix;
 };
 
@@ -546,7 +548,7 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const Q8AttendArgs& a)
   k.splits = a.splits; k.split_iters = a.split_iters;
   k.Hq = dm.Hq; k.Hkv = dm.Hkv; k.g = dm.g; k.cap = dm.cap; k.LB = dm.L * dm.B; k.w = dm.w; k.step = a.step;
   k.has_base = dm.step_base != nullptr; k.copy_q = a.copy_q; k.write_stats = a.write_stats;
-  k.scale_hi = dm.scale_l2_hi; k.scale_lo = dm.scale_l2_lo; k.prefix = a.prefix;
+  k.scale_hi = dm.scale_l2_hi * Q8_K_GROWN; k.scale_lo = dm.scale_l2_lo * Q8_K_GROWN; k.prefix = a.prefix;
   return gkv_launch(ln, q8_attend_mfma_kernel<T, D, NW, OCC, ONCE>, dim3(dm.L * dm.B * dm.Hkv * a.splits), dim3(NW * 64),
                     gkv_q8_attend_mfma_lds(D, dm.g, NW), k);
 }

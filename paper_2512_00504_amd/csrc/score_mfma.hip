@@ -69,17 +69,17 @@ __device__ __forceinline__ void expand(Tile<T, D>& k, const Raw<T, D, true>& raw
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float x[4];
-        q8_values(raw[c][i], x);
-        k[4 * c + i] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+        const q8_f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(raw[c][i], Q8_K_SHRUNK, false);
+        const q8_f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(raw[c][i], Q8_K_SHRUNK, true);
+        k[4 * c + i] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(y[0]), __float_as_uint(y[1])};
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        k[2 * c + i] = u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i], 1.0f, false)),
-                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i], 1.0f, true)),
-                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i + 1], 1.0f, false)),
-                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i + 1], 1.0f, true))};
+        k[2 * c + i] = u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i], Q8_K_SHRUNK, false)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i], Q8_K_SHRUNK, true)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i + 1], Q8_K_SHRUNK, false)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[c][2 * i + 1], Q8_K_SHRUNK, true))};
     }
   }
 }
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
 
   const char* Kh = (const char*)a.K + (size_t)unit * cap * (K8 ? D : G::ROW_BYTES);
   const uint32_t* scales = K8 ? a.scales + (size_t)unit * cap : nullptr;
-  const float hi = dm.scale_l2_hi, lo = dm.scale_l2_lo;
+  const float hi = dm.scale_l2_hi * (K8 ? Q8_K_GROWN : 1.f), lo = dm.scale_l2_lo * (K8 ? Q8_K_GROWN : 1.f);
   // a tile: f(operand, the logits' factor as hi + lo)
   auto load_tile = [&](Raw<T, D, K8>& k, int t) {
     if constexpr (K8) load_k8_tile<T, D, false, true>(k, Kh, scales, t, seq.n_tiled, lane, r, kb);
@@ -698,7 +698,7 @@ __global__ __launch_bounds__(NW * 64, 2) void score_regs_kernel(GkvDims dm, Scor
   if (g0 >= g1) return;
   // a tile: f(operand, the logits' factors of keys 4 kb + e as hi + lo)
   auto opened = [&](const Raw<T, D, K8>& raw, auto f) {
-    const float hi = dm.scale_l2_hi, lo = dm.scale_l2_lo;
+    const float hi = dm.scale_l2_hi * (K8 ? Q8_K_GROWN : 1.f), lo = dm.scale_l2_lo * (K8 ? Q8_K_GROWN : 1.f);
     if constexpr (K8) {
       Tile<T, D> k;
       expand<T, D>(k, raw);
