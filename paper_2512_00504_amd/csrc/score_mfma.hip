@@ -207,13 +207,14 @@ struct ScorePlan {
 };
 
 // Dynamic LDS: q pieces [nt_pass*n_blk][NL][1 KiB]; float row_hi[rows], row_lo[rows]; float sbuf[cap] if
-// use_sbuf; and, when the row statistics are computed here, float2 red_ms[NW][rows].
+// use_sbuf; and, when the row statistics are (or may have to be) computed here, float2 red_ms[NW][rows].
 // HAVE_STATS: a.stats holds (max, sum) of every window row, recorded by the decode kernel.
 // K8: the keys are codes of 8 bits; a key's scale, a power of two, goes into the logits' factor.
 template <typename T, int D, int NW, int KT, bool HAVE_STATS, bool K8>
 __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreArgs a, ScorePlan pl) {
   using G = Geo<T, D>;
   constexpr int NL = G::NL;
+  constexpr bool OWN_LOGITS = HAVE_STATS && K8 && G::F32;    // the recorded statistics are of other roundings of the logits
   a.step = resolve_step(dm, a.step);
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -483,7 +484,8 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
           }
       }
     }
-    if constexpr (!HAVE_STATS) {
+    // the wavefronts' statistics
+    auto combine = [&]() {
       __syncthreads();
       for (int x = tid; x < rows; x += NW * 64) {
         float M = red_ms[x].x;
@@ -498,6 +500,44 @@ __global__ __launch_bounds__(NW * 64) void score_mfma_kernel(GkvDims dm, ScoreAr
         store_offset(x, M, Z);
       }
       __syncthreads();
+    };
+    if constexpr (!HAVE_STATS) combine();
+    if constexpr (OWN_LOGITS) {
+      // Seldom: the recorded statistics are of logits that the decode kernel formed from bf16 parts of the queries, and logits of thousands
+      // are rounded to another number here; the rows' statistics are formed again from these.
+      bool far = false;
+      for (int x = lane; x < rows; x += 64) far |= fabsf(row_hi[x]) >= 0x1p10f && row_hi[x] != -INFINITY;
+      if (__any(far)) {                                      // (all wavefronts see all rows)
+        const int n_tiles = (l + 15) >> 4, n_blocks = nts * pl.n_blk;
+#pragma unroll 1
+        for (int blk = 0; blk < n_blocks; ++blk) {
+          const int seen = cc + k_of(16 * blk + r, nt0);
+          float m = GKV_NO_MAX, sum = 0.f;
+          u32x4 q[NL];
+          load_q(q, blk);
+#pragma unroll 1
+          for (int t = wave; t < n_tiles; t += NW) {
+            Raw<T, D, K8> raw;
+            load_k8_tile<T, D, false, false>(raw, Kh, scales, t, seq.n_tiled, lane, r, kb);
+            Tile<T, D> k;
+            expand<T, D>(k, raw);
+            const f32x4 z = logits<T, NL>(k, q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool unseen = 16 * t + 4 * kb + e > seen;
+              const float scale = unseen ? 1.f : q8_k_scale(raw[D / 64][e]);
+              add_to_stats<true>(unseen ? -INFINITY : z[e], hi * scale, lo * scale, m, sum);
+            }
+          }
+          float M = fmaxf(m, __shfl_xor(m, 16));
+          M = fmaxf(M, __shfl_xor(M, 32));
+          sum *= __builtin_amdgcn_exp2f(m - M);
+          sum += __shfl_xor(sum, 16);
+          sum += __shfl_xor(sum, 32);
+          if (kb == 0) red_ms[wave * rows_pass + 16 * blk + r] = make_float2(M, sum);
+        }
+        combine();
+      }
     }
 
     // ---- scores of this share's candidates ------------------------------------------------------
@@ -1009,7 +1049,7 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const ScoreArgs& a, in
   pl.by_ksplit = gkv_divisor(pl.ksplit);
   const size_t rows = (size_t)pl.nt_pass * pl.n_blk * 16;
   const size_t shmem = rows * G::ROW_BYTES + rows * 8 + (pl.use_sbuf ? 4 * (size_t)dm.cap : 0) +
-                       (a.stats ? 0 : NW * rows * 8);
+                       (a.stats && !(K8 && G::F32) ? 0 : NW * rows * 8);
   auto kern = a.stats ? score_mfma_kernel<T, D, NW, KT, true, K8> : score_mfma_kernel<T, D, NW, KT, false, K8>;
   if (shmem > GKV_LDS_LIMIT) {                             // beyond the default per-workgroup limit: opt in (a CU holds 160 KiB)
     const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)shmem);

@@ -70,3 +70,40 @@ def test_window_score_of_huge_queries(dtype, d, g, params, power):
 @pytest.mark.parametrize("power", [100, 118, 121])
 def test_window_score_of_huge_queries_behind_decode_steps(dtype, d, g, params, power):
     _score_case(dtype, d, g, params, power, True)
+
+
+@pytest.mark.parametrize("d,g", [(64, 4), (128, 2), (64, 9), (128, 16)])
+@pytest.mark.parametrize("power", [5, 12, 21, 40, 100, 118, 121])
+@pytest.mark.parametrize("w", [8, 40])
+def test_fp32_window_score_takes_statistics_of_its_own_logits(d, g, power, w):
+    # The decode step forms logits from bf16 parts of the queries, the score from 32-bit products: two roundings of a logit of 2^power.  Probabilities
+    # are below 1 (and 2^-20) for every size all the same, and a row's sum over all of its keys is 1: with the w newest keys far below, over the
+    # candidates (up to the logits' rounding, 2^(power - 20) and less where they are ordinary).
+    b, s, n, cap = 64, 48, 112, 128
+    st = Q8DecodeState(make_config(1, 1, g, 1, d, b, w, s, cap, "f32"))
+    gen = torch.Generator().manual_seed(power + d)
+    K, V = rows(gen, "f32", 1, 1, 1, cap, d), rows(gen, "f32", 1, 1, 1, cap, d)
+    q = torch.randn(w, 1, 1, 1, d, generator=gen).expand(w, 1, 1, g, d).contiguous()   # one query for all heads: the largest of them is each of them
+    K[..., 0], q[..., 0] = 1.0, 8.0
+    K[0, 0, 0, n - w:, 0] = -1.0                           # the window's own keys: lower by 16 and more
+    K[0, 0, 0, n - w:, 1:] = 0.0
+    q = q * 2.0 ** power
+    t = 2 * w + 3
+    _fill(st, K, V, [n - w], b, since=t - w + 1)
+    for k in range(w):
+        kn, vn = K[:, :, :, n - w + k].contiguous(), V[:, :, :, n - w + k].contiguous()
+        st.attend_decode(q[k].cuda(), kn.cuda(), vn.cuda(), t - w + 1 + k)
+    st.score_window(t)
+    S = st.S[0, 0, 0, :n - w].cpu().double()
+    qw, kv = q[:, 0, 0].double(), values(K[0, 0, 0, :n])
+    ref = score(qw, kv, 1 / math.sqrt(d))
+    off = min(1.0, 2.0 ** (power + 6 - 20))                # logits of up to 2^(power + 6)
+    assert (S <= 1 + 2.0 ** -20).all() and abs(S.sum().item() - ref.sum().item()) <= max(2.0 ** -18, off if power < 10 else 2.0 ** -18), (S.sum(), ref.sum())
+    if power >= 40:
+        assert ((S - ref).abs() <= 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("dtype,d,g,params", [f for f in FORMS[:8] if f[0] == "f32" and not f[3]])
+@pytest.mark.parametrize("power", [100, 118, 121])
+def test_window_score_of_huge_fp32_queries_behind_decode_steps(dtype, d, g, params, power):
+    _score_case(dtype, d, g, params, power, True)
