@@ -11,12 +11,13 @@
 //   by a part of how far that value is from the mean, and not at all where one key dominates or the values are equal.  Error of the result, whose own
 //   rounding makes 1.7e-3: 1.7e-3 to 2.0e-3 with peaked weights (sum of the unrounded ones: 1.9e-3 to 2.4e-3), 2.4e-3 with flat ones.  With the maximum
 //   followed at once, not at a distance of up to 8, peaked 1.7e-3 to 1.8e-3, but 5 to 8% more time (28 layers, 64 sequences x 4000 rows 158 -> 169 us).
+//   Weights as two bf16 numbers: 1.7e-3 with all of them, but half as many products again (there 158 -> 191, 16 x 8000 92 -> 111, 4 x 8000 71.0 -> 72.3).
 // LDS holds a tile's rows as they are, their 16-byte pieces exchanged within the row so that neither kind of read finds two
 // rows in the same banks.
 // Bound: HBM with few rows (28 layers, 4 KV heads, 32000 rows of d = 128, g = 7: 289 us, 6.3 TB/s).  With several hundred the products
 // and the vector unit in turn: 32 keys of 32 rows are 16 products (512 cycles) and 16 x (maximum, fma, exponential, sum, half a
 // conversion), about as many; what a wavefront does of one does not overlap with the other, and three of them on a SIMD overlap little
-// (64 sequences x 16384 rows, g = 5, 4 layers, 8 KV heads 117 us, 0.73 PFLOP/s; counters: products 48% of the time, vector instructions
+// (64 sequences x 16384 rows, g = 5, 4 layers, 8 KV heads 119 us, 0.72 PFLOP/s; counters: products 48% of the time, vector instructions
 // 51%).  Two tiles' logits in turn within a wavefront, which takes the registers of the third: 117 -> 138 us.
 #include "gkv_internal.h"
 
