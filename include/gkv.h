@@ -149,7 +149,7 @@ int64_t gkv_k_offset(const gkv_config* cfg, int32_t row, int32_t channel, int32_
  * ones the matrix-core decode kernel recorded during the window's decode steps; see
  * gkv_score_window), "evict_fuse_select" (default 1: gkv_evict
  * forms the global score at the head of the selection kernel, one launch less per compression;
- * 0 = a launch of its own as in gkv_global_update; same bits either way), "evict_fuse_global" (1 = never
+ * 0 = a launch of its own as in gkv_global_update; same bits either way; gkv_q8_evict always forms it there), "evict_fuse_global" (1 = never
  * a launch of its own, whatever "evict_fuse_select" says). */
 gkv_status gkv_set_param(gkv_ctx* ctx, const char* name, int32_t value);
 

@@ -294,7 +294,7 @@ class Q8DecodeState(DecodeState):
                 cuts[-2] = (cuts[-3] + n) // 2
             self._part_ctx = [(lo, self.ctx.part(hi - lo)) for lo, hi in zip(cuts, cuts[1:])]
             most = max(hi - lo for lo, hi in zip(cuts, cuts[1:]))
-            self._K_part = torch.zeros(most, *self.K8.shape[2:], dtype=self.qwin.dtype, device=self.device)
+            self._K_part = torch.empty(most, *self.K8.shape[2:], dtype=self.qwin.dtype, device=self.device)
         return self._part_ctx
 
     def redundancy_combine(self, step, lam, tau, n_recent, eps=1e-8):

@@ -97,6 +97,22 @@ def test_decode_ends_of_long_and_of_many_units(cls, dtype, d, g):
         _case(cls, dtype, d, g, [i % 96 for i in range(B)], None, cap=96, hkv=3)
 
 
+@pytest.mark.parametrize("cls", [DecodeState, Q8DecodeState])
+@pytest.mark.parametrize("params", [{"attend_tile": 32}, {"attend_waves": 16}, {"attend_tile": 32, "attend_splits": 3}])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("f32", 128)])
+def test_ends_with_the_other_knobs(cls, params, dtype, d):
+    for P in (None, 1, 777):
+        _case(cls, dtype, d, 2, [200, 17, 1000, 0, 32, 1], P, cap=1024, n_tiled=512, params=params)
+
+
+@pytest.mark.parametrize("cls", [DecodeState, Q8DecodeState])
+@pytest.mark.parametrize("dtype,d,g", [("bf16", 128, 7), ("f32", 64, 2), ("bf16", 64, 3)])
+def test_cut_units_joined_with_many_pieces(cls, dtype, d, g):
+    for P in (2049, 20000):
+        _case(cls, dtype, d, g, [3000, 900], P, cap=3008, n_tiled=1024)
+        _case(cls, dtype, d, g, [2000], P, cap=3008, n_tiled=0, hkv=1, append=False)
+
+
 # ---- larger than the memory-side cache: what is read once is asked for in another way ----------------
 @pytest.mark.parametrize("dtype,d,g,B,P", [("bf16", 128, 7, 4, 33000), ("bf16", 128, 7, 8, 33001), ("bf16", 128, 7, 16, 32999), ("bf16", 64, 3, 10, 65999),
                                            ("bf16", 64, 4, 16, 66000), ("bf16", 64, 4, 32, 65970), ("f32", 128, 5, 2, 16500), ("f32", 128, 5, 12, 16501),

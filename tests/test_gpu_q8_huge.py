@@ -5,10 +5,11 @@ import pytest
 import torch
 
 from paper_2512_00504_amd import make_config
-from paper_2512_00504_amd.state import Q8DecodeState
+from paper_2512_00504_amd.state import DecodeState, Q8DecodeState, SharedPrefix
 
 from planted import DT, rows, score
 from q8_reference import values
+from test_gpu_prefix import _own
 from test_gpu_q8 import _fill
 
 pytestmark = pytest.mark.gpu
@@ -107,3 +108,26 @@ def test_fp32_window_score_takes_statistics_of_its_own_logits(d, g, power, w):
 @pytest.mark.parametrize("power", [100, 118, 121])
 def test_window_score_of_huge_fp32_queries_behind_decode_steps(dtype, d, g, params, power):
     _score_case(dtype, d, g, params, power, True)
+
+
+@pytest.mark.parametrize("cls", [DecodeState, Q8DecodeState])
+@pytest.mark.parametrize("dtype,d,g,params", FORMS)
+@pytest.mark.parametrize("power", [100, 118, 121])
+@pytest.mark.parametrize("P", [33, 3000])
+def test_the_largest_logit_of_prefix_and_own_rows_takes_all(cls, dtype, d, g, params, power, P):
+    lens, cap = [40, 0, 200, 255], 256
+    st = cls(make_config(1, 4, 2 * g, 2, d, 64, 8, 16, cap, dtype), params=params)
+    gen = torch.Generator().manual_seed(power + P)
+    K, V = rows(gen, dtype, 1, 4, 2, cap, d), rows(gen, dtype, 1, 4, 2, cap, d)
+    q = rows(gen, dtype, 1, 4, 2 * g, d) * 2.0 ** power
+    pk, pv = rows(gen, dtype, 1, 2, P, d), rows(gen, dtype, 1, 2, P, d)
+    pk[:, :, P - 1] *= 2                                   # (so that some heads have it in the last piece)
+    _own(st, K, V, lens, 48)
+    out = st.attend_decode(q.cuda(), None, None, 5, prefix=SharedPrefix(st, pk.cuda(), pv.cuda())).cpu().double()
+    half = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -23
+    held = values if cls is Q8DecodeState else lambda x: x.double()
+    for i, n in enumerate(lens):
+        for j in range(2):
+            k, v = torch.cat([held(K[0, i, j, :n]), pk[0, j].double()]), torch.cat([held(V[0, i, j, :n]), pv[0, j].double()])
+            best = v[(q[0, i, j * g:(j + 1) * g].double() @ k.T).argmax(dim=-1)]
+            assert ((out[0, i, j * g:(j + 1) * g] - best).abs() <= half * best.abs()).all(), (i, j)

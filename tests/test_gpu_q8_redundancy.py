@@ -103,3 +103,19 @@ def test_profile_counts_the_parts():
     assert ms > 0 and calls == 2 * len(st._parts()) == 6
     st.ctx.profile_reset()
     assert st.ctx.profile_read("redundancy") == (0.0, 0)
+
+
+def test_a_first_call_that_is_recorded():
+    st, ref = _pair(2, 80, 4, 1, 128, "bf16", 40, 8, 16, 64)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        st.redundancy_combine(27, 0.7, 0.3, 8)
+    ref.redundancy_combine(27, 0.7, 0.3, 8)
+    for _ in range(3):
+        for f in (graph.replay, lambda: st.redundancy_combine(27, 0.7, 0.3, 8)):
+            st.R.fill_(-7.0); st.F_sel.fill_(-7.0)
+            torch.cuda.synchronize()
+            f()
+            torch.cuda.synchronize()
+            assert torch.equal(st.R, ref.R) and torch.equal(st.F_sel, ref.F_sel)
