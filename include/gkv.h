@@ -387,6 +387,84 @@ gkv_status gkv_attend_decode_prefix(gkv_ctx* ctx, const void* q, const void* k_n
                                     const int32_t* d_state, int32_t len_max_host, const void* part, void* out,
                                     void* workspace, void* stream);
 
+/*
+ * ---- Rotary positions ---------------------------------------------------------------------------
+ * Pair p of a head's first `dim` channels, (x1, x2) = channels (p, p + dim/2) in the half layout and (2p, 2p + 1) in the
+ * interleaved one, is turned by its token's position:
+ *     y1 = m (x1 cos a - x2 sin a),  y2 = m (x1 sin a + x2 cos a),  a = position * freq[p] radians,  m = amplitude.
+ * The other channels stay.  The angle is formed and reduced in 64 bits, so far positions are as good as near ones.
+ *   freq       device memory, dim/2 doubles, the caller's, 8-byte aligned.  It may be rewritten between calls (lengths that scale with the context).
+ *   dim        even, 2 .. d.
+ *
+ * gkv_rotary_frequencies (host only) fills freq[0 .. dim/2) (host memory) and *amplitude from a base, f_p = base^(-2p/dim), scaled for contexts
+ * that are `factor` times as long as those trained on:
+ *   NONE      f_p                                         (factor is not used, but has to be above 0)
+ *   LINEAR    f_p / factor
+ *   BASE      f_p of the base times factor^(dim / (dim - 2)), which leaves the first pair and divides the last by factor (dim = 2: f_p)
+ *   BY_PARTS  (arXiv 2309.00071) pairs of at least `high` turns over trained_length keep f_p, those of at most `low` have f_p / factor, and between the
+ *             two pairs (rounded outwards) the share changes linearly with p; amplitude 0.1 ln(factor) + 1 where factor > 1
+ *   SMOOTH    the same with the share linear in the number of turns, and no rounding; amplitude 1
+ * amplitude is 1 where nothing else is said.  base > 1; trained_length > 0 and 0 < low < high for the last two.
+ */
+typedef enum { GKV_ROTARY_HALF = 0, GKV_ROTARY_INTERLEAVED = 1 } gkv_rotary_layout;
+typedef enum { GKV_ROTARY_NONE = 0, GKV_ROTARY_LINEAR = 1, GKV_ROTARY_BASE = 2, GKV_ROTARY_BY_PARTS = 3, GKV_ROTARY_SMOOTH = 4 } gkv_rotary_scaling;
+gkv_status gkv_rotary_frequencies(int32_t dim, double base, int32_t scaling, double factor, double trained_length,
+                                  double low, double high, double* freq, float* amplitude);
+
+/* The queries and keys of `tokens` tokens of every layer turned (decode step: tokens = batch).  q, k: [L,tokens,heads,d] with q_stride, k_stride
+ * elements from one token to the next (0: side by side, heads * d) and tokens times that from layer to layer, so slices of one projection's
+ * output can be given as they are.  q_out, k_out: [L,tokens,heads,d] side by side.  Either of q and k may be NULL, and its output then too.
+ * In place (q_out == q) where rows lie side by side; other overlaps are not allowed.
+ * positions: device, int32 [tokens], the same in every layer, any value; NULL: `step` for every token (relative to the step base if one is set).
+ * q_out may be the ring slot of the step, whose gkv_attend_decode then copies nothing.
+ * transposed = 1: by -a instead of a, which takes the gradient of the outputs to that of the inputs.
+ * Rows and strides of whole 16-byte pieces, with dim/2 (interleaved: dim) a whole number of them, are fastest.  L * tokens at most 2^30. */
+gkv_status gkv_rotate(gkv_ctx* ctx, const void* q, int32_t q_stride, const void* k, int32_t k_stride, int32_t tokens,
+                      const int32_t* positions, int32_t step, const double* freq, int32_t dim, int32_t layout,
+                      float amplitude, int32_t transposed, void* q_out, void* k_out, void* stream);
+
+/*
+ * ---- Paged cache --------------------------------------------------------------------------------
+ * A cache that is not capped: every row is kept, and sequences grow page by page.  For layers that are not compressed, and full attention to
+ * compare with.  Budget, window, interval and capacity of the configuration mean nothing here.
+ *   K, V        [L,n_pages,h_kv,page_rows,d] of config.dtype; a page is page_rows rows of every KV head.  page_rows of a multiple of 16 is fastest.
+ *   page_table  [B,table_width] int32: row n of sequence i is row n % page_rows of page page_table[i, n / page_rows], in every layer.  Sequences may
+ *               share pages that none of them appends to.  Entries behind a sequence's length are not looked at.  A row whose entry is outside
+ *               [0, n_pages) is not there: not stored, and not attended to.
+ *   d_len       [B] int32: rows of each sequence, WITH the tokens that this step appends; gkv_paged_advance counts them before the
+ *               first layer's calls.  Above table_width * page_rows counts as that, below 0 as 0.
+ * table_width * page_rows at most 2^30 (else GKV_ERR_SHAPE).  All calls can be recorded; table and lengths are read when they run.
+ *
+ * gkv_paged_advance: sequence i grows by d_start[i+1] - d_start[i] rows, from 0 if d_len[i] was below; d_start == NULL: by one where d_len[i] >= 0 (a
+ * sequence of length -1 takes no part).
+ */
+gkv_status gkv_paged_advance(gkv_ctx* ctx, int32_t* d_len, const int32_t* d_start, void* stream);
+
+/* New tokens' keys and values into their sequences' pages.  Tokens are packed: sequence i's are d_start[i] .. d_start[i+1]-1 (device, int32 [B+1],
+ * ascending), n_i of them, and become its rows d_len[i]-n_i .. d_len[i]-1.  d_start == NULL: one token for each sequence, tokens = B.
+ * k, v (and q): [L,tokens,heads,d] with strides as gkv_rotate takes them.  With freq, keys are turned on the way, by positions[token] (device, int32 [tokens])
+ * or, where that is NULL, by the row they become; and so are queries, if given, to q_out [L,tokens,h_q,d] (in place as in gkv_rotate).  freq == NULL: keys are stored
+ * as they are, dim, layout and amplitude mean nothing, and q has to be NULL.
+ * Tokens at or beyond d_start[B], before d_start[0], or whose row would be below 0 are not looked at: their q_out stays as it is. */
+gkv_status gkv_paged_append(gkv_ctx* ctx, const void* q, int32_t q_stride, const void* k, int32_t k_stride, const void* v,
+                            int32_t v_stride, int32_t tokens, const int32_t* d_start, const int32_t* d_len,
+                            const int32_t* positions, const double* freq, int32_t dim, int32_t layout, float amplitude,
+                            const int32_t* page_table, int32_t table_width, int32_t page_rows, int32_t n_pages,
+                            void* K, void* V, void* q_out, void* stream);
+
+/* One new token's queries over each sequence's rows: out[i] = softmax(q[i] . K[i/g]^T * scale) V[i/g] over rows [0, d_len).  q, out [L,B,h_q,d].
+ * A sequence without rows gets zeros.  Long sequences are cut into pieces that the same launch joins.
+ * len_max_host: host bound with every d_len <= len_max_host <= table_width * page_rows (else GKV_ERR_OVERFLOW); it sizes the launch and does not show
+ * in the result.
+ * workspace: device memory of gkv_paged_workspace_bytes() bytes, 16-byte aligned, zeroed once by the caller; calls that may overlap in time (also replays
+ * of recorded ones) need one each.  gkv_workspace_bytes' is another.
+ * Logits, weights, sums and outputs are formed in 32 bits; with bf16 the matrix-core kernel takes a weight as the sum of two bf16 numbers for its product
+ * with V (2^-16 of it). */
+gkv_status gkv_paged_workspace_bytes(gkv_ctx* ctx, size_t* out_bytes);
+gkv_status gkv_paged_attend_decode(gkv_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* page_table,
+                                   int32_t table_width, int32_t page_rows, int32_t n_pages, const int32_t* d_len,
+                                   int32_t len_max_host, void* out, void* workspace, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

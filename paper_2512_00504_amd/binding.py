@@ -32,7 +32,10 @@ EXPORTS = [
     "gkv_evict_static", "gkv_set_step_base", "gkv_advance_step_base",
     "gkv_q8_store_prompt", "gkv_q8_read", "gkv_q8_attend_decode", "gkv_q8_score_window", "gkv_q8_compact", "gkv_q8_evict",
     "gkv_prefix_bytes", "gkv_prefix_attend", "gkv_attend_decode_prefix",
+    "gkv_rotary_frequencies", "gkv_rotate", "gkv_paged_append", "gkv_paged_advance", "gkv_paged_workspace_bytes", "gkv_paged_attend_decode",
 ]
+ROTARY_LAYOUT = {"half": 0, "interleaved": 1}
+ROTARY_SCALING = {"none": 0, "linear": 1, "base": 2, "by_parts": 3, "smooth": 4}
 
 
 class GkvConfig(ctypes.Structure):
@@ -92,6 +95,12 @@ def load_library():
     lib.gkv_prefix_bytes.argtypes = [vp, i32, POINTER(c_size_t)]
     lib.gkv_prefix_attend.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, vp]
     lib.gkv_attend_decode_prefix.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp]
+    lib.gkv_rotary_frequencies.argtypes = [i32, c_double, i32, c_double, c_double, c_double, c_double, vp, POINTER(c_float)]
+    lib.gkv_rotate.argtypes = [vp, vp, i32, vp, i32, i32, vp, i32, vp, i32, i32, c_float, i32, vp, vp, vp]
+    lib.gkv_paged_advance.argtypes = [vp, vp, vp, vp]
+    lib.gkv_paged_append.argtypes = [vp, vp, i32, vp, i32, vp, i32, i32, vp, vp, vp, vp, i32, i32, c_float, vp, i32, i32, i32, vp, vp, vp, vp]
+    lib.gkv_paged_workspace_bytes.argtypes = [vp, POINTER(c_size_t)]
+    lib.gkv_paged_attend_decode.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp]
     lib.gkv_profile_enable.argtypes = [vp, i32]
     lib.gkv_profile_read.argtypes = [vp, i32, POINTER(c_double), POINTER(c_int64)]
     lib.gkv_profile_reset.argtypes = [vp]
@@ -121,12 +130,50 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _ptr_here(t, contiguous=True):
+    """The same, of the current device; an address stays one."""
+    if t is None or isinstance(t, int):
+        return t
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"gkv: a tensor is on {t.device}, which is not the current GPU")
+    return _ptr(t) if contiguous else t.data_ptr()
+
+
 def _stream():
     """The raw handle of the current device's current stream.  A decode step is one call of a few
     microseconds of GPU time: building a torch.cuda.Stream object only to read its handle, and a
     c_void_p per argument, cost about a third of the call."""
     import torch
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def rotary_frequencies(dim, base=10000.0, scaling="none", factor=1.0, trained_length=0.0, low=1.0, high=32.0):
+    """Radians a position of each pair of channels, and what cosines and sines are multiplied by (gkv_rotary_frequencies)."""
+    lib = load_library()
+    if not 2 <= dim < 1 << 16:
+        raise GkvError(1, "gkv_rotary_frequencies")
+    freq, amplitude = (c_double * (dim // 2))(), c_float()
+    st = lib.gkv_rotary_frequencies(dim, base, ROTARY_SCALING[scaling] if isinstance(scaling, str) else int(scaling), factor,
+                                    trained_length, low, high, freq, byref(amplitude))
+    if st != 0:
+        raise GkvError(st, "gkv_rotary_frequencies")
+    return list(freq), amplitude.value
+
+
+class Rotary:
+    """Rotary positions of heads' first `dim` channels: frequencies on the device, layout ("half" or "interleaved") and amplitude.
+    freq (float64 [dim/2]) may be rewritten in place, or given instead of what base and scaling say."""
+
+    def __init__(self, dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained_length=0.0, low=1.0, high=32.0,
+                 device="cuda:0", freq=None, amplitude=None):
+        import torch
+        values, own = rotary_frequencies(dim, base, scaling, factor, trained_length, low, high)
+        self.dim, self.layout = dim, ROTARY_LAYOUT[layout] if isinstance(layout, str) else int(layout)
+        self.amplitude = own if amplitude is None else float(amplitude)
+        self.freq = torch.tensor(values, dtype=torch.float64).to(device) if freq is None else freq.to(device, torch.float64).contiguous()
+        if self.freq.shape != (dim // 2,):
+            raise ValueError(f"gkv: freq has to be [{dim // 2}]")
 
 
 _call = None
@@ -171,6 +218,8 @@ class Context:
         self._handle = h.value
         self._call = _load_call()
         self._params, self._step_base, self._profiled, self._parts = {}, None, False, {}
+        import torch
+        self._dtype, self._int32, self._paged_bytes = (torch.float32, torch.bfloat16)[cfg.dtype], torch.int32, None
         self._prefix_bytes, self._prefix_rows = {}, -1       # rows -> size of a buffer for them; the most rows asked for
 
     def part(self, sequences: int) -> "Context":
@@ -375,6 +424,118 @@ class Context:
                                                    _ptr(workspace), _stream())
         if st:
             raise GkvError(st, "gkv_attend_decode_prefix")
+
+    def _heads(self, t, tokens, heads, what, apart=True):
+        """A tensor [L, tokens, heads, d] as the calls take it: itself and 0, or, where tokens lie apart, its address and the elements between them."""
+        if t is None:
+            return None, 0
+        L, d = self.cfg.n_layers, self.cfg.head_dim
+        if t.shape != (L, tokens, heads, d) or t.dtype is not self._dtype:
+            raise ValueError(f"gkv: {what} has to be [{L}, {tokens}, {heads}, {d}] of {self._dtype}, not {list(t.shape)} of {t.dtype}")
+        if t.is_contiguous():
+            return t, 0
+        sl, st, sh, sd = t.stride()
+        stride = st if tokens > 1 else sl
+        if (not apart or (sd != 1 and d > 1) or (sh != d and heads > 1) or (L > 1 and sl != stride * tokens)
+                or not heads * d <= stride < 1 << 31):
+            raise ValueError(f"gkv: {what}'s heads have to lie side by side and its layers one behind the other" if apart
+                             else f"gkv: {what} must be contiguous")
+        _ptr_here(t, False)
+        return t.data_ptr(), stride
+
+    def _pages(self, page_table, d_len, K, V):
+        """Shapes of a paged cache: pages of a sequence, rows of a page, pages."""
+        cfg = self.cfg
+        if K.dim() != 5 or (K.shape[0], K.shape[2], K.shape[4]) != (cfg.n_layers, cfg.n_kv_heads, cfg.head_dim) or V.shape != K.shape:
+            raise ValueError(f"gkv: K and V have to be [{cfg.n_layers}, pages, {cfg.n_kv_heads}, rows, {cfg.head_dim}]")
+        if K.dtype is not self._dtype or V.dtype is not self._dtype:
+            raise ValueError(f"gkv: K and V have to be {self._dtype}")
+        if page_table.dim() != 2:
+            raise ValueError("gkv: page_table has to be [B, pages of a sequence]")
+        self._ints(page_table, (cfg.batch, page_table.shape[1]), "page_table")
+        self._ints(d_len, (cfg.batch,), "d_len")
+        return page_table.shape[1], K.shape[3], K.shape[1]
+
+    def _ints(self, t, shape, what):
+        if t.shape != shape or t.dtype is not self._int32:
+            raise ValueError(f"gkv: {what} has to be int32 {list(shape)}, not {t.dtype} {list(t.shape)}")
+
+    # rotary positions: q, k [L, tokens, heads, d], slices of one projection's output too; rotary: a Rotary
+    def rotate(self, q, k, positions, step, rotary, q_out, k_out, transposed=False):
+        cfg = self.cfg
+        tokens = (k if q is None else q).shape[1]
+        (q, qs), (k, ks) = self._heads(q, tokens, cfg.n_q_heads, "q"), self._heads(k, tokens, cfg.n_kv_heads, "k")
+        q_out, _ = self._heads(q_out, tokens, cfg.n_q_heads, "q_out", False)
+        k_out, _ = self._heads(k_out, tokens, cfg.n_kv_heads, "k_out", False)
+        if positions is not None:
+            self._ints(positions, (tokens,), "positions")
+        if tokens == 0:
+            return
+        r = rotary
+        st = self._call.gkv_rotate(self._handle, q, qs, k, ks, tokens, positions, step, r.freq, r.dim, r.layout, r.amplitude, int(transposed),
+                                   q_out, k_out)
+        if st is None:
+            st = self.lib.gkv_rotate(self.h, _ptr_here(q), qs, _ptr_here(k), ks, tokens, _ptr_here(positions), step, _ptr_here(r.freq), r.dim,
+                                     r.layout, r.amplitude, int(transposed), _ptr_here(q_out), _ptr_here(k_out), _stream())
+        if st:
+            raise GkvError(st, "gkv_rotate")
+
+    # paged cache: K, V [L, n_pages, h_kv, page_rows, d], page_table int32 [B, table_width], d_len int32 [B]
+    def paged_advance(self, d_len, d_start):
+        self._ints(d_len, (self.cfg.batch,), "d_len")
+        if d_start is not None:
+            self._ints(d_start, (self.cfg.batch + 1,), "d_start")
+        st = self._call.gkv_paged_advance(self._handle, d_len, d_start)
+        if st is None:
+            st = self.lib.gkv_paged_advance(self.h, _ptr_here(d_len), _ptr_here(d_start), _stream())
+        if st:
+            raise GkvError(st, "gkv_paged_advance")
+
+    def paged_append(self, q, k, v, d_start, d_len, positions, rotary, page_table, K, V, q_out):
+        """rotary: a Rotary, or None where keys are turned already (q and q_out are None then)."""
+        cfg = self.cfg
+        tokens = k.shape[1]
+        (q, qs), (k, ks), (v, vs) = (self._heads(q, tokens, cfg.n_q_heads, "q"), self._heads(k, tokens, cfg.n_kv_heads, "k"),
+                                     self._heads(v, tokens, cfg.n_kv_heads, "v"))
+        q_out, _ = self._heads(q_out, tokens, cfg.n_q_heads, "q_out", False)
+        if d_start is not None:
+            self._ints(d_start, (cfg.batch + 1,), "d_start")
+        if positions is not None:
+            self._ints(positions, (tokens,), "positions")
+        width, rows, pages = self._pages(page_table, d_len, K, V)
+        if tokens == 0:
+            return
+        freq, dim, layout, amplitude = (None, 0, 0, 1.0) if rotary is None else (rotary.freq, rotary.dim, rotary.layout, rotary.amplitude)
+        st = self._call.gkv_paged_append(self._handle, q, qs, k, ks, v, vs, tokens, d_start, d_len, positions, freq, dim, layout, amplitude,
+                                         page_table, width, rows, pages, K, V, q_out)
+        if st is None:
+            st = self.lib.gkv_paged_append(self.h, _ptr_here(q), qs, _ptr_here(k), ks, _ptr_here(v), vs, tokens, _ptr_here(d_start),
+                                           _ptr_here(d_len), _ptr_here(positions), _ptr_here(freq), dim, layout, amplitude,
+                                           _ptr_here(page_table), width, rows, pages, _ptr_here(K), _ptr_here(V), _ptr_here(q_out), _stream())
+        if st:
+            raise GkvError(st, "gkv_paged_append")
+
+    def paged_workspace_bytes(self) -> int:
+        if self._paged_bytes is None:
+            n = c_size_t()
+            self._check(self.lib.gkv_paged_workspace_bytes(self.h, byref(n)), "gkv_paged_workspace_bytes")
+            self._paged_bytes = n.value
+        return self._paged_bytes
+
+    def paged_attend_decode(self, q, K, V, page_table, d_len, len_max_host, out, workspace):
+        """Refuses a workspace that is too small, which the C call cannot tell."""
+        cfg = self.cfg
+        if workspace is not None and workspace.numel() * workspace.element_size() < self.paged_workspace_bytes():
+            raise GkvError(GKV_ERR_WORKSPACE, "gkv_paged_attend_decode")
+        q, _ = self._heads(q, cfg.batch, cfg.n_q_heads, "q", False)
+        out, _ = self._heads(out, cfg.batch, cfg.n_q_heads, "out", False)
+        width, rows, pages = self._pages(page_table, d_len, K, V)
+        st = self._call.gkv_paged_attend_decode(self._handle, q, K, V, page_table, width, rows, pages, d_len, len_max_host, out, workspace)
+        if st is None:
+            st = self.lib.gkv_paged_attend_decode(self.h, _ptr_here(q), _ptr_here(K), _ptr_here(V), _ptr_here(page_table), width, rows, pages,
+                                                  _ptr_here(d_len), len_max_host, _ptr_here(out), _ptr_here(workspace), _stream())
+        if st:
+            raise GkvError(st, "gkv_paged_attend_decode")
 
     def profile_enable(self, on: bool):
         self._check(self.lib.gkv_profile_enable(self.h, int(on)), "gkv_profile_enable")

@@ -835,6 +835,136 @@ extern "C" gkv_status gkv_prefix_attend(gkv_ctx* ctx, const void* q, const void*
                          : gkv_launch_prefix_generic(ln, d, ctx->cfg.dtype, a));
 }
 
+// ---- rotary positions, paged caches ------------------------------------------------------------------
+extern "C" gkv_status gkv_rotary_frequencies(int32_t dim, double base, int32_t scaling, double factor, double trained_length,
+                                             double low, double high, double* freq, float* amplitude) {
+  if (!freq || !amplitude || dim < 2 || dim % 2 != 0 || !(base > 1.0) || isinf(base) || !(factor > 0.0) || isinf(factor)) return GKV_ERR_INVALID_ARG;
+  if (scaling < GKV_ROTARY_NONE || scaling > GKV_ROTARY_SMOOTH) return GKV_ERR_INVALID_ARG;
+  const bool by_turns = scaling == GKV_ROTARY_BY_PARTS || scaling == GKV_ROTARY_SMOOTH;
+  if (by_turns && (!(trained_length > 0.0) || isinf(trained_length) || !(low > 0.0) || !(high > low) || isinf(high))) return GKV_ERR_INVALID_ARG;
+  constexpr double TURN = 6.283185307179586476925;
+  if (scaling == GKV_ROTARY_BASE && dim > 2) base *= pow(factor, dim / (dim - 2.0));
+  double first = 0, last = 0;
+  if (scaling == GKV_ROTARY_BY_PARTS) {
+    auto pair = [&](double turns) { return dim * log(trained_length / (turns * TURN)) / (2.0 * log(base)); };
+    first = fmax(floor(pair(high)), 0.0);
+    last = fmin(ceil(pair(low)), dim - 1.0);
+  }
+  for (int32_t p = 0; p < dim / 2; ++p) {
+    const double f = pow(base, -2.0 * p / dim);
+    double keep = 1.0;                                     // share of the pair's own frequency, beside f / factor
+    if (scaling == GKV_ROTARY_LINEAR) keep = 0.0;
+    if (scaling == GKV_ROTARY_BY_PARTS) keep = 1.0 - fmin(1.0, fmax(0.0, (p - first) / fmax(last - first, 0.001)));
+    if (scaling == GKV_ROTARY_SMOOTH) keep = fmin(1.0, fmax(0.0, (trained_length * f / TURN - low) / (high - low)));
+    freq[p] = keep == 1.0 ? f : f / factor * (1.0 - keep) + f * keep;
+  }
+  *amplitude = scaling == GKV_ROTARY_BY_PARTS && factor > 1.0 ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+  return GKV_OK;
+}
+
+static gkv_status check_rotary(const gkv_ctx* ctx, const GkvRotary& r) {
+  if (r.dim < 2 || r.dim % 2 != 0 || r.dim > ctx->dims.d || ((uintptr_t)r.freq & 7) != 0) return GKV_ERR_INVALID_ARG;
+  if (r.layout != GKV_ROTARY_HALF && r.layout != GKV_ROTARY_INTERLEAVED) return GKV_ERR_INVALID_ARG;
+  return isfinite(r.amplitude) ? GKV_OK : GKV_ERR_INVALID_ARG;
+}
+// Elements between tokens; 0 stands for rows side by side.
+static bool row_stride(int32_t given, int32_t heads, int32_t d, int64_t* out) {
+  *out = given == 0 ? (int64_t)heads * d : given;
+  return *out >= (int64_t)heads * d;
+}
+
+extern "C" gkv_status gkv_rotate(gkv_ctx* ctx, const void* q, int32_t q_stride, const void* k, int32_t k_stride, int32_t tokens,
+                                 const int32_t* positions, int32_t step, const double* freq, int32_t dim, int32_t layout,
+                                 float amplitude, int32_t transposed, void* q_out, void* k_out, void* stream) {
+  if (!ctx || (!q && !k) || (q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr) || !freq || tokens < 0 || step < 0)
+    return GKV_ERR_INVALID_ARG;
+  RotateArgs a{q, k, nullptr, 0, 0, 0, tokens, positions, step, {freq, dim, layout, amplitude, transposed != 0}, q_out, k_out};
+  const GkvDims& d = ctx->dims;
+  const gkv_status st = check_rotary(ctx, a.rotary);
+  if (st != GKV_OK) return st;
+  if (!row_stride(q_stride, d.Hq, d.d, &a.q_stride) || !row_stride(k_stride, d.Hkv, d.d, &a.k_stride)) return GKV_ERR_INVALID_ARG;
+  if ((q && q == q_out && a.q_stride != (int64_t)d.Hq * d.d) || (k && k == k_out && a.k_stride != (int64_t)d.Hkv * d.d)) return GKV_ERR_INVALID_ARG;
+  if ((int64_t)d.L * tokens > GKV_MOST_ROWS) return GKV_ERR_SHAPE;
+  GkvLaunch ln{ctx, -1, (hipStream_t)stream};
+  return hip_status(gkv_launch_rotate(ln, d, ctx->cfg.dtype, a));
+}
+
+static gkv_status check_pages(const int32_t* table, int32_t width, int32_t page_rows, int32_t n_pages) {
+  if (!table || width < 1 || page_rows < 1 || n_pages < 1) return GKV_ERR_INVALID_ARG;
+  return (int64_t)width * page_rows <= GKV_MOST_ROWS ? GKV_OK : GKV_ERR_SHAPE;
+}
+
+extern "C" gkv_status gkv_paged_append(gkv_ctx* ctx, const void* q, int32_t q_stride, const void* k, int32_t k_stride, const void* v,
+                                       int32_t v_stride, int32_t tokens, const int32_t* d_start, const int32_t* d_len,
+                                       const int32_t* positions, const double* freq, int32_t dim, int32_t layout, float amplitude,
+                                       const int32_t* page_table, int32_t table_width, int32_t page_rows, int32_t n_pages,
+                                       void* K, void* V, void* q_out, void* stream) {
+  if (!ctx || !k || !v || !d_len || !K || !V || (q != nullptr) != (q_out != nullptr) || tokens < 0 || (q && !freq)) return GKV_ERR_INVALID_ARG;
+  const GkvDims& d = ctx->dims;
+  if (!d_start && tokens != d.B) return GKV_ERR_INVALID_ARG;
+  AppendArgs a{{q, k, v, 0, 0, 0, tokens, positions, 0, {freq, dim, layout, amplitude, 0}, q_out, nullptr}, d_start, d_len,
+               {page_table, table_width, page_rows, n_pages, {}}, K, V};
+  gkv_status st = check_pages(page_table, table_width, page_rows, n_pages);
+  if (st == GKV_OK && freq) st = check_rotary(ctx, a.in.rotary);
+  if (st != GKV_OK) return st;
+  if (!freq) a.in.rotary = GkvRotary{nullptr, 0, GKV_ROTARY_HALF, 1.f, 0};
+  if (!row_stride(q_stride, d.Hq, d.d, &a.in.q_stride) || !row_stride(k_stride, d.Hkv, d.d, &a.in.k_stride) ||
+      !row_stride(v_stride, d.Hkv, d.d, &a.in.v_stride) || (q && q == q_out && a.in.q_stride != (int64_t)d.Hq * d.d))
+    return GKV_ERR_INVALID_ARG;
+  if ((int64_t)d.L * tokens > GKV_MOST_ROWS) return GKV_ERR_SHAPE;
+  a.pages.by_rows = gkv_divisor(page_rows);
+  GkvLaunch ln{ctx, -1, (hipStream_t)stream};
+  return hip_status(gkv_launch_paged_append(ln, d, ctx->cfg.dtype, a));
+}
+
+extern "C" gkv_status gkv_paged_advance(gkv_ctx* ctx, int32_t* d_len, const int32_t* d_start, void* stream) {
+  if (!ctx || !d_len) return GKV_ERR_INVALID_ARG;
+  GkvLaunch ln{ctx, -1, (hipStream_t)stream};
+  return hip_status(gkv_launch_paged_advance(ln, ctx->dims, d_len, d_start));
+}
+
+// Pieces of a unit there is room for, and slices of 16 rows a piece has at least.  By the configuration alone: the same call gives the same bits
+// whatever bound of the lengths it comes with.
+struct PagedPlan { int32_t most, iters; };
+static PagedPlan paged_plan(const gkv_ctx* ctx) {
+  const GkvDims& d = ctx->dims;
+  const int64_t units = (int64_t)d.L * d.B * d.Hkv, of_one = (int64_t)d.L * d.Hkv;
+  int64_t most = 512 / of_one;
+  if (most > 32768 / units) most = 32768 / units;
+  return PagedPlan{(int32_t)(most < 1 ? 1 : most > 128 ? 128 : most), units >= 512 ? 64 : 16};
+}
+static size_t paged_tickets_bytes(const GkvDims& d) { return gkv_align256(sizeof(int32_t) * GKV_TICKETS * (size_t)d.L * d.B * d.Hkv); }
+
+extern "C" gkv_status gkv_paged_workspace_bytes(gkv_ctx* ctx, size_t* out_bytes) {
+  if (!ctx || !out_bytes) return GKV_ERR_INVALID_ARG;
+  const GkvDims& d = ctx->dims;
+  const PagedPlan plan = paged_plan(ctx);
+  *out_bytes = paged_tickets_bytes(d);
+  if (plan.most > 1) *out_bytes += gkv_align256(sizeof(float) * (size_t)d.L * d.B * d.Hkv * plan.most * d.g * (d.d + 2));
+  return GKV_OK;
+}
+
+extern "C" gkv_status gkv_paged_attend_decode(gkv_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* page_table,
+                                              int32_t table_width, int32_t page_rows, int32_t n_pages, const int32_t* d_len,
+                                              int32_t len_max_host, void* out, void* workspace, void* stream) {
+  if (!ctx || !q || !K || !V || !d_len || !out || len_max_host < 0) return GKV_ERR_INVALID_ARG;
+  const gkv_status st = check_pages(page_table, table_width, page_rows, n_pages);
+  if (st != GKV_OK) return st;
+  if (len_max_host > (int64_t)table_width * page_rows) return GKV_ERR_OVERFLOW;
+  if (!workspace || ((uintptr_t)workspace & 15) != 0) return GKV_ERR_WORKSPACE;
+  const GkvDims& d = ctx->dims;
+  const PagedPlan plan = paged_plan(ctx);
+  const int64_t pieces = ((int64_t)len_max_host + 16 * plan.iters - 1) / (16 * plan.iters);
+  PagedAttendArgs a{q, K, V, {page_table, table_width, page_rows, n_pages, gkv_divisor(page_rows)}, d_len, out, (int32_t*)workspace,
+                    (float*)((char*)workspace + paged_tickets_bytes(d)), plan.most,
+                    (int32_t)(pieces < 1 ? 1 : pieces < plan.most ? pieces : plan.most), plan.iters};
+  GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
+  // (the matrix-core kernel counts rows in 32 bits where pages are not whole slices)
+  const bool mfma = use_mfma(ctx, {q, K, V, out}) && (page_rows % 16 == 0 || (int64_t)n_pages * d.Hkv * page_rows <= INT32_MAX);
+  return hip_status(mfma ? gkv_launch_paged_attend_mfma(ln, d, ctx->cfg.dtype, a)
+                         : gkv_launch_paged_attend_generic(ln, d, ctx->cfg.dtype, a));
+}
+
 // ---- profiling API ------------------------------------------------------------------------------
 extern "C" gkv_status gkv_profile_enable(gkv_ctx* ctx, int32_t on) {
   if (!ctx || !ctx->prof) return GKV_ERR_INVALID_ARG;

@@ -187,6 +187,39 @@ struct PrefixArgs {
 struct PrefixPlan { int32_t splits, tiles, blocks, key_groups; };
 hipError_t gkv_launch_prefix_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a, const PrefixPlan& plan);
 hipError_t gkv_launch_prefix_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PrefixArgs& a);
+// ---- rotary positions, paged caches ----------------------------------------------------------
+// freq: radians a position of each pair (64 bits); null: nothing is turned.
+struct GkvRotary { const double* freq; int32_t dim, layout; float amplitude; int32_t transposed; };
+struct RotateArgs {
+  const void* q; const void* k; const void* v;           // null: none of them
+  int64_t q_stride, k_stride, v_stride;                  // elements between tokens
+  int32_t tokens; const int32_t* positions; int32_t step;   // positions == nullptr: `step` for all (rotate), the row (append)
+  GkvRotary rotary;
+  void* q_out; void* k_out;                              // [L, tokens, heads, d]
+};
+struct GkvPages {                                        // K, V [L, n_pages, h_kv, page_rows, d]
+  const int32_t* table; int32_t width, page_rows, n_pages;
+  GkvDivisor by_rows;
+};
+struct AppendArgs {
+  RotateArgs in;                                         // k_out not used
+  const int32_t* start; const int32_t* len;
+  GkvPages pages; void* K; void* V;
+};
+hipError_t gkv_launch_rotate(const GkvLaunch& ln, const GkvDims& dm, int dtype, const RotateArgs& a);
+hipError_t gkv_launch_paged_append(const GkvLaunch& ln, const GkvDims& dm, int dtype, const AppendArgs& a);
+hipError_t gkv_launch_paged_advance(const GkvLaunch& ln, const GkvDims& dm, int32_t* len, const int32_t* start);
+
+struct PagedAttendArgs {
+  const void* q; const void* K; const void* V; GkvPages pages; const int32_t* len; void* out;
+  int32_t* ticket; float* partials;                      // [units][GKV_TICKETS]; [units][most][g][d + 2]
+  int32_t most;                                          // pieces of a unit that there is room for
+  int32_t splits;                                        // pieces that the launch has
+  int32_t split_iters;                                   // slices of 16 rows a piece has at least
+};
+hipError_t gkv_launch_paged_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a);
+hipError_t gkv_launch_paged_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a);
+
 hipError_t gkv_launch_fill_zero(hipStream_t stream, int32_t* p, size_t n);
 hipError_t gkv_launch_add_int(hipStream_t stream, int32_t* p, int32_t delta);
 

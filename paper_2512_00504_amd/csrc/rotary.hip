@@ -1,0 +1,270 @@
+// Rotary positions: queries and keys turned by their tokens' positions, on their own or on the way into a paged cache.
+//
+// Pair p of a head's first `dim` channels, (x1, x2) = channels (p, p + dim/2) or (2p, 2p + 1), becomes
+//   m (x1 cos a - x2 sin a, x1 sin a + x2 cos a),  a = position * freq[p]   (transposed: -a, which is the gradient's way back).
+// A position of a million at one radian each needs 20 bits before the point, so the angle is formed and reduced to a quarter turn in
+// 64 bits; what is left, within +-pi/4, takes a Taylor polynomial in 32 (remainders 2^-29 and 2^-33).  Products and sums are in 32 bits,
+// rounded once to the type.
+//
+// Bound: memory, two passes over the data and nothing else of size.  A workgroup has the cosines and sines of its tokens in LDS, made
+// once for all heads (an angle is some 40 instructions, a turned pair 6), while its first loads are on their way.
+#include "gkv_internal.h"
+
+namespace {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int THREADS = 256, AT_ONCE = 4, MOST_TOKENS = 8;   // of a workgroup; items a thread has on their way; tokens of a workgroup
+
+// cos and sin of position * freq, times m.
+__device__ __forceinline__ float2 turn(double freq, int position, float m, int transposed) {
+  const double a = (double)position * freq;
+  double n = rint(a * 0.63661977236758134308);             // quarter turns
+  const double r = fma(-n, 6.123233995736766036e-17, fma(-n, 1.57079632679489661923, a));
+  n *= 0.25;
+  const int quarter = (int)((n - floor(n)) * 4.0);           // exact
+  const float x = (float)r, z = x * x;
+  const float s = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), x);
+  const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+  float cs = quarter & 1 ? s : c, sn = quarter & 1 ? c : s;
+  if (quarter == 1 || quarter == 2) cs = -cs;
+  if ((quarter >= 2) != (transposed != 0)) sn = -sn;
+  return make_float2(cs * m, sn * m);
+}
+
+// PIECE elements as they are in memory, and as floats.
+template <typename T, int PIECE> struct Piece;
+template <> struct Piece<float, 4> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const float* p) { w = *(const u32x4*)p; }
+  __device__ __forceinline__ void store(float* p) const { *(u32x4*)p = w; }
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
+  __device__ __forceinline__ void set2(int i, float a, float b) { w[i] = __float_as_uint(a); w[i + 1] = __float_as_uint(b); }
+};
+template <> struct Piece<uint16_t, 8> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const uint16_t* p) { w = *(const u32x4*)p; }
+  __device__ __forceinline__ void store(uint16_t* p) const { *(u32x4*)p = w; }
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+  __device__ __forceinline__ void set2(int i, float a, float b) {
+    w[i >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+  }
+};
+template <typename T> struct Piece<T, 1> {
+  T x;
+  __device__ __forceinline__ void load(const T* p) { x = *p; }
+  __device__ __forceinline__ void store(T* p) const { *p = x; }
+  __device__ __forceinline__ float get(int) const { return Elem<T>::ld(&x); }
+  __device__ __forceinline__ void set1(float a) { Elem<T>::st(&x, a); }
+};
+
+struct Args {
+  RotateArgs in;
+  const int32_t *start, *len;
+  GkvPages pages; void *K, *V;
+  int32_t groups, per_group;       // workgroups of a layer, tokens of each
+  GkvDivisor by_groups, by_per_head, by_heads, by_half;
+};
+
+// Which sequence token t is of, and its row there; row < 0: of none.  The wavefront looks through `start` 64 entries at a time.
+struct Place { int seq; int64_t row; };
+__device__ __forceinline__ Place place_of(int t, const int32_t* start, const int32_t* len, int B, int lane) {
+  int seq = t, end = t + 1;
+  if (start) {
+    int before = 0;                                          // entries at or below t
+    for (int i = lane; i - lane <= B; i += 64) before += __popcll(__ballot(i <= B && start[min(i, B)] <= t));
+    if (before == 0 || before > B) return Place{0, -1};
+    seq = before - 1;
+    end = start[seq + 1];
+  }
+  return Place{seq, (int64_t)len[seq] - ((int64_t)end - t)};
+}
+
+// An item is two pieces of a row: of its turned channels the two halves of some pairs (half layout), else neighbours.
+//   VECTOR: pieces of 16 bytes, of which dim/2 (half layout) or dim (interleaved) has to be a whole number; else of one element.
+// Dynamic LDS: float2 angles[per_group][dim/2].
+template <typename T, bool VECTOR, bool HALF, bool APPEND>
+__global__ __launch_bounds__(THREADS) void rotate_kernel(GkvDims dm, Args a) {
+  constexpr int E = VECTOR ? 16 / (int)sizeof(T) : 1;
+  using P = Piece<T, E>;
+  extern __shared__ float2 angles[];
+  __shared__ int64_t row_of[MOST_TOKENS];                     // in the pages of K and V, in rows of d elements; -1: the row is dropped
+  __shared__ int present[MOST_TOKENS], position_of[MOST_TOKENS];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int layer = quotient(blockIdx.x, a.by_groups), group = (int)blockIdx.x - layer * a.groups;
+  const int t0 = group * a.per_group, n = min(a.per_group, a.in.tokens - t0);
+  const int d = dm.d, dim = a.in.rotary.dim, half = dim >> 1, in_half = half / E, pieces = d / E;
+  const int hq = a.in.q ? dm.Hq : 0, hk = a.in.k ? dm.Hkv : 0, heads = hq + hk * (APPEND ? 2 : 1);
+  const int per_head = (pieces + 1) >> 1, items = n * heads * per_head;
+
+  struct Item { int token, slot, i, p0, p1; bool turned0, turned1; };
+  auto item = [&](int x) {
+    Item it;
+    const int row = quotient(x, a.by_per_head);
+    it.i = x - row * per_head;
+    it.token = quotient(row, a.by_heads);
+    it.slot = row - it.token * heads;
+    const bool turns = it.slot < hq + hk;                     // (a row of v does not)
+    if constexpr (HALF) {
+      it.turned0 = it.turned1 = turns && it.i < in_half;
+      it.p0 = it.turned0 ? it.i : 2 * it.i;
+      it.p1 = it.turned0 ? it.i + in_half : 2 * it.i + 1;
+    } else {
+      it.p0 = 2 * it.i;
+      it.p1 = it.p0 + 1;
+      it.turned0 = turns && it.p0 * E < dim;
+      it.turned1 = turns && it.p1 * E < dim;
+    }
+    return it;
+  };
+  auto load = [&](const Item& it, P& x0, P& x1) {
+    const int64_t at = (int64_t)layer * a.in.tokens + t0 + it.token;
+    const T* from;
+    if (it.slot < hq) from = (const T*)a.in.q + at * a.in.q_stride + it.slot * d;
+    else if (it.slot < hq + hk) from = (const T*)a.in.k + at * a.in.k_stride + (it.slot - hq) * d;
+    else from = (const T*)a.in.v + at * a.in.v_stride + (it.slot - hq - hk) * d;
+    x0.load(from + it.p0 * E);
+    x1.load(from + min(it.p1, pieces - 1) * E);
+  };
+  auto store = [&](const Item& it, P& x0, P& x1) {
+    if (!present[it.token]) return;
+    const float2* w = angles + it.token * half;
+    if constexpr (HALF || !VECTOR) {
+      if (it.turned0) {
+        w += it.i * E;
+        if constexpr (VECTOR) {
+#pragma unroll
+          for (int e = 0; e < E; e += 2) {
+            const float u0 = x0.get(e), u1 = x0.get(e + 1), v0 = x1.get(e), v1 = x1.get(e + 1);
+            x0.set2(e, u0 * w[e].x - v0 * w[e].y, u1 * w[e + 1].x - v1 * w[e + 1].y);
+            x1.set2(e, u0 * w[e].y + v0 * w[e].x, u1 * w[e + 1].y + v1 * w[e + 1].x);
+          }
+        } else {
+          const float u = x0.get(0), v = x1.get(0);
+          x0.set1(u * w->x - v * w->y);
+          x1.set1(u * w->y + v * w->x);
+        }
+      }
+    } else {
+      auto pairs = [&](P& x, int p) {
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const float2 cs = w[(p * E + e) >> 1];
+          const float u = x.get(e), v = x.get(e + 1);
+          x.set2(e, u * cs.x - v * cs.y, u * cs.y + v * cs.x);
+        }
+      };
+      if (it.turned0) pairs(x0, it.p0);
+      if (it.turned1) pairs(x1, it.p1);
+    }
+    T* to;
+    const int64_t at = (int64_t)layer * a.in.tokens + t0 + it.token;
+    if (it.slot < hq) to = (T*)a.in.q_out + (at * dm.Hq + it.slot) * d;
+    else if constexpr (APPEND) {
+      if (row_of[it.token] < 0) return;
+      const int h = it.slot - hq;
+      to = (T*)(h < hk ? a.K : a.V) + (row_of[it.token] + (int64_t)(h < hk ? h : h - hk) * a.pages.page_rows) * d;
+    } else to = (T*)a.in.k_out + (at * dm.Hkv + it.slot - hq) * d;
+    x0.store(to + it.p0 * E);
+    if (it.p1 < pieces) x1.store(to + it.p1 * E);
+  };
+
+  // the first items' pieces are on their way while the angles are made
+  Item it[AT_ONCE];
+  P x0[AT_ONCE], x1[AT_ONCE];
+  auto load_all = [&](int first) {
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      it[u] = item(min(first + u * THREADS, items - 1));
+      load(it[u], x0[u], x1[u]);
+    }
+  };
+  load_all(tid);
+  for (int k = wave; k < n; k += THREADS / 64) {
+    const int t = t0 + k;
+    int64_t at = -1;
+    int there = 1, position;
+    if constexpr (APPEND) {
+      const Place place = place_of(t, a.start, a.len, dm.B, lane);
+      there = place.row >= 0;
+      position = a.in.positions ? a.in.positions[t] : (int)place.row;
+      if (there && place.row < (int64_t)a.pages.width * a.pages.page_rows) {
+        const int page = quotient((int)place.row, a.pages.by_rows);
+        const int32_t id = a.pages.table[(int64_t)place.seq * a.pages.width + page];
+        if (id >= 0 && id < a.pages.n_pages)
+          at = ((int64_t)layer * a.pages.n_pages + id) * dm.Hkv * a.pages.page_rows + ((int)place.row - page * a.pages.page_rows);
+      }
+    } else {
+      position = a.in.positions ? a.in.positions[t] : resolve_step(dm, a.in.step);
+    }
+    if (lane == 0) { row_of[k] = at; present[k] = there; position_of[k] = position; }
+  }
+  __syncthreads();
+  for (int x = tid; x < n * half; x += THREADS) {
+    const int k = quotient(x, a.by_half), p = x - k * half;
+    angles[x] = turn(a.in.rotary.freq[p], position_of[k], a.in.rotary.amplitude, a.in.rotary.transposed);
+  }
+  __syncthreads();
+  for (int x = tid;;) {
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u)
+      if (x + u * THREADS < items) store(it[u], x0[u], x1[u]);
+    x += AT_ONCE * THREADS;
+    if (x >= items) break;
+    load_all(x);
+  }
+}
+
+__global__ void advance_kernel(int32_t* len, const int32_t* start, int B) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= B) return;
+  const int now = len[i];
+  const int more = start ? start[i + 1] - start[i] : now >= 0 ? 1 : 0;
+  if (more > 0) len[i] = max(now, 0) + more;
+}
+
+template <typename T, bool APPEND>
+hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, Args a) {
+  if (a.in.tokens == 0) return hipSuccess;
+  constexpr int E = 16 / (int)sizeof(T);
+  const GkvRotary& r = a.in.rotary;
+  const uintptr_t bits = (uintptr_t)a.in.q | (uintptr_t)a.in.k | (uintptr_t)a.in.v | (uintptr_t)a.in.q_out | (uintptr_t)a.in.k_out |
+                         (uintptr_t)a.K | (uintptr_t)a.V |
+                         (uintptr_t)((a.in.q_stride | a.in.k_stride | a.in.v_stride) * (int64_t)sizeof(T));
+  const bool vector = (bits & 15) == 0 && (r.layout == GKV_ROTARY_HALF ? r.dim / 2 : r.dim) % E == 0;
+  const int pieces = dm.d / (vector ? E : 1), per_head = (pieces + 1) / 2;
+  const int heads = (a.in.q ? dm.Hq : 0) + (a.in.k ? dm.Hkv : 0) * (APPEND ? 2 : 1);
+  const int64_t rows = (int64_t)dm.L * a.in.tokens;
+  a.per_group = rows >= 8 * 2048 ? 8 : rows >= 2 * 2048 ? 2 : 1;
+  a.groups = (a.in.tokens + a.per_group - 1) / a.per_group;
+  a.by_groups = gkv_divisor(a.groups);
+  a.by_per_head = gkv_divisor(per_head);
+  a.by_heads = gkv_divisor(heads);
+  a.by_half = gkv_divisor(r.dim > 0 ? r.dim / 2 : 1);
+  const size_t shmem = sizeof(float2) * a.per_group * (r.dim / 2);
+  auto kern = vector ? (r.layout == GKV_ROTARY_HALF ? rotate_kernel<T, true, true, APPEND> : rotate_kernel<T, true, false, APPEND>)
+                     : (r.layout == GKV_ROTARY_HALF ? rotate_kernel<T, false, true, APPEND> : rotate_kernel<T, false, false, APPEND>);
+  return gkv_launch(ln, kern, dim3(dm.L * a.groups), dim3(THREADS), shmem, dm, a);
+}
+
+}  // namespace
+
+hipError_t gkv_launch_rotate(const GkvLaunch& ln, const GkvDims& dm, int dtype, const RotateArgs& in) {
+  Args a{};
+  a.in = in;
+  return dtype == GKV_F32 ? launch<float, false>(ln, dm, a) : launch<uint16_t, false>(ln, dm, a);
+}
+
+hipError_t gkv_launch_paged_append(const GkvLaunch& ln, const GkvDims& dm, int dtype, const AppendArgs& in) {
+  Args a{};
+  a.in = in.in;
+  a.start = in.start; a.len = in.len; a.pages = in.pages; a.K = in.K; a.V = in.V;
+  return dtype == GKV_F32 ? launch<float, true>(ln, dm, a) : launch<uint16_t, true>(ln, dm, a);
+}
+
+hipError_t gkv_launch_paged_advance(const GkvLaunch& ln, const GkvDims& dm, int32_t* len, const int32_t* start) {
+  return gkv_launch(ln, advance_kernel, dim3((dm.B + 255) / 256), dim3(256), 0, len, start, (int)dm.B);
+}

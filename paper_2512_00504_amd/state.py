@@ -52,6 +52,7 @@ class DecodeState:
         dev = torch.device(device)
         self.device = dev
         z = lambda *s, dtype: torch.zeros(*s, dtype=dtype, device=dev)
+        self._k_turned = None
         self._allocate_cache()
         self.pos = torch.full((L, B, Hkv, cap), -1, dtype=torch.int32, device=dev)
         self.qwin = z(w, L, B, Hq, d, dtype=dt)          # ring of the last w q tensors
@@ -165,8 +166,20 @@ class DecodeState:
         self._set_host([b if x else n for x, n in zip(done, self._len)], [0 if x else k for x, k in zip(done, self._since)])
 
     # one call each -------------------------------------------------------------------------
-    def attend_decode(self, q, k_new, v_new, step, prefix=None):
-        """prefix: a SharedPrefix, attended to together with the sequences' own rows."""
+    def _turned(self, q, k_new, step, rotary):
+        """q turned by the step into its slot of the window ring, where the decode kernel finds it, and k_new."""
+        if self._k_turned is None:
+            self._k_turned = torch.empty(self.out.shape[0], self.out.shape[1], self.cfg.n_kv_heads, self.cfg.head_dim, dtype=self.out.dtype,
+                                         device=self.device)
+        slot, k_turned = self.qwin[step % self.cfg.window], None if k_new is None else self._k_turned
+        self.ctx.rotate(q, k_new, None, step, rotary, slot, k_turned)
+        return slot, k_turned
+
+    def attend_decode(self, q, k_new, v_new, step, prefix=None, rotary=None):
+        """prefix: a SharedPrefix, attended to together with the sequences' own rows.  rotary: a Rotary; q and k_new are not turned yet, `step` is
+        their position, and the rows that the cache holds are turned by theirs."""
+        if rotary is not None:
+            q, k_new = self._turned(q, k_new, step, rotary)
         if prefix is None:
             self.ctx.attend_decode(q, k_new, v_new, self.K, self.V, self.pos, step, self.qwin, self.d_state,
                                    self.len_host, self.out, self.workspace)
@@ -272,7 +285,9 @@ class Q8DecodeState(DecodeState):
         self.ctx.q8_read(self.K8, self.V8, self.scales, self.d_state, step, K, V)
         return K, V
 
-    def attend_decode(self, q, k_new, v_new, step, prefix=None):
+    def attend_decode(self, q, k_new, v_new, step, prefix=None, rotary=None):
+        if rotary is not None:
+            q, k_new = self._turned(q, k_new, step, rotary)
         if prefix is not None:
             prefix.attend(q, self)
         self.ctx.q8_attend_decode(q, k_new, v_new, self.K8, self.V8, self.scales, self.pos, step, self.qwin, self.d_state,
@@ -315,6 +330,101 @@ class Q8DecodeState(DecodeState):
         self.ctx.q8_evict(self.qwin, self.K8, self.V8, self.scales, self.F_hist, self.pos, self.d_state, step, self.len_host,
                           self.S, self.F, self.keep_idx, self.workspace)
         self._after_compression()
+
+
+class PagedDecodeState:
+    """Device state of L layers x B sequences whose rows are all kept, in pages: full attention beside the capped caches, or to compare
+    with.  Of cfg the shapes, type and scale count.  Pages are handed out as sequences grow and come back with release().
+
+    max_rows: rows a sequence may have at most.  n_pages: pages of the cache, for all sequences together (default: enough for all of that length).
+    rotary: a Rotary; queries and keys are turned by their positions on the way in, which are their rows unless given."""
+
+    def __init__(self, cfg: GkvConfig, max_rows, page_rows=64, n_pages=None, rotary=None, device="cuda:0", params=None):
+        self.cfg, self.ctx, self.rotary, self.page_rows = cfg, Context(cfg), rotary, page_rows
+        for name, val in (params or {}).items():
+            self.ctx.set_param(name, val)
+        L, B, Hq, Hkv, d = cfg.n_layers, cfg.batch, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+        self.device, dt = torch.device(device), _TORCH_DTYPE[cfg.dtype]
+        width = -(-max_rows // page_rows)
+        n_pages = B * width if n_pages is None else n_pages
+        z = lambda *s, dtype=dt: torch.zeros(*s, dtype=dtype, device=self.device)
+        self.K, self.V = z(L, n_pages, Hkv, page_rows, d), z(L, n_pages, Hkv, page_rows, d)
+        self.page_table = torch.full((B, width), -1, dtype=torch.int32, device=self.device)
+        self.d_len = z(B, dtype=torch.int32)
+        self.out, self.q_turned = z(L, B, Hq, d), z(L, B, Hq, d)
+        self.workspace = z(self.ctx.paged_workspace_bytes(), dtype=torch.uint8)
+        self._table = torch.full((B, width), -1, dtype=torch.int32)          # host mirror
+        self._free = list(range(n_pages))[::-1]
+        self._pages, self._len = [0] * B, [0] * B                            # pages and rows of each sequence; -1 rows: takes no part
+
+    @property
+    def lengths(self):
+        return [max(n, 0) for n in self._len]
+
+    def reserve(self, rows):
+        """Pages for sequences of so many rows (one number, or one for each): steps up to there change the lengths alone and can be recorded."""
+        rows = [rows] * self.cfg.batch if isinstance(rows, int) else list(rows)
+        if len(rows) != self.cfg.batch:
+            raise ValueError(f"gkv: lengths of {self.cfg.batch} sequences are wanted")
+        want = [max(-(-n // self.page_rows), have) for n, have in zip(rows, self._pages)]
+        if want == self._pages:
+            return
+        if max(want) > self._table.shape[1]:
+            raise ValueError(f"gkv: a sequence of {max(rows)} rows is longer than {self._table.shape[1]} pages of {self.page_rows}")
+        if sum(want) - sum(self._pages) > len(self._free):
+            raise ValueError(f"gkv: {sum(want) - sum(self._pages)} pages are needed, {len(self._free)} are free")
+        for i, n in enumerate(want):
+            for p in range(self._pages[i], n):
+                self._table[i, p] = self._free.pop()
+        self._pages = want
+        self.page_table.copy_(self._table)
+
+    def release(self, i):
+        """Sequence i's pages come back, and it takes no part until append() gives it tokens again."""
+        self._free += [int(p) for p in self._table[i, :self._pages[i]].flip(0)]
+        self._table[i] = -1
+        self._pages[i], self._len[i] = 0, -1
+        self.page_table[i] = -1
+        self.d_len[i] = -1
+
+    def append(self, k, v, counts=None, q=None, positions=None, q_out=None):
+        """New tokens k, v [L, tokens, h_kv, d], packed: counts of them for each sequence (None: one for each that takes part, tokens = B); tokens
+        behind the last are padding.  Returns q [L, tokens, h_q, d] turned, in q_out or a new tensor, if it is given."""
+        cfg = self.cfg
+        if counts is not None and (len(counts) != cfg.batch or min(counts) < 0 or sum(counts) > k.shape[1]):
+            raise ValueError(f"gkv: {cfg.batch} counts of {k.shape[1]} tokens are wanted")
+        if counts is None and k.shape[1] != cfg.batch:
+            raise ValueError(f"gkv: one token for each of {cfg.batch} sequences is wanted")
+        if self.rotary is None and q is not None:
+            raise ValueError("gkv: queries are turned where there is a rotary")
+        lens = [n + 1 if n >= 0 else n for n in self._len] if counts is None else [max(n, 0) + m if m else n for n, m in zip(self._len, counts)]
+        self.reserve(lens)
+        start = None
+        if counts is not None:
+            start = torch.tensor([0, *counts], dtype=torch.int32).cumsum(0, dtype=torch.int32).to(self.device)
+        if q is not None and q_out is None:
+            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        self.ctx.paged_advance(self.d_len, start)
+        self._len = lens
+        self.ctx.paged_append(q, k, v, start, self.d_len, positions, self.rotary, self.page_table, self.K, self.V, q_out)
+        return q_out
+
+    def attend(self, q):
+        """The newest tokens' queries, turned, over all rows."""
+        self.ctx.paged_attend_decode(q, self.K, self.V, self.page_table, self.d_len, max(self._pages) * self.page_rows, self.out, self.workspace)
+        return self.out
+
+    def attend_decode(self, q, k_new, v_new, positions=None):
+        """One decode step: q [L, B, h_q, d], k_new, v_new [L, B, h_kv, d]."""
+        if self.rotary is None:
+            self.append(k_new, v_new)
+        else:
+            q = self.append(k_new, v_new, None, q, positions, self.q_turned)
+        return self.attend(q)
+
+    def replayed(self, steps=1):
+        """So many recorded decode steps were replayed: what was not told to this object otherwise."""
+        self._len = [n + steps if n >= 0 else n for n in self._len]
 
 
 class SharedPrefix:

@@ -1,0 +1,473 @@
+"""Paged caches: appends and decode attention over pages, against 64 bits."""
+import pytest
+import torch
+
+import paper_2512_00504_amd as P
+from paper_2512_00504_amd import Rotary, make_config
+from paper_2512_00504_amd.state import DecodeState, PagedDecodeState
+
+from paged_reference import DT, HALF_STEP, attended, place, scale_of, turned
+
+pytestmark = pytest.mark.gpu
+INT = {"bf16": torch.int16, "f32": torch.int32}
+
+
+def _ctx(L=1, B=1, hkv=2, g=2, d=64, dtype="bf16", params=None):
+    ctx = P.Context(make_config(L, B, hkv * g, hkv, d, 64, 8, 16, 96, dtype))
+    for name, value in (params or {}).items():
+        ctx.set_param(name, value)
+    return ctx
+
+
+def _rows(gen, dtype, *shape):
+    x = torch.randn(*shape, generator=gen)
+    return (x * (1 + 4 * (torch.rand(*shape, generator=gen) < 0.02))).to(DT[dtype])
+
+
+def _table(gen, lens, page_rows, n_pages, width):
+    """Pages in no order; -1 behind a sequence's own."""
+    order, table, used = torch.randperm(n_pages, generator=gen), torch.full((len(lens), width), -1, dtype=torch.int32), 0
+    for i, n in enumerate(lens):
+        m = min(-(-max(n, 0) // page_rows), width)
+        table[i, :m] = order[used:used + m].int()
+        used += m
+    assert used <= n_pages
+    return table
+
+
+def _attend(ctx, q, K, V, table, lens, len_max=None):
+    out = torch.full(q.shape, float("nan"), dtype=q.dtype, device="cuda")
+    ws = torch.zeros(ctx.paged_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    room = table.shape[1] * K.shape[3]
+    len_max = min(room, max(max(lens), 0)) if len_max is None else len_max
+    for _ in range(2):                                       # a second call finds what the first left
+        ctx.paged_attend_decode(q.cuda(), K, V, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), len_max, out, ws)
+    return out
+
+
+def _case(dtype, d, g, lens, page_rows, L=1, hkv=2, params=None, seed=0, spoil=True, spare=2, holes=()):
+    B = len(lens)
+    ctx = _ctx(L, B, hkv, g, d, dtype, params)
+    gen = torch.Generator().manual_seed(seed + d + page_rows)
+    width = -(-max(max(lens), 1) // page_rows) + 1
+    n_pages = sum(-(-max(n, 0) // page_rows) for n in lens) + spare
+    K, V = _rows(gen, dtype, L, n_pages, hkv, page_rows, d), _rows(gen, dtype, L, n_pages, hkv, page_rows, d)
+    q = _rows(gen, dtype, L, B, hkv * g, d)
+    table = _table(gen, lens, page_rows, n_pages, width)
+    for i, p, value in holes:
+        table[i, p] = value
+    if spoil:                                                # whatever no sequence has is no number
+        used = torch.zeros(n_pages, page_rows, dtype=torch.bool)
+        for i, n in enumerate(lens):
+            for r in range(max(n, 0)):
+                page = int(table[i, r // page_rows])
+                if 0 <= page < n_pages:
+                    used[page, r % page_rows] = True
+        for x in (K, V):
+            x.masked_fill_(~used[None, :, None, :, None], float("nan"))
+    out = _attend(ctx, q, K.cuda(), V.cuda(), table, lens)
+    ref, tol = attended(q, K, V, table, lens, scale_of(d), dtype)
+    err = (out.cpu().double() - ref).abs()
+    assert (err <= tol).all(), (err - tol).max().item()
+    return ctx, out
+
+
+SHAPES = [("bf16", 128, 7), ("bf16", 128, 1), ("bf16", 64, 5), ("f32", 64, 4), ("f32", 128, 2), ("bf16", 128, 16), ("f32", 128, 16), ("bf16", 64, 16),
+          ("bf16", 48, 3), ("f32", 20, 2), ("bf16", 64, 17), ("bf16", 512, 2)]
+LENS = [0, 1, 15, 16, 17, 33, 129, 255, 256, 257]
+
+
+@pytest.mark.parametrize("dtype,d,g", SHAPES)
+@pytest.mark.parametrize("page_rows", [1, 5, 8, 12, 16, 20, 32, 48, 256])
+def test_lengths_and_pages(dtype, d, g, page_rows):
+    _case(dtype, d, g, LENS, page_rows)
+
+
+@pytest.mark.parametrize("page_rows", [16, 12])
+@pytest.mark.parametrize("dtype,d,params", [("bf16", 128, None), ("bf16", 64, None), ("f32", 64, None), ("f32", 128, None), ("bf16", 128, {"force_generic": 1}),
+                                            ("f32", 64, {"force_generic": 1})])
+def test_long_sequences_in_pieces(dtype, d, params, page_rows):
+    _case(dtype, d, 3, [5000], page_rows, hkv=1, params=params)
+    _case(dtype, d, 2, [3001, 0, 17, 2048, 600], page_rows, L=2, hkv=2, params=params)
+
+
+@pytest.mark.parametrize("dtype,d,g,B,hkv,L", [("bf16", 128, 7, 130, 4, 1), ("bf16", 64, 2, 70, 8, 2), ("f32", 64, 4, 300, 2, 1), ("f32", 128, 1, 66, 8, 1)])
+def test_many_units(dtype, d, g, B, hkv, L):
+    _case(dtype, d, g, [(37 * i) % 190 for i in range(B)], 16, L=L, hkv=hkv, spoil=False)
+
+
+def test_ragged_batch_with_one_long_sequence():
+    _case("bf16", 128, 2, [20000] + [(31 * i) % 300 for i in range(70)], 64, hkv=8, spoil=False)
+
+
+@pytest.mark.parametrize("dtype,d,params", [("bf16", 128, None), ("f32", 64, None), ("bf16", 128, {"force_generic": 1})])
+@pytest.mark.parametrize("page_rows", [16, 12, 64])
+def test_pages_that_are_not_there(dtype, d, params, page_rows):
+    # a hole at the start, in the middle, at the end; all of them; numbers far outside
+    holes = [(0, 0, -1), (1, 3, 1 << 30), (2, 200 // page_rows, -(2 ** 31)), *[(3, p, -5) for p in range(-(-201 // page_rows))], (4, 1, 2 ** 31 - 1)]
+    _, out = _case(dtype, d, 3, [201, 201, 201, 201, 2900], page_rows, params=params, holes=holes)
+    assert (out[:, 3] == 0).all()
+
+
+def test_lengths_beyond_the_table_and_below_zero():
+    ctx = _ctx(1, 3, 1, 2, 64)
+    gen = torch.Generator().manual_seed(1)
+    K, V, q = _rows(gen, "bf16", 1, 9, 1, 16, 64), _rows(gen, "bf16", 1, 9, 1, 16, 64), _rows(gen, "bf16", 1, 3, 2, 64)
+    table = _table(gen, [48, 48, 48], 16, 9, 3)
+    for lens in ([49, 48, -3], [2 ** 31 - 1, 1, -(2 ** 31)]):
+        out = _attend(ctx, q, K.cuda(), V.cuda(), table, lens, 48)
+        ref, tol = attended(q, K, V, table, lens, scale_of(64), "bf16")
+        assert ((out.cpu().double() - ref).abs() <= tol).all() and (out[0, 2] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,d,page_rows", [("bf16", 128, 16), ("f32", 64, 12), ("bf16", 48, 16)])
+def test_the_bound_of_lengths_does_not_show(dtype, d, page_rows):
+    lens = [1500, 700, 1, 0]
+    B = len(lens)
+    ctx = _ctx(1, B, 2, 3, d, dtype)
+    gen = torch.Generator().manual_seed(2)
+    n = sum(-(-x // page_rows) for x in lens)
+    K, V, q = _rows(gen, dtype, 1, n, 2, page_rows, d).cuda(), _rows(gen, dtype, 1, n, 2, page_rows, d).cuda(), _rows(gen, dtype, 1, B, 6, d)
+    table = _table(gen, lens, page_rows, n, 6000 // page_rows)
+    outs = [_attend(ctx, q, K, V, table, lens, bound) for bound in (1500, 1501, 4000, 6000 // page_rows * page_rows)]
+    assert all(torch.equal(outs[0], x) for x in outs)
+
+
+def test_a_bound_that_is_too_low_still_covers_every_row():
+    ctx = _ctx(1, 1, 1, 2, 64)
+    gen = torch.Generator().manual_seed(5)
+    K, V, q = _rows(gen, "bf16", 1, 200, 1, 16, 64), _rows(gen, "bf16", 1, 200, 1, 16, 64), _rows(gen, "bf16", 1, 1, 2, 64)
+    table = _table(gen, [3200], 16, 200, 200)
+    ref, tol = attended(q, K, V, table, [3200], scale_of(64), "bf16")
+    for bound in (0, 1, 600, 3200):
+        out = _attend(ctx, q, K.cuda(), V.cuda(), table, [3200], bound)
+        assert ((out.cpu().double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype,d,params", [("bf16", 128, None), ("bf16", 64, None), ("f32", 64, None), ("f32", 128, None), ("bf16", 128, {"force_generic": 1})])
+@pytest.mark.parametrize("page_rows", [16, 12])
+@pytest.mark.parametrize("n", [70, 1500])
+def test_hard_logits_and_values(dtype, d, params, page_rows, n):
+    B, g = 7, 2
+    ctx = _ctx(1, B, 1, g, d, dtype, params)
+    gen = torch.Generator().manual_seed(7)
+    pages = -(-n // page_rows)
+    K, V = (torch.randn(B, pages * page_rows, d, generator=gen).to(DT[dtype]) for _ in range(2))
+    K[..., :4] = 0.0
+    q = torch.randn(1, B, g, d, generator=gen).to(DT[dtype])
+    q[..., :4] = 0.0
+    best = n // 2
+    K[0, best, 0] = 1.0; q[0, 0, :, 0] = 2.0 ** 40           # one row takes all
+    q[0, 1] *= 2.0 ** 40                                     # huge logits of either sign
+    K[2, :, 1] = 1.0; q[0, 2, :, 1] = -2.0 ** 120            # all of them far below zero, alike
+    K[3, best, 2] = 1.0; q[0, 3, :, 2] = -2.0 ** 120         # one row counts for nothing
+    q[0, 4, 0, 5] = float("nan")                             # one head is no number
+    V[5, best, 7] = float("inf")                             # one value is infinite
+    K[6, :, 3] = 1.0; q[0, 6, :, 3] = float("-inf")          # every logit -inf
+    pool = lambda x: x.view(B * pages, 1, page_rows, d)[None].cuda()
+    table = torch.arange(B * pages, dtype=torch.int32).view(B, pages)
+    out = _attend(ctx, q, pool(K), pool(V), table, [n] * B)[0].cpu().double()
+    v = V[:, :n].double()
+    assert ((out[0] - v[0, best]).abs() <= HALF_STEP[dtype] * v[0, best].abs()).all()
+    z = q[0, 1].double() @ K[1, :n].double().T
+    want = v[1][z.argmax(dim=-1)]
+    top2 = z.topk(2, dim=-1).values
+    sure = (top2[:, 0] - top2[:, 1]) / scale_of(d) > 2.0 ** 20       # (the winner is the same in 32 bits)
+    assert sure.all() and ((out[1] - want).abs() <= HALF_STEP[dtype] * want.abs()).all()
+    some = [x for x in range(n) if x != best]
+    zz = torch.softmax(q[0, 3].double()[:, 4:] @ K[3, some].double()[:, 4:].T * scale_of(d), dim=-1)
+    size = (q[0, 3].double()[:, 4:].abs() @ K[3, some].double()[:, 4:].abs().T * scale_of(d)).max().item()
+    top = v[3].abs().max().item()
+    bound = (2 * (d + 4) * size + n + 32) * 2.0 ** -24 * top + (2.0 ** -15 * top if dtype == "bf16" else 0)
+    want = zz @ v[3][some]
+    assert ((out[3] - want).abs() <= bound + HALF_STEP[dtype] * want.abs()).all()
+    assert torch.isnan(out[4, 0]).all() and torch.isfinite(out[4, 1]).all()
+    assert torch.isposinf(out[5, :, 7]).all() and torch.isfinite(out[5, :, [c for c in range(d) if c != 7]]).all()
+    assert torch.isnan(out[6]).all()
+    assert torch.isfinite(out[2]).all() and out[2].abs().max() <= top * 1.01
+
+
+def test_pages_beyond_32_bits_of_offset():
+    # the pool of one layer is 4.3 GB of K; the pages in use lie at its end
+    d, hkv, page_rows, n_pages = 128, 8, 16, 132000
+    ctx = _ctx(1, 2, hkv, 2, d)
+    gen = torch.Generator().manual_seed(3)
+    K, V = (torch.zeros(1, n_pages, hkv, page_rows, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    lens = [70, 33]
+    ids = [[n_pages - 1, 5, n_pages - 2, n_pages - 9, n_pages - 3], [n_pages - 4, 0, n_pages - 5, -1, -1]]
+    table = torch.tensor(ids, dtype=torch.int32)
+    small = _rows(gen, "bf16", 1, 8, hkv, page_rows, d), _rows(gen, "bf16", 1, 8, hkv, page_rows, d)
+    order = sorted({p for row in ids for p in row if p >= 0})
+    for x, y in zip((K, V), small):
+        for n, p in enumerate(order):
+            x[0, p] = y[0, n].cuda()
+    q = _rows(gen, "bf16", 1, 2, hkv * 2, d)
+    renamed = torch.tensor([[order.index(p) if p >= 0 else -1 for p in row] for row in ids], dtype=torch.int32)
+    for params in (None, {"force_generic": 1}):
+        ctx = _ctx(1, 2, hkv, 2, d, params=params)
+        out = _attend(ctx, q, K, V, table, lens)
+        ref, tol = attended(q, *small, renamed, lens, scale_of(d), "bf16")
+        assert ((out.cpu().double() - ref).abs() <= tol).all()
+    # and appended to there
+    k, v = _rows(gen, "bf16", 1, 2, hkv, d).cuda(), _rows(gen, "bf16", 1, 2, hkv, d).cuda()
+    ctx.paged_append(None, k, v, None, torch.tensor(lens, dtype=torch.int32).cuda(), None, None, table.cuda(), K, V, None)
+    for i, n in enumerate(lens):
+        page, row = ids[i][(n - 1) // page_rows], (n - 1) % page_rows
+        assert torch.equal(K[0, page, :, row], k[0, i]) and torch.equal(V[0, page, :, row], v[0, i])
+
+
+def test_sequences_that_share_pages():
+    ctx = _ctx(1, 3, 2, 3, 128)
+    gen = torch.Generator().manual_seed(6)
+    K, V, q = _rows(gen, "bf16", 1, 9, 2, 16, 128), _rows(gen, "bf16", 1, 9, 2, 16, 128), _rows(gen, "bf16", 1, 3, 6, 128)
+    table = torch.tensor([[4, 2, 7], [4, 2, 8], [4, 4, 4]], dtype=torch.int32)
+    lens = [40, 45, 48]
+    out = _attend(ctx, q, K.cuda(), V.cuda(), table, lens)
+    ref, tol = attended(q, K, V, table, lens, scale_of(128), "bf16")
+    assert ((out.cpu().double() - ref).abs() <= tol).all()
+
+
+# ---- appends ---------------------------------------------------------------------------------------
+def _append(dtype, d, page_rows, counts, lens, pad=0, dim=None, layout="half", L=2, hkv=2, g=2, fused=False, positions=False, rotate=True, table=None, one_each=False,
+            width=None):
+    B = len(lens)
+    ctx = _ctx(L, B, hkv, g, d, dtype)
+    gen = torch.Generator().manual_seed(d + page_rows + sum(counts))
+    width = width or -(-max(max(lens), 1) // page_rows) + 1
+    n_pages = sum(-(-max(n, 0) // page_rows) for n in lens) + 2
+    T, hq = sum(counts) + pad, hkv * g
+    x = _rows(gen, dtype, L, T, hq + 2 * hkv, d).cuda()
+    q, k, v = x[:, :, :hq], x[:, :, hq:hq + hkv], x[:, :, hq + hkv:]
+    if not fused:
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+    K0, V0 = (torch.randint(-2 ** 15, 2 ** 15, (L, n_pages, hkv, page_rows, d), generator=gen).to(INT[dtype]).view(DT[dtype]) for _ in range(2))
+    q0 = torch.full((L, T, hq, d), 7.0, dtype=DT[dtype])
+    table = _table(gen, lens, page_rows, n_pages, width) if table is None else table(n_pages, width)
+    rotary = Rotary(d if dim is None else dim, 10000.0, layout, "smooth", 8.0, 4096.0, 1.0, 4.0) if rotate else None
+    starts = [sum(counts[:i]) for i in range(B + 1)]
+    at = (torch.arange(T, dtype=torch.int32) * 37 + 100000).cuda() if positions else None
+    K, V, q_out = K0.cuda(), V0.cuda(), q0.cuda()
+    ctx.paged_append(q if rotate else None, k, v, None if one_each else torch.tensor(starts, dtype=torch.int32).cuda(),
+                     torch.tensor(lens, dtype=torch.int32).cuda(), at, rotary, table.cuda(), K, V, q_out if rotate else None)
+    K, V, q_out, q, k, v = (y.cpu() for y in (K, V, q_out, q, k, v))
+    bits = lambda y: y.contiguous().view(INT[dtype])
+    for t in range(T):
+        to = place(lens, starts, t)
+        if to is None:
+            assert torch.equal(bits(q_out[:, t]), bits(q0[:, t]))
+            continue
+        i, row = to
+        if rotate:
+            p = at[t:t + 1].cpu() if positions else torch.tensor([row])
+            ref, tol = turned(q[:, t:t + 1], p, rotary.freq.cpu(), layout, rotary.amplitude, dtype=dtype)
+            assert ((q_out[:, t:t + 1].double() - ref).abs() <= tol).all(), t
+        page = int(table[i, row // page_rows]) if row // page_rows < table.shape[1] else -1
+        if not 0 <= page < n_pages:
+            continue
+        got = K[:, page, :, row % page_rows]
+        if rotate:
+            ref, tol = turned(k[:, t:t + 1], p, rotary.freq.cpu(), layout, rotary.amplitude, dtype=dtype)
+            assert ((got.double() - ref[:, 0]).abs() <= tol[:, 0]).all(), t
+        else:
+            assert torch.equal(bits(got), bits(k[:, t]))
+        assert torch.equal(bits(V[:, page, :, row % page_rows]), bits(v[:, t]))
+        K0[:, page, :, row % page_rows], V0[:, page, :, row % page_rows] = got, v[:, t]
+    assert torch.equal(bits(K), bits(K0)) and torch.equal(bits(V), bits(V0))      # every other row as it was
+
+
+@pytest.mark.parametrize("dtype,d,dim,layout", [("bf16", 128, 128, "half"), ("bf16", 64, 48, "interleaved"), ("f32", 64, 64, "half"), ("f32", 20, 10, "half"), ("bf16", 72, 72, "half"),
+                                                ("bf16", 128, 50, "interleaved")])
+@pytest.mark.parametrize("page_rows", [1, 12, 16, 64])
+@pytest.mark.parametrize("fused", [False, True])
+def test_append_packed_tokens(dtype, d, dim, layout, page_rows, fused):
+    _append(dtype, d, page_rows, [1, 0, 33, 7, 0, 60], [1, 0, 40, 7, 30, 75], pad=5, dim=dim, layout=layout, fused=fused)
+    _append(dtype, d, page_rows, [0, 2, 0], [-1, 90, 3], pad=0, dim=dim, layout=layout, fused=fused, positions=True)
+
+
+def test_append_one_each_and_sequences_that_take_no_part():
+    _append("bf16", 128, 16, [1, 1, 1, 1], [17, 1, 64, 33], one_each=True)
+    _append("bf16", 128, 16, [1, 1, 1, 1], [17, 0, -1, 33], one_each=True)
+
+
+def test_append_keys_that_are_turned_already():
+    _append("bf16", 128, 16, [5, 40], [9, 41], rotate=False, fused=True)
+    _append("f32", 36, 7, [5, 40], [9, 41], rotate=False)
+
+
+def test_append_rows_without_a_page():
+    # holes, a table that is too short, more new tokens than rows
+    _append("bf16", 64, 16, [30, 10], [64, 20], width=3)
+    _append("bf16", 64, 16, [30, 10], [64, 20], table=lambda n, w: torch.tensor([[0, 1, -1, n][:w] + [0] * (w - 4), [2, 10 ** 9] + [-1] * (w - 2)], dtype=torch.int32))
+    _append("bf16", 64, 16, [30, 10], [12, 10])
+
+
+def test_append_many_sequences_and_tokens():
+    B = 150
+    counts = [(i * 7) % 5 for i in range(B)]
+    _append("bf16", 64, 16, counts, [n + (i * 3) % 20 for i, n in enumerate(counts)], pad=3, L=1, hkv=1, g=1)
+    _append("f32", 64, 16, [0] * 63 + [9] + [0] * 64, [20] * 128, L=1, hkv=1, g=1)
+
+
+@pytest.mark.parametrize("T", [2500, 17000])
+def test_append_long_prompts(T):
+    ctx = _ctx(1, 2, 1, 2, 64)
+    gen = torch.Generator().manual_seed(1)
+    q, k, v = (_rows(gen, "bf16", 1, T, h, 64).cuda() for h in (2, 1, 1))
+    a = T // 3
+    n_pages = -(-a // 16) + -(-(T - a) // 16)
+    table = _table(gen, [a, T - a], 16, n_pages, -(-T // 16))
+    K, V = (torch.zeros(1, n_pages, 1, 16, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    rotary, q_out = Rotary(64), torch.empty_like(q)
+    ctx.paged_append(q, k, v, torch.tensor([0, a, T], dtype=torch.int32).cuda(), torch.tensor([a, T - a], dtype=torch.int32).cuda(), None, rotary, table.cuda(), K, V, q_out)
+    rows = torch.cat([torch.arange(a), torch.arange(T - a)])
+    ref, tol = turned(q.cpu(), rows, rotary.freq.cpu(), "half")
+    assert ((q_out.cpu().double() - ref).abs() <= tol).all()
+    ref, tol = turned(k.cpu(), rows, rotary.freq.cpu(), "half")
+    page = torch.cat([table[0, torch.arange(a) // 16], table[1, torch.arange(T - a) // 16]]).long()
+    assert ((K.cpu()[0, page, 0, rows % 16].double() - ref[0, :, 0]).abs() <= tol[0, :, 0]).all()
+    assert torch.equal(V.cpu()[0, page, 0, rows % 16], v[0, :, 0].cpu())
+
+
+def test_advance():
+    ctx = _ctx(1, 5)
+    d_len = torch.tensor([0, 7, -1, -9, 3], dtype=torch.int32).cuda()
+    ctx.paged_advance(d_len, None)
+    assert d_len.tolist() == [1, 8, -1, -9, 4]
+    ctx.paged_advance(d_len, torch.tensor([0, 3, 3, 5, 5, 6], dtype=torch.int32).cuda())
+    assert d_len.tolist() == [4, 8, 2, -9, 5]
+
+
+# ---- together --------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype,d,page_rows,layout", [("bf16", 128, 16, "half"), ("f32", 64, 12, "interleaved"), ("bf16", 72, 32, "half")])
+def test_prompts_and_decode_steps(dtype, d, page_rows, layout):
+    # prompts of all lengths, steps, a sequence that leaves and another that comes in its place; every step against 64 bits on the
+    # cache's own rows, which are the turned keys
+    L, B, hkv, g = 2, 4, 2, 3
+    rotary = Rotary(d // 2 * 2 if d != 72 else 40, 10000.0, layout, "linear", 2.0)
+    st = PagedDecodeState(make_config(L, B, hkv * g, hkv, d, 64, 8, 16, 96, dtype), max_rows=120, page_rows=page_rows, rotary=rotary)
+    gen = torch.Generator().manual_seed(11)
+    new = lambda n: [_rows(gen, dtype, L, n, h, d) for h in (hkv * g, hkv, hkv)]
+    held = [[] for _ in range(B)]                            # of each sequence: (k, v) per row, not turned
+    cuda = lambda xs: [x.cuda() for x in xs]
+
+    def note(counts, k, v):
+        at = 0
+        for i, n in enumerate(counts):
+            held[i] += [(k[:, at + m], v[:, at + m]) for m in range(n)]
+            at += n
+
+    def check(out, q):
+        lens = [len(h) for h in held]
+        assert st.lengths == lens and [max(x, 0) for x in st.d_len.tolist()] == lens
+        K, V, table = st.K.cpu(), st.V.cpu(), st.page_table.cpu()
+        for i, rows in enumerate(held):
+            for r, (k, v) in enumerate(rows):
+                ref, tol = turned(k[:, None], torch.tensor([r]), rotary.freq.cpu(), layout, dtype=dtype)
+                page = int(table[i, r // page_rows])
+                assert ((K[:, page, :, r % page_rows].double() - ref[:, 0]).abs() <= tol[:, 0]).all()
+                assert torch.equal(V[:, page, :, r % page_rows], v)
+        pos = torch.tensor([n - 1 for n in lens])
+        ref, tol = turned(q, pos, rotary.freq.cpu(), layout, dtype=dtype)
+        qt = st.q_turned.cpu()
+        on = [i for i, n in enumerate(lens) if n]
+        assert ((qt[:, on].double() - ref[:, on]).abs() <= tol[:, on]).all()
+        ref, tol = attended(qt, K, V, table, lens, scale_of(d), dtype)
+        assert ((out.cpu().double() - ref).abs() <= tol).all()
+
+    counts = [17, 0, 64, 1]
+    q, k, v = new(sum(counts) + 3)
+    st.append(*cuda((k, v)), counts, q.cuda())
+    note(counts, k, v)
+    for t in range(20):
+        if t == 9:
+            st.release(2)
+            held[2] = []
+        if t == 12:
+            counts = [0, 0, 33, 0]
+            q, k, v = new(33)
+            st.append(*cuda((k, v)), counts)
+            note(counts, k, v)
+        q, k, v = new(B)
+        out = st.attend_decode(*cuda((q, k, v)))
+        for i in range(B):
+            if st._len[i] >= 0:
+                held[i].append((k[:, i], v[:, i]))
+        if t in (0, 8, 10, 13, 19):
+            check(out, q)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+def test_agrees_with_the_contiguous_cache(dtype, d):
+    # the same tokens, nothing evicted: the two kernels may differ by what either may from 64 bits
+    cfg = make_config(2, 3, 8, 2, d, 512, 8, 16, 544, dtype)
+    a, b = DecodeState(cfg), PagedDecodeState(cfg, max_rows=300)
+    gen = torch.Generator().manual_seed(2)
+    for t in range(130):
+        q, k, v = (_rows(gen, dtype, 2, 3, h, d).cuda() for h in (8, 2, 2))
+        one, two = a.attend_decode(q, k, v, t), b.attend_decode(q, k, v)
+    top = 15.0
+    tol = 2 * (2 * (d + 4) * 30 + 160) * 2.0 ** -24 * top + (2.0 ** -7 * top if dtype == "bf16" else 0)
+    assert (one.double() - two.double()).abs().max() <= tol
+    ref, bound = attended(q.cpu(), b.K.cpu(), b.V.cpu(), b.page_table.cpu(), [130] * 3, scale_of(d), dtype)
+    assert ((two.cpu().double() - ref).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("page_rows,d,dtype", [(16, 128, "bf16"), (12, 64, "f32"), (16, 48, "bf16")])
+def test_recorded_steps_replay(page_rows, d, dtype):
+    # steps of a long sequence (in pieces) and short ones, recorded once: each replay against eager steps of another state
+    L, B, hkv, g = 2, 3, 2, 2
+    cfg = make_config(L, B, hkv * g, hkv, d, 64, 8, 16, 96, dtype)
+    rotary = Rotary(d)
+    a, b = (PagedDecodeState(cfg, max_rows=2400, page_rows=page_rows, rotary=rotary) for _ in range(2))
+    gen = torch.Generator().manual_seed(4)
+    counts = [2000, 0, 37]
+    q, k, v = (_rows(gen, dtype, L, sum(counts), h, d).cuda() for h in (hkv * g, hkv, hkv))
+    for st in (a, b):
+        st.append(k, v, counts)
+        st.reserve([2100, 100, 137])
+    ins = [_rows(gen, dtype, L, B, h, d).cuda() for h in (hkv * g, hkv, hkv)]
+    a.attend_decode(*ins)                                    # warm
+    b.attend_decode(*ins)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        first = a.attend_decode(*ins).clone()
+        second = a.attend_decode(*ins).clone()
+    a.replayed(2)                                            # two replays of two steps, one counted when recorded
+    a.replayed(2)
+    for i in range(3):
+        for x in ins:
+            x.mul_(-1.5).add_(0.25)
+        graph.replay()
+        torch.cuda.synchronize()
+        one = b.attend_decode(*ins).clone()
+        assert torch.equal(first, one)
+        assert torch.equal(second, b.attend_decode(*ins))
+        assert torch.equal(a.d_len, b.d_len)
+    assert a.lengths == b.lengths == a.d_len.tolist()
+
+
+def test_calls_on_two_streams_with_a_workspace_each():
+    ctx = _ctx(1, 2, 2, 4, 128)
+    gen = torch.Generator().manual_seed(8)
+    lens, n = [3000, 2000], 320
+    K, V = _rows(gen, "bf16", 1, n, 2, 16, 128).cuda(), _rows(gen, "bf16", 1, n, 2, 16, 128).cuda()
+    table = _table(gen, lens, 16, n, 200).cuda()
+    d_len = torch.tensor(lens, dtype=torch.int32).cuda()
+    qs = [_rows(gen, "bf16", 1, 2, 8, 128).cuda() for _ in range(2)]
+    wss = [torch.zeros(ctx.paged_workspace_bytes(), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    refs = []
+    for q in qs:
+        out = torch.empty_like(q)
+        ctx.paged_attend_decode(q, K, V, table, d_len, 3000, out, wss[0])
+        refs.append(out)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.empty_like(q) for q in qs]
+    for _ in range(30):
+        for s, q, out, ws in zip(streams, qs, outs, wss):
+            with torch.cuda.stream(s):
+                ctx.paged_attend_decode(q, K, V, table, d_len, 3000, out, ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(outs, refs))
