@@ -923,17 +923,31 @@ extern "C" gkv_status gkv_paged_advance(gkv_ctx* ctx, int32_t* d_len, const int3
   return hip_status(gkv_launch_paged_advance(ln, ctx->dims, d_len, d_start));
 }
 
-// Pieces of a unit there is room for, and slices of 16 rows a piece has at least.  By the configuration alone: the same call gives the same bits
+// How units are cut (gkv_paged_pieces), and the pieces there is room for.  By the configuration alone: the same call gives the same bits
 // whatever bound of the lengths it comes with.
-struct PagedPlan { int32_t most, iters; };
+//   A workgroup (8 wavefronts) takes as many slices at a time as it has wavefronts, of 32 rows at bf16, d = 64 and of 16 else; the chip holds 512
+//   workgroups.  A piece more costs its start and its part of the joining, some 2 us beside others' reading.  us, by slices a piece:
+//     iters  4 units of 577 rows 8 / 16 / 32: 6.4 / 7.5 / 8.3, of 4096 7.6 / 7.6 / 9.8; 128 units of 577 16 / 32 / whole 10.1 / 9.4 / 9.7; 256 units
+//            of up to 4000 16 / 32 / 64 / 128 45.1 / 45.1 / 47.5 / 53; 512 units of up to 16384 64 / 128 / 256 / 512 362 / 353 / 356 / 374, of 8192
+//            350 / 336 / 329 / 322; bf16, d = 64 96 units of up to 3001 16 / 24 / 32 11.4 / 11.3 / 11.5.
+//     soft   pieces of a unit: 256 workgroups in all (4 units of 131071 rows 32 / 64 / 128 pieces 50.0 / 45.2 / 49.4), or 8 (32 units of 8192 rows,
+//            4 / 8 / 16 27.6 / 23.7 / 24.3).
+//     long_iters  in batches, where the longest sequence would end alone: 4096 rows a piece, up to what 512 workgroups of one sequence are.
+struct PagedPlan { int32_t most, iters, soft, long_iters; };
 static PagedPlan paged_plan(const gkv_ctx* ctx) {
   const GkvDims& d = ctx->dims;
   const int64_t units = (int64_t)d.L * d.B * d.Hkv, of_one = (int64_t)d.L * d.Hkv;
-  int64_t most = 512 / of_one;
-  if (most > 32768 / units) most = 32768 / units;
-  return PagedPlan{(int32_t)(most < 1 ? 1 : most > 128 ? 128 : most), units >= 512 ? 64 : 16};
+  auto within = [](int64_t x, int64_t lo, int64_t hi) { return (int32_t)(x < lo ? lo : x > hi ? hi : x); };
+  PagedPlan p;
+  p.iters = units >= 512 ? 256 : within(units / 4, d.d == 64 && ctx->cfg.dtype == GKV_BF16 ? 16 : 8, 32);
+  p.soft = within(256 / units, 8, 64);
+  p.long_iters = units >= 32 ? 256 : GKV_MOST_ROWS;
+  p.most = within(512 / of_one, 1, within(32768 / units, 1, 64));
+  if (units < 32 && p.most < p.soft) p.most = p.soft;
+  if (p.soft > p.most) p.soft = p.most;
+  return p;
 }
-static size_t paged_tickets_bytes(const GkvDims& d) { return gkv_align256(sizeof(int32_t) * GKV_TICKETS * (size_t)d.L * d.B * d.Hkv); }
+static size_t paged_tickets_bytes(const GkvDims& d) { return gkv_align256(sizeof(int32_t) * GKV_PAGED_TICKET * GKV_TICKETS * (size_t)d.L * d.B * d.Hkv); }
 
 extern "C" gkv_status gkv_paged_workspace_bytes(gkv_ctx* ctx, size_t* out_bytes) {
   if (!ctx || !out_bytes) return GKV_ERR_INVALID_ARG;
@@ -954,10 +968,10 @@ extern "C" gkv_status gkv_paged_attend_decode(gkv_ctx* ctx, const void* q, const
   if (!workspace || ((uintptr_t)workspace & 15) != 0) return GKV_ERR_WORKSPACE;
   const GkvDims& d = ctx->dims;
   const PagedPlan plan = paged_plan(ctx);
-  const int64_t pieces = ((int64_t)len_max_host + 16 * plan.iters - 1) / (16 * plan.iters);
+  const int pieces = gkv_paged_pieces(((int64_t)len_max_host + 15) / 16, plan.iters, plan.soft, plan.long_iters);
   PagedAttendArgs a{q, K, V, {page_table, table_width, page_rows, n_pages, gkv_divisor(page_rows)}, d_len, out, (int32_t*)workspace,
                     (float*)((char*)workspace + paged_tickets_bytes(d)), plan.most,
-                    (int32_t)(pieces < 1 ? 1 : pieces < plan.most ? pieces : plan.most), plan.iters};
+                    pieces < 1 ? 1 : pieces < plan.most ? pieces : plan.most, plan.iters, plan.soft, plan.long_iters};
   GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
   // (the matrix-core kernel counts rows in 32 bits where pages are not whole slices)
   const bool mfma = use_mfma(ctx, {q, K, V, out}) && (page_rows % 16 == 0 || (int64_t)n_pages * d.Hkv * page_rows <= INT32_MAX);

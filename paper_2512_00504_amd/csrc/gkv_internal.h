@@ -210,13 +210,21 @@ hipError_t gkv_launch_rotate(const GkvLaunch& ln, const GkvDims& dm, int dtype, 
 hipError_t gkv_launch_paged_append(const GkvLaunch& ln, const GkvDims& dm, int dtype, const AppendArgs& a);
 hipError_t gkv_launch_paged_advance(const GkvLaunch& ln, const GkvDims& dm, int32_t* len, const int32_t* start);
 
+// A unit's ticket has a 128-byte line of its own: its pieces' additions to it come one after the other, and would wait for other units' too.
+constexpr int GKV_PAGED_TICKET = 32;
 struct PagedAttendArgs {
   const void* q; const void* K; const void* V; GkvPages pages; const int32_t* len; void* out;
-  int32_t* ticket; float* partials;                      // [units][GKV_TICKETS]; [units][most][g][d + 2]
+  int32_t* ticket; float* partials;                      // [units][GKV_PAGED_TICKET]; [units][most][g][d + 2]
   int32_t most;                                          // pieces of a unit that there is room for
   int32_t splits;                                        // pieces that the launch has
-  int32_t split_iters;                                   // slices of 16 rows a piece has at least
+  int32_t split_iters, soft, long_iters;                 // as gkv_paged_pieces has them
 };
+// Pieces of a unit of n slices of 16 rows: of split_iters slices, but not more than `soft`; of long_iters slices where those are more.
+static inline int gkv_paged_pieces(int64_t n, int split_iters, int soft, int long_iters) {
+  int64_t a = (n + split_iters - 1) / split_iters, b = (n + long_iters - 1) / long_iters;
+  if (a > soft) a = soft;
+  return (int)(a > b ? a : b);
+}
 hipError_t gkv_launch_paged_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a);
 hipError_t gkv_launch_paged_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a);
 

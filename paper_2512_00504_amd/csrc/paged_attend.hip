@@ -22,12 +22,12 @@ __global__ __launch_bounds__(NWG * 64) void paged_attend_generic_kernel(GkvDims 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int d = dm.d, g = dm.g, pr = a.pages.page_rows;
-  const int unit = blockIdx.x / a.splits, sp = blockIdx.x % a.splits;
+  const int units = dm.L * dm.B * dm.Hkv, sp = blockIdx.x / units, unit = blockIdx.x % units;
   const int lb = unit / dm.Hkv, j = unit - lb * dm.Hkv, layer = lb / dm.B, i = lb - layer * dm.B;
   const int64_t room = (int64_t)a.pages.width * pr;
   const int len = (int)min((int64_t)max(a.len[i], 0), room);
   const int n_iter = (len + 15) >> 4;
-  const int ns = max(1, min(a.splits, (n_iter + a.split_iters - 1) / a.split_iters));
+  const int ns = max(1, min(a.splits, max(min((n_iter + a.split_iters - 1) / a.split_iters, a.soft), (n_iter + a.long_iters - 1) / a.long_iters)));
   if (sp >= ns) return;
   const int per = (n_iter + ns - 1) / ns;
   const int n0 = min(len, sp * per * 16), n1 = min(len, (sp + 1) * per * 16);
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(NWG * 64) void paged_attend_generic_kernel(GkvDims 
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   uint32_t arrived = 0;
   if (lane == 0)
-    arrived = __builtin_amdgcn_atomic_inc32((uint32_t*)a.ticket + (size_t)unit * GKV_TICKETS + wave, (uint32_t)ns - 1u, __ATOMIC_RELAXED, "agent");
+    arrived = __builtin_amdgcn_atomic_inc32((uint32_t*)a.ticket + ((size_t)unit * GKV_TICKETS + wave) * GKV_PAGED_TICKET, (uint32_t)ns - 1u, __ATOMIC_RELAXED, "agent");
   if ((int)__builtin_amdgcn_readfirstlane(arrived) != ns - 1) return;
   asm volatile("" ::: "memory");
   for (int hi = wave; hi < g; hi += NWG) {

@@ -13,28 +13,56 @@
 
 namespace {
 
+__device__ __forceinline__ void store_row2(float* p, const f32x2& o) { *(f32x2*)p = o; }
+__device__ __forceinline__ void store_row2(uint16_t* p, const f32x2& o) { *(uint32_t*)p = __builtin_bit_cast(uint32_t, __builtin_convertvector(o, bf16x2)); }
+
+// Maximum or sum over N = 32 or 64 neighbouring lanes, in each of them, without a trip through LDS (12 of those in a row took 0.6 us).
+template <int N, bool MAX>
+__device__ __forceinline__ float over_lanes(float x) {
+  auto with = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+  auto moved = [](float a, auto how) {
+    const int u = __float_as_int(a);
+    return __int_as_float(__builtin_amdgcn_update_dpp(u, u, decltype(how)::value, 0xf, 0xf, false));
+  };
+  x = with(x, moved(x, std::integral_constant<int, 0xb1>{}));        // lane ^ 1
+  x = with(x, moved(x, std::integral_constant<int, 0x4e>{}));        // lane ^ 2
+  x = with(x, moved(x, std::integral_constant<int, 0x141>{}));       // the other four of eight
+  x = with(x, moved(x, std::integral_constant<int, 0x140>{}));       // the other eight of sixteen
+  const uint32_t u = __float_as_uint(x);
+  const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(u, u, false, false));
+  x = with(__uint_as_float(y[0]), __uint_as_float(y[1]));
+  if (N == 64) {
+    const uint32_t v = __float_as_uint(x);
+    const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
+    x = with(__uint_as_float(z[0]), __uint_as_float(z[1]));
+  }
+  return x;
+}
+
 struct PagedArgs {
   const int32_t *len, *table;
   const char *q, *K, *V;
   char* out;
   float* partials; int32_t* ticket;
-  GkvDivisor by_splits, by_hkv, by_batch, by_iters, by_page;   // by_page: rows of a page, or slices
+  GkvDivisor by_units, by_hkv, by_batch, by_iters, by_long, by_page;   // by_page: rows of a page, or slices
   int64_t layer_bytes;                                         // K of a layer
-  int32_t splits, most, split_iters, Hq, Hkv, g, B, width, page_rows, n_pages;
+  int32_t units, splits, most, split_iters, soft, long_iters, Hq, Hkv, g, B, width, page_rows, n_pages;
   float scale_hi, scale_lo;
 };
 
-template <typename T, int D, int NW, int OCC, bool WHOLE_SLICES>
+template <typename T, int D, int NW, int KT, int OCC, bool WHOLE_SLICES>
 __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedArgs a) {
   using G = Geo<T, D>;
-  constexpr bool WHOLE = !G::F32;
+  constexpr bool WHOLE = !G::F32 && KT == 1;
+  constexpr int KEYS = 16 * KT;                                // rows of a slice
   constexpr int ROW_BYTES = G::ROW_BYTES, OSTR = G::OSTR, PSTR = G::PSTR;
   extern __shared__ __attribute__((aligned(16))) float smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, kb = lane >> 4;
   const int g = a.g, page_rows = a.page_rows, n_pages = a.n_pages;
-  const int unit = quotient(blockIdx.x, a.by_splits), sp = (int)blockIdx.x - unit * a.splits;
+  // (units first: workgroups go to the XCDs in turn, and the last pieces are those of the longest sequences only)
+  const int sp = quotient(blockIdx.x, a.by_units), unit = (int)blockIdx.x - sp * a.units;
   const int lb = quotient(unit, a.by_hkv), j = unit - lb * a.Hkv;
   const int layer = quotient(lb, a.by_batch), seq = lb - layer * a.B;
   const size_t head0 = (size_t)lb * a.Hq + j * g;
@@ -50,48 +78,70 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
 #pragma unroll
     for (int c = 0; c < G::NL; ++c) qB[c] = ld16(q_g + at + c * 64);
   }
-  const int n_tot = max(0, min(held, a.width * page_rows));
-  const int n_iter = (n_tot + 15) >> 4;
-  const int ns = max(1, min(a.splits, quotient(n_iter + a.split_iters - 1, a.by_iters)));
-  if (sp >= ns) return;
-  const int it0 = sp * NW + wave, stride = ns * NW;
-
-  // The page (or pages, a lane each) of a slice, on their way a slice ahead.
-  auto ask = [&](int it) -> int {
-    if constexpr (WHOLE_SLICES) return table[quotient(min(it, max(n_iter - 1, 0)), a.by_page)];
-    else return table[quotient(min(16 * it + r, max(n_tot - 1, 0)), a.by_page)];
+  // Pages of a slice, of each 16 rows or a lane each, on their way a slice ahead, the first ones' together with the length: where that ends is
+  // not known then, where the table does is.
+  const int it_first = sp * NW + wave;                         // (of any number of pieces)
+  struct Pages { int of[KT]; };
+  auto ask = [&](int it) {
+    Pages p;
+#pragma unroll
+    for (int t = 0; t < KT; ++t) p.of[t] = table[min(quotient(WHOLE_SLICES ? it * KT + t : it * KEYS + 16 * t + r, a.by_page), a.width - 1)];
+    return p;
   };
-  Slice<T, D, 1> s;
-  uint32_t missing = 0;                                        // rows of the slice whose pages are not there, a bit each (their loads go to page 0)
-  uint32_t k_off = r * ROW_BYTES + kb * 16, v_off = kb * 4 * ROW_BYTES + r * (G::VW == 2 ? 8 : 16);
-  asm volatile("" : "+v"(k_off), "+v"(v_off));                 // (offsets stay offsets)
-  auto request = [&](int it, int page) {
-    if constexpr (WHOLE_SLICES) {
-      page = __builtin_amdgcn_readfirstlane(page);
-      const bool there = (uint32_t)page < (uint32_t)n_pages;
-      missing = there ? 0u : 0xffffu;
-      const int in_page = it * 16 - quotient(it, a.by_page) * page_rows;
-      int64_t at = (((int64_t)(there ? page : 0) * a.Hkv + j) * page_rows + in_page) * ROW_BYTES;
-      asm volatile("" : "+s"(at));                             // (and bases scalar)
-      const char *Kt = K + at, *Vt = V + at;
+  const Pages pages0 = ask(it_first);
+  const int n_tot = max(0, min(held, a.width * page_rows));
+  const int n_tiles = (n_tot + 15) >> 4, n_iter = (int)((uint32_t)(n_tot + KEYS - 1) / KEYS);
+  const int ns = max(1, min(a.splits, max(min(quotient(n_tiles + a.split_iters - 1, a.by_iters), a.soft), quotient(n_tiles + a.long_iters - 1, a.by_long))));
+  if (sp >= ns) return;
+  const int it0 = it_first, stride = ns * NW;
+
+  // Where a slice's rows are, from its page or pages.  missing: rows whose pages are not there, a bit each (their loads go to page 0).
+  struct Place { int64_t at[KT]; uint32_t k_row[KT], v_row[KT][4], missing; };
+  auto locate = [&](int it, const Pages& p) {
+    Place w;
+    w.missing = 0;
 #pragma unroll
-      for (int c = 0; c < G::NL; ++c) s.kA[0][c] = ld16(Kt + k_off + c * 64);
+    for (int t = 0; t < KT; ++t) {
+      if constexpr (WHOLE_SLICES) {
+        const int tile = KT == 1 ? it : min(it * KT + t, n_tiles - 1), page = __builtin_amdgcn_readfirstlane(p.of[t]);
+        const bool there = (uint32_t)page < (uint32_t)n_pages;
+        if (!there && (KT == 1 || it * KT + t < n_tiles)) w.missing |= 0xffffu << (16 * t);
+        const int in_page = tile * 16 - quotient(tile, a.by_page) * page_rows;
+        w.at[t] = (((int64_t)(there ? page : 0) * a.Hkv + j) * page_rows + in_page) * ROW_BYTES;
+      } else {
+        const int at = it * KEYS + 16 * t + r, n = min(at, n_tot - 1);
+        const bool there = (uint32_t)p.of[t] < (uint32_t)n_pages && at < n_tot;
+        w.missing |= ((uint32_t)__ballot(!there && at < n_tot) & 0xffffu) << (16 * t);
+        w.k_row[t] = there ? ((uint32_t)p.of[t] * (uint32_t)a.Hkv + (uint32_t)j) * (uint32_t)page_rows + (uint32_t)(n - quotient(n, a.by_page) * page_rows) : 0u;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) ld_v<T, D>(s.vR[e], Vt + v_off + e * ROW_BYTES);
-    } else {
-      const int n = min(16 * it + r, n_tot - 1);
-      const bool there = (uint32_t)page < (uint32_t)n_pages;
-      missing = (uint32_t)__ballot(!there) & 0xffffu;
-      const uint32_t row = there ? ((uint32_t)page * (uint32_t)a.Hkv + (uint32_t)j) * (uint32_t)page_rows + (uint32_t)(n - quotient(n, a.by_page) * page_rows) : 0u;
-      const char* Kt = K + (uint64_t)row * ROW_BYTES + kb * 16;
-#pragma unroll
-      for (int c = 0; c < G::NL; ++c) s.kA[0][c] = ld16(Kt + c * 64);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t v_row = (uint32_t)__shfl((int)row, 4 * kb + e);
-        ld_v<T, D>(s.vR[e], V + (uint64_t)v_row * ROW_BYTES + r * (G::VW == 2 ? 8 : 16));
+        for (int e = 0; e < 4; ++e) w.v_row[t][e] = (uint32_t)__shfl((int)w.k_row[t], 4 * kb + e);
       }
     }
+    return w;
+  };
+  uint32_t k_off = r * ROW_BYTES + kb * 16, v_off = kb * 4 * ROW_BYTES + r * (G::VW == 2 ? 8 : 16);
+  asm volatile("" : "+v"(k_off), "+v"(v_off));                 // (offsets stay offsets)
+  auto request = [&](Slice<T, D, KT>& s, Place w) {
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      if constexpr (WHOLE_SLICES) {
+        asm volatile("" : "+s"(w.at[t]));                      // (and bases scalar)
+        const char* Kt = K + w.at[t];
+#pragma unroll
+        for (int c = 0; c < G::NL; ++c) s.kA[t][c] = ld16(Kt + k_off + c * 64);
+      } else {
+        const char* Kt = K + (uint64_t)w.k_row[t] * ROW_BYTES + kb * 16;
+#pragma unroll
+        for (int c = 0; c < G::NL; ++c) s.kA[t][c] = ld16(Kt + c * 64);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (WHOLE_SLICES) ld_v<T, D>(s.vR[4 * t + e], V + w.at[t] + v_off + e * ROW_BYTES);
+        else ld_v<T, D>(s.vR[4 * t + e], V + (uint64_t)w.v_row[t][e] * ROW_BYTES + r * (G::VW == 2 ? 8 : 16));
+      }
   };
   Running<G::NC> st;
   auto reset = [&]() {
@@ -101,28 +151,31 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
     for (int m = 0; m < G::NC; ++m) st.oacc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
   };
   reset();
-  auto process = [&](int it, bool last) {
-    process_slice<T, D, 1, false, WHOLE>(s, st, qB, it, false, last, a.scale_hi, a.scale_lo, r, kb, [&](int row) { return row >= n_tot; }, Nothing{});
+  auto process = [&](Slice<T, D, KT>& s, int it, bool last) {
+    process_slice<T, D, KT, false, WHOLE>(s, st, qB, it, false, last, a.scale_hi, a.scale_lo, r, kb, [&](int row) { return row >= n_tot; }, Nothing{});
   };
   if (it0 < n_iter) {
-    int page = ask(it0);
-    request(it0, page);
-    page = ask(it0 + stride);
-    uint32_t any_missing = missing;
+    Slice<T, D, KT> s0;
+    Pages next = ask(it0 + stride);
+    Place w = locate(it0, pages0);
+    request(s0, w);
+    uint32_t any_missing = w.missing;
     int it = it0;
     for (; it + stride < n_iter; it += stride) {
-      process(it, false);
+      // the next slice's place is known before this one is there, and the one's after that is asked for
+      w = locate(it + stride, next);
+      next = ask(it + 2 * stride);
+      any_missing |= w.missing;
+      process(s0, it, false);
       __builtin_amdgcn_sched_barrier(0);                       // (requests that move up between the products need registers of their own)
-      request(it + stride, page);
-      any_missing |= missing;
-      page = ask(it + 2 * stride);
+      request(s0, w);
       asm volatile("; next slice");                            // (the same requests ahead of the loop stay apart from these)
     }
-    process(it, it == n_iter - 1);
+    process(s0, it, it == n_iter - 1);
     // Seldom: a page that is not there, a maximum that the short form of the weights is not right for, or a NaN that may be its doing or that
     // of an infinite value and a part of P that is zero.  The slices are gone through again.
     bool again = any_missing != 0 || fabsf(st.m_run) >= GKV_HUGE_LOG2 || st.l_run != st.l_run;
-    if constexpr (WHOLE) {
+    if constexpr (!G::F32) {
       float x = st.l_run;
 #pragma unroll
       for (int m = 0; m < G::NC; ++m)
@@ -134,9 +187,10 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
     if (__any(again)) {
       reset();
       for (int it = it0; it < n_iter; it += stride) {
-        request(it, ask(it));
-        process_slice<T, D, 1, true, WHOLE>(s, st, qB, it, false, true, a.scale_hi, a.scale_lo, r, kb,
-                                            [&](int row) { return row >= n_tot || (missing >> (row & 15)) & 1; }, Nothing{});
+        w = locate(it, ask(it));
+        request(s0, w);
+        process_slice<T, D, KT, true, WHOLE>(s0, st, qB, it, false, true, a.scale_hi, a.scale_lo, r, kb,
+                                            [&](int row) { return row >= n_tot || (w.missing >> (row & (KEYS - 1))) & 1; }, Nothing{});
       }
     }
   }
@@ -158,19 +212,20 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
     }
     if (kb == 0) { sm[r * NW + wave] = st.m_run; sl[r * NW + wave] = l_tot; }
   }
-  constexpr int TPH = D / 4;                // threads per head
+  constexpr int TPH = D / 2;                // threads per head: two channels each
   __syncthreads();
 
   T* out = (T*)a.out + head0 * D;
-  float* part = a.partials + (size_t)unit * a.most * g * PSTR;        // [ns][g][PSTR]
-  auto finish = [&](int x, float L, f32x4 o) {
+  float* part = a.partials + (size_t)unit * a.most * g * PSTR;        // outputs [most][g][D], then maximum and sum [g][most]
+  float* part_ms = part + (size_t)a.most * g * D;
+  auto finish = [&](int x, float L, f32x2 o) {
     bool any = false;
     if (L == 0.f)                                              // seldom: no row, or none with weight
       for (int p = 0; p * page_rows < n_tot; ++p) any |= (uint32_t)table[p] < (uint32_t)n_pages;
-    store_row4(out + (uint32_t)(x * 4), o * inv_sum(L, any, false));
+    store_row2(out + (uint32_t)(x * 2), o * inv_sum(L, any, false));
   };
   for (int x = tid; x < g * TPH; x += NW * 64) {
-    const int h = x / TPH, c4 = (x % TPH) * 4;
+    const int h = x / TPH, c = (x % TPH) * 2;
     float mw[NW], lw[NW];
 #pragma unroll
     for (int i = 0; i < NW / 4; ++i) {
@@ -182,20 +237,18 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
 #pragma unroll
     for (int wv = 0; wv < NW; ++wv) M = fmaxf(M, mw[wv]);
     float Lsum = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    f32x2 o = {0.f, 0.f};
 #pragma unroll
     for (int wv = 0; wv < NW; ++wv) {
       const float f = __builtin_amdgcn_exp2f(mw[wv] - M);
       Lsum += lw[wv] * f;
-      o += *(const f32x4*)(so + (wv * g + h) * OSTR + c4) * f;
+      o += *(const f32x2*)(so + (wv * g + h) * OSTR + c) * f;
     }
     if (ns == 1) {
       finish(x, Lsum, o);
     } else {
-      float* ph = part + (uint32_t)((sp * g + h) * PSTR);
-      store_agent(ph + c4, o[0], o[1]);
-      store_agent(ph + c4 + 2, o[2], o[3]);
-      if (c4 == 0) store_agent(ph + D, M, Lsum);
+      store_agent(part + (uint32_t)((sp * g + h) * D + c), o[0], o[1]);
+      if (c == 0) store_agent(part_ms + (uint32_t)((h * a.most + sp) * 2), M, Lsum);
     }
   }
   if (ns == 1 || wave * 64 >= g * TPH) return;
@@ -205,38 +258,39 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
   // Partial results go through memory with agent-scope accesses, each wavefront waits for its own stores, and its ticket follows.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   uint32_t arrived = 0;
-  if (lane == 0) arrived = __builtin_amdgcn_atomic_inc32((uint32_t*)a.ticket + (size_t)unit * GKV_TICKETS + wave, (uint32_t)ns - 1u, __ATOMIC_RELAXED, "agent");
+  if (lane == 0)
+    arrived = __builtin_amdgcn_atomic_inc32((uint32_t*)a.ticket + ((size_t)unit * GKV_TICKETS + wave) * GKV_PAGED_TICKET, (uint32_t)ns - 1u, __ATOMIC_RELAXED, "agent");
   if ((int)__builtin_amdgcn_readfirstlane(arrived) != ns - 1) return;
   asm volatile("" ::: "memory");
-  for (int x = tid; x < g * TPH; x += NW * 64) {
-    const int h = x / TPH, c4 = (x % TPH) * 4;
+  // A lane has maximum and sum of one piece and makes its factor, so all outputs can be asked for at once.  A wavefront has one head (D = 128) or two.
+  constexpr int AT_A_TIME = TPH, AT_ONCE = 16;
+  for (int x = tid; x < g * TPH; x += NW * 64) {               // (the same for the lanes of a head)
+    const int h = x / TPH, c = (x % TPH) * 2, in_head = lane % TPH, lane0 = lane - in_head;
     float M = GKV_NO_MAX, Lsum = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    constexpr int AT_ONCE = 8;
-    for (int s0 = 0; s0 < ns; s0 += AT_ONCE) {
-      float2 got[AT_ONCE][3];
-      const float* ph = part + (size_t)(s0 * g + h) * PSTR;
+    f32x2 o = {0.f, 0.f};
+    float2 got[AT_ONCE];
+    auto ask_for = [&](int s1) {
 #pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i)
-        if (s0 + i < ns) {                                   // uniform, here and below
-          got[i][0] = load_agent(ph + D); got[i][1] = load_agent(ph + c4); got[i][2] = load_agent(ph + c4 + 2);
-          ph += (uint32_t)(g * PSTR);
-        }
-      float Mn = M;
-#pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i)
-        if (s0 + i < ns) Mn = fmaxf(Mn, got[i][0].x);
-      const float f0 = __builtin_amdgcn_exp2f(M - Mn);
+      for (int i = 0; i < AT_ONCE; ++i) got[i] = load_agent(part + (uint32_t)((min(s1 + i, ns - 1) * g + h) * D + c));
+    };
+    for (int s0 = 0; s0 < ns; s0 += AT_A_TIME) {
+      float2 ms = load_agent(part_ms + (uint32_t)((h * a.most + min(s0 + in_head, ns - 1)) * 2));
+      ask_for(s0);
+      if (s0 + in_head >= ns) ms = make_float2(GKV_NO_MAX, 0.f);
+      const float Mn = fmaxf(M, over_lanes<TPH, true>(ms.x));
+      const float f = __builtin_amdgcn_exp2f(ms.x - Mn), f0 = __builtin_amdgcn_exp2f(M - Mn);
       M = Mn;
-      Lsum *= f0;
+      Lsum = Lsum * f0 + over_lanes<TPH, false>(ms.y * f);
       o *= f0;
+      for (int s1 = s0; s1 < min(ns, s0 + AT_A_TIME); s1 += AT_ONCE) {
+        if (s1 > s0) ask_for(s1);
 #pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i)
-        if (s0 + i < ns) {
-          const float f = __builtin_amdgcn_exp2f(got[i][0].x - Mn);
-          Lsum += got[i][0].y * f;
-          o += f32x4{got[i][1].x, got[i][1].y, got[i][2].x, got[i][2].y} * f;
+        for (int i = 0; i < AT_ONCE; ++i) {
+          const int from = (s1 + i - s0) & (TPH - 1);
+          const float fi = TPH == 64 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), from)) : __shfl(f, lane0 + from);
+          if (s1 + i < ns) o += f32x2{got[i].x, got[i].y} * fi;
         }
+      }
     }
     finish(x, Lsum, o);
   }
@@ -244,31 +298,30 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
 
 size_t lds_bytes(const GkvDims& dm, int waves) { return sizeof(float) * waves * ((size_t)dm.g * (dm.d + 4) + 2 * 16); }
 
-template <typename T, int D, int NW, int OCC>
+template <typename T, int D, int NW, int KT, int OCC>
 hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const PagedAttendArgs& a) {
   const bool whole = a.pages.page_rows % 16 == 0;
   PagedArgs k;
   k.len = a.len; k.table = a.pages.table;
   k.q = (const char*)a.q; k.K = (const char*)a.K; k.V = (const char*)a.V; k.out = (char*)a.out;
   k.partials = a.partials; k.ticket = a.ticket;
-  k.by_splits = gkv_divisor(a.splits); k.by_hkv = dm.by_hkv; k.by_batch = gkv_divisor(dm.B); k.by_iters = gkv_divisor(a.split_iters);
+  k.units = dm.L * dm.B * dm.Hkv; k.by_units = gkv_divisor(k.units); k.by_hkv = dm.by_hkv; k.by_batch = gkv_divisor(dm.B); k.by_iters = gkv_divisor(a.split_iters); k.by_long = gkv_divisor(a.long_iters);
   k.by_page = gkv_divisor(whole ? a.pages.page_rows / 16 : a.pages.page_rows);
   k.layer_bytes = (int64_t)a.pages.n_pages * dm.Hkv * a.pages.page_rows * Geo<T, D>::ROW_BYTES;
-  k.splits = a.splits; k.most = a.most; k.split_iters = a.split_iters;
+  k.splits = a.splits; k.most = a.most; k.split_iters = a.split_iters; k.soft = a.soft; k.long_iters = a.long_iters;
   k.Hq = dm.Hq; k.Hkv = dm.Hkv; k.g = dm.g; k.B = dm.B;
   k.width = a.pages.width; k.page_rows = a.pages.page_rows; k.n_pages = a.pages.n_pages;
   k.scale_hi = dm.scale_l2_hi; k.scale_lo = dm.scale_l2_lo;
-  auto kern = whole ? paged_attend_mfma_kernel<T, D, NW, OCC, true> : paged_attend_mfma_kernel<T, D, NW, OCC, false>;
+  auto kern = whole ? paged_attend_mfma_kernel<T, D, NW, KT, OCC, true> : paged_attend_mfma_kernel<T, D, NW, KT, OCC, false>;
   return gkv_launch(ln, kern, dim3(dm.L * dm.B * dm.Hkv * a.splits), dim3(NW * 64), lds_bytes(dm, NW), k);
 }
 
 }  // namespace
 
 hipError_t gkv_launch_paged_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a) {
-  if (lds_bytes(dm, 8) > GKV_LDS_LIMIT) {                    // d = 128, g = 16
-    if (dtype == GKV_F32) return launch<float, 128, 4, 2>(ln, dm, a);
-    return launch<uint16_t, 128, 4, 4>(ln, dm, a);
-  }
-  if (dtype == GKV_F32) return dm.d == 64 ? launch<float, 64, 8, 4>(ln, dm, a) : launch<float, 128, 8, 2>(ln, dm, a);
-  return dm.d == 64 ? launch<uint16_t, 64, 8, 4>(ln, dm, a) : launch<uint16_t, 128, 8, 4>(ln, dm, a);
+  const bool f32 = dtype == GKV_F32;
+  if (dm.d == 64) return f32 ? launch<float, 64, 8, 1, 4>(ln, dm, a) : launch<uint16_t, 64, 8, 2, 4>(ln, dm, a);
+  if (lds_bytes(dm, 8) > GKV_LDS_LIMIT)                      // g = 16
+    return f32 ? launch<float, 128, 4, 1, 2>(ln, dm, a) : launch<uint16_t, 128, 4, 1, 4>(ln, dm, a);
+  return f32 ? launch<float, 128, 8, 1, 2>(ln, dm, a) : launch<uint16_t, 128, 8, 1, 4>(ln, dm, a);
 }
