@@ -197,7 +197,7 @@ def _load_call():
                           "`python -c 'import __graft_entry__ as g; g.build()'`", RuntimeWarning, stacklevel=3)
             _call = _LeavesAllToCtypes()
             return _call
-        for name in dir(_gkv_call):
+        for name in [*dir(_gkv_call), "gkv_rotate", "gkv_paged_append", "gkv_paged_attend_decode", "gkv_paged_advance"]:
             if name.startswith("gkv_"):
                 _gkv_call.bind(name, ctypes.cast(getattr(lib, name), c_void_p).value)
         _call = _gkv_call
@@ -219,7 +219,8 @@ class Context:
         self._call = _load_call()
         self._params, self._step_base, self._profiled, self._parts = {}, None, False, {}
         import torch
-        self._dtype, self._int32, self._paged_bytes = (torch.float32, torch.bfloat16)[cfg.dtype], torch.int32, None
+        self._spec = GkvConfig.from_buffer_copy(cfg)           # as the library has it
+        self._spec_at, self._dtype, self._paged_bytes = ctypes.addressof(self._spec), (torch.float32, torch.bfloat16)[cfg.dtype], None
         self._prefix_bytes, self._prefix_rows = {}, -1       # rows -> size of a buffer for them; the most rows asked for
 
     def part(self, sequences: int) -> "Context":
@@ -429,7 +430,7 @@ class Context:
         """A tensor [L, tokens, heads, d] as the calls take it: itself and 0, or, where tokens lie apart, its address and the elements between them."""
         if t is None:
             return None, 0
-        L, d = self.cfg.n_layers, self.cfg.head_dim
+        L, d = self._spec.n_layers, self._spec.head_dim
         if t.shape != (L, tokens, heads, d) or t.dtype is not self._dtype:
             raise ValueError(f"gkv: {what} has to be [{L}, {tokens}, {heads}, {d}] of {self._dtype}, not {list(t.shape)} of {t.dtype}")
         if t.is_contiguous():
@@ -440,12 +441,11 @@ class Context:
                 or not heads * d <= stride < 1 << 31):
             raise ValueError(f"gkv: {what}'s heads have to lie side by side and its layers one behind the other" if apart
                              else f"gkv: {what} must be contiguous")
-        _ptr_here(t, False)
-        return t.data_ptr(), stride
+        return _ptr_here(t, False), stride
 
     def _pages(self, page_table, d_len, K, V):
         """Shapes of a paged cache: pages of a sequence, rows of a page, pages."""
-        cfg = self.cfg
+        cfg = self._spec
         if K.dim() != 5 or (K.shape[0], K.shape[2], K.shape[4]) != (cfg.n_layers, cfg.n_kv_heads, cfg.head_dim) or V.shape != K.shape:
             raise ValueError(f"gkv: K and V have to be [{cfg.n_layers}, pages, {cfg.n_kv_heads}, rows, {cfg.head_dim}]")
         if K.dtype is not self._dtype or V.dtype is not self._dtype:
@@ -456,64 +456,80 @@ class Context:
         self._ints(d_len, (cfg.batch,), "d_len")
         return page_table.shape[1], K.shape[3], K.shape[1]
 
-    def _ints(self, t, shape, what):
-        if t.shape != shape or t.dtype is not self._int32:
+    def _ints(self, t, shape, what, may_be_none=False):
+        import torch
+        if t is None and may_be_none:
+            return
+        if t.shape != shape or t.dtype is not torch.int32:
             raise ValueError(f"gkv: {what} has to be int32 {list(shape)}, not {t.dtype} {list(t.shape)}")
 
-    # rotary positions: q, k [L, tokens, heads, d], slices of one projection's output too; rotary: a Rotary
+    def _freq(self, rotary):
+        import torch
+        if rotary.freq.dtype is not torch.float64 or rotary.freq.numel() < rotary.dim // 2:
+            raise ValueError(f"gkv: frequencies have to be float64 [{rotary.dim // 2}]")
+
+    # Rotary positions: q, k [L, tokens, heads, d], slices of one projection's output too; rotary: a Rotary.
+    # Paged cache: K, V [L, n_pages, h_kv, page_rows, d], page_table int32 [B, table_width], d_len int32 [B].
+    # The native half takes what has the right shapes, types and device; the rest is refused here, or goes through ctypes.
     def rotate(self, q, k, positions, step, rotary, q_out, k_out, transposed=False):
-        cfg = self.cfg
+        r = rotary
+        st = self._call.rotate(self._handle, self._spec_at, q, k, positions, step, r.freq, r.dim, r.layout, r.amplitude, int(transposed), q_out, k_out)
+        if st is None:
+            st = self._rotate(q, k, positions, step, r, q_out, k_out, transposed)
+        if st:
+            raise GkvError(st, "gkv_rotate")
+
+    def _rotate(self, q, k, positions, step, r, q_out, k_out, transposed):
+        cfg = self._spec
+        if q is None and k is None:
+            raise GkvError(1, "gkv_rotate")
         tokens = (k if q is None else q).shape[1]
         (q, qs), (k, ks) = self._heads(q, tokens, cfg.n_q_heads, "q"), self._heads(k, tokens, cfg.n_kv_heads, "k")
         q_out, _ = self._heads(q_out, tokens, cfg.n_q_heads, "q_out", False)
         k_out, _ = self._heads(k_out, tokens, cfg.n_kv_heads, "k_out", False)
-        if positions is not None:
-            self._ints(positions, (tokens,), "positions")
+        self._ints(positions, (tokens,), "positions", True)
+        self._freq(r)
         if tokens == 0:
-            return
-        r = rotary
-        st = self._call.gkv_rotate(self._handle, q, qs, k, ks, tokens, positions, step, r.freq, r.dim, r.layout, r.amplitude, int(transposed),
-                                   q_out, k_out)
-        if st is None:
-            st = self.lib.gkv_rotate(self.h, _ptr_here(q), qs, _ptr_here(k), ks, tokens, _ptr_here(positions), step, _ptr_here(r.freq), r.dim,
-                                     r.layout, r.amplitude, int(transposed), _ptr_here(q_out), _ptr_here(k_out), _stream())
-        if st:
-            raise GkvError(st, "gkv_rotate")
+            return 0
+        return self.lib.gkv_rotate(self.h, _ptr_here(q), qs, _ptr_here(k), ks, tokens, _ptr_here(positions), step, _ptr_here(r.freq), r.dim, r.layout,
+                                   r.amplitude, int(transposed), _ptr_here(q_out), _ptr_here(k_out), _stream())
 
-    # paged cache: K, V [L, n_pages, h_kv, page_rows, d], page_table int32 [B, table_width], d_len int32 [B]
     def paged_advance(self, d_len, d_start):
-        self._ints(d_len, (self.cfg.batch,), "d_len")
-        if d_start is not None:
-            self._ints(d_start, (self.cfg.batch + 1,), "d_start")
-        st = self._call.gkv_paged_advance(self._handle, d_len, d_start)
+        st = self._call.paged_advance(self._handle, self._spec_at, d_len, d_start)
         if st is None:
+            self._ints(d_len, (self._spec.batch,), "d_len")
+            self._ints(d_start, (self._spec.batch + 1,), "d_start", True)
             st = self.lib.gkv_paged_advance(self.h, _ptr_here(d_len), _ptr_here(d_start), _stream())
         if st:
             raise GkvError(st, "gkv_paged_advance")
 
     def paged_append(self, q, k, v, d_start, d_len, positions, rotary, page_table, K, V, q_out):
         """rotary: a Rotary, or None where keys are turned already (q and q_out are None then)."""
-        cfg = self.cfg
+        freq, dim, layout, amplitude = (None, 0, 0, 1.0) if rotary is None else (rotary.freq, rotary.dim, rotary.layout, rotary.amplitude)
+        st = self._call.paged_append(self._handle, self._spec_at, q, k, v, d_start, positions, freq, dim, layout, amplitude, d_len, page_table, K, V, q_out)
+        if st is None:
+            st = self._paged_append(q, k, v, d_start, d_len, positions, rotary, freq, dim, layout, amplitude, page_table, K, V, q_out)
+        if st:
+            raise GkvError(st, "gkv_paged_append")
+
+    def _paged_append(self, q, k, v, d_start, d_len, positions, rotary, freq, dim, layout, amplitude, page_table, K, V, q_out):
+        cfg = self._spec
+        if k is None or v is None:
+            raise GkvError(1, "gkv_paged_append")
         tokens = k.shape[1]
         (q, qs), (k, ks), (v, vs) = (self._heads(q, tokens, cfg.n_q_heads, "q"), self._heads(k, tokens, cfg.n_kv_heads, "k"),
                                      self._heads(v, tokens, cfg.n_kv_heads, "v"))
         q_out, _ = self._heads(q_out, tokens, cfg.n_q_heads, "q_out", False)
-        if d_start is not None:
-            self._ints(d_start, (cfg.batch + 1,), "d_start")
-        if positions is not None:
-            self._ints(positions, (tokens,), "positions")
+        self._ints(d_start, (cfg.batch + 1,), "d_start", True)
+        self._ints(positions, (tokens,), "positions", True)
+        if rotary is not None:
+            self._freq(rotary)
         width, rows, pages = self._pages(page_table, d_len, K, V)
         if tokens == 0:
-            return
-        freq, dim, layout, amplitude = (None, 0, 0, 1.0) if rotary is None else (rotary.freq, rotary.dim, rotary.layout, rotary.amplitude)
-        st = self._call.gkv_paged_append(self._handle, q, qs, k, ks, v, vs, tokens, d_start, d_len, positions, freq, dim, layout, amplitude,
-                                         page_table, width, rows, pages, K, V, q_out)
-        if st is None:
-            st = self.lib.gkv_paged_append(self.h, _ptr_here(q), qs, _ptr_here(k), ks, _ptr_here(v), vs, tokens, _ptr_here(d_start),
-                                           _ptr_here(d_len), _ptr_here(positions), _ptr_here(freq), dim, layout, amplitude,
-                                           _ptr_here(page_table), width, rows, pages, _ptr_here(K), _ptr_here(V), _ptr_here(q_out), _stream())
-        if st:
-            raise GkvError(st, "gkv_paged_append")
+            return 0
+        return self.lib.gkv_paged_append(self.h, _ptr_here(q), qs, _ptr_here(k), ks, _ptr_here(v), vs, tokens, _ptr_here(d_start), _ptr_here(d_len),
+                                         _ptr_here(positions), _ptr_here(freq), dim, layout, amplitude, _ptr_here(page_table), width, rows, pages,
+                                         _ptr_here(K), _ptr_here(V), _ptr_here(q_out), _stream())
 
     def paged_workspace_bytes(self) -> int:
         if self._paged_bytes is None:
@@ -524,18 +540,22 @@ class Context:
 
     def paged_attend_decode(self, q, K, V, page_table, d_len, len_max_host, out, workspace):
         """Refuses a workspace that is too small, which the C call cannot tell."""
-        cfg = self.cfg
-        if workspace is not None and workspace.numel() * workspace.element_size() < self.paged_workspace_bytes():
-            raise GkvError(GKV_ERR_WORKSPACE, "gkv_paged_attend_decode")
+        need = self._paged_bytes or self.paged_workspace_bytes()
+        st = self._call.paged_attend_decode(self._handle, self._spec_at, q, d_len, page_table, K, V, len_max_host, out, workspace, need)
+        if st is None:
+            st = self._paged_attend_decode(q, K, V, page_table, d_len, len_max_host, out, workspace, need)
+        if st:
+            raise GkvError(st, "gkv_paged_attend_decode")
+
+    def _paged_attend_decode(self, q, K, V, page_table, d_len, len_max_host, out, workspace, need):
+        cfg = self._spec
+        if workspace is not None and workspace.numel() * workspace.element_size() < need:
+            return GKV_ERR_WORKSPACE
         q, _ = self._heads(q, cfg.batch, cfg.n_q_heads, "q", False)
         out, _ = self._heads(out, cfg.batch, cfg.n_q_heads, "out", False)
         width, rows, pages = self._pages(page_table, d_len, K, V)
-        st = self._call.gkv_paged_attend_decode(self._handle, q, K, V, page_table, width, rows, pages, d_len, len_max_host, out, workspace)
-        if st is None:
-            st = self.lib.gkv_paged_attend_decode(self.h, _ptr_here(q), _ptr_here(K), _ptr_here(V), _ptr_here(page_table), width, rows, pages,
-                                                  _ptr_here(d_len), len_max_host, _ptr_here(out), _ptr_here(workspace), _stream())
-        if st:
-            raise GkvError(st, "gkv_paged_attend_decode")
+        return self.lib.gkv_paged_attend_decode(self.h, _ptr_here(q), _ptr_here(K), _ptr_here(V), _ptr_here(page_table), width, rows, pages,
+                                                _ptr_here(d_len), len_max_host, _ptr_here(out), _ptr_here(workspace), _stream())
 
     def profile_enable(self, on: bool):
         self._check(self.lib.gkv_profile_enable(self.h, int(on)), "gkv_profile_enable")

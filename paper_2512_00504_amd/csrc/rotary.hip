@@ -6,8 +6,11 @@
 // 64 bits; what is left, within +-pi/4, takes a Taylor polynomial in 32 (remainders 2^-29 and 2^-33).  Products and sums are in 32 bits,
 // rounded once to the type.
 //
-// Bound: memory, two passes over the data and nothing else of size.  A workgroup has the cosines and sines of its tokens in LDS, made
-// once for all heads (an angle is some 40 instructions, a turned pair 6), while its first loads are on their way.
+// Bound: memory, each element read and written once.  A workgroup has the cosines and sines of its tokens in LDS, made once for all
+// heads (an angle is some 40 instructions, a turned pair 6), while its first loads are on their way.  Neighbouring lanes have neighbouring 16
+// bytes in every load and store, and stores are non-temporal: 32749 tokens of 40 and 8 heads, three quarters of 128 channels interleaved, 805 MB, 162 us
+// with two neighbouring pieces a lane, 142 so, 131 with those stores (6.1 TB/s, where a copy of 1 GiB makes 5.1; non-temporal loads as well 10% slower); appends
+// of 67 MB 14.5 -> 11.8, of 625 MB 113 -> 107.
 #include "gkv_internal.h"
 
 namespace {
@@ -16,7 +19,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int THREADS = 256, AT_ONCE = 4, MOST_TOKENS = 8;   // of a workgroup; items a thread has on their way; tokens of a workgroup
+constexpr int THREADS = 256, AT_ONCE = 2, MOST_TOKENS = 32;   // of a workgroup; items a thread has on their way; tokens of a workgroup
 
 // cos and sin of position * freq, times m.
 __device__ __forceinline__ float2 turn(double freq, int position, float m, int transposed) {
@@ -39,14 +42,14 @@ template <typename T, int PIECE> struct Piece;
 template <> struct Piece<float, 4> {
   u32x4 w;
   __device__ __forceinline__ void load(const float* p) { w = *(const u32x4*)p; }
-  __device__ __forceinline__ void store(float* p) const { *(u32x4*)p = w; }
+  __device__ __forceinline__ void store(float* p) const { __builtin_nontemporal_store(w, (u32x4*)p); }
   __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
   __device__ __forceinline__ void set2(int i, float a, float b) { w[i] = __float_as_uint(a); w[i + 1] = __float_as_uint(b); }
 };
 template <> struct Piece<uint16_t, 8> {
   u32x4 w;
   __device__ __forceinline__ void load(const uint16_t* p) { w = *(const u32x4*)p; }
-  __device__ __forceinline__ void store(uint16_t* p) const { *(u32x4*)p = w; }
+  __device__ __forceinline__ void store(uint16_t* p) const { __builtin_nontemporal_store(w, (u32x4*)p); }
   __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
   __device__ __forceinline__ void set2(int i, float a, float b) {
     w[i >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
@@ -82,7 +85,8 @@ __device__ __forceinline__ Place place_of(int t, const int32_t* start, const int
   return Place{seq, (int64_t)len[seq] - ((int64_t)end - t)};
 }
 
-// An item is two pieces of a row: of its turned channels the two halves of some pairs (half layout), else neighbours.
+// An item is two pieces of a row: of its turned channels the two halves of some pairs (half layout), of the others, and in the interleaved layout,
+// one of the first half and one of the second, so that lanes have neighbours.
 //   VECTOR: pieces of 16 bytes, of which dim/2 (half layout) or dim (interleaved) has to be a whole number; else of one element.
 // Dynamic LDS: float2 angles[per_group][dim/2].
 template <typename T, bool VECTOR, bool HALF, bool APPEND>
@@ -110,11 +114,12 @@ __global__ __launch_bounds__(THREADS) void rotate_kernel(GkvDims dm, Args a) {
     const bool turns = it.slot < hq + hk;                     // (a row of v does not)
     if constexpr (HALF) {
       it.turned0 = it.turned1 = turns && it.i < in_half;
-      it.p0 = it.turned0 ? it.i : 2 * it.i;
-      it.p1 = it.turned0 ? it.i + in_half : 2 * it.i + 1;
+      const int first = turns ? in_half : 0;                 // the others: pieces from 2 first on, those of the first half of them and of the second
+      it.p0 = it.turned0 ? it.i : first + it.i;
+      it.p1 = it.turned0 ? it.i + in_half : per_head + it.i;
     } else {
-      it.p0 = 2 * it.i;
-      it.p1 = it.p0 + 1;
+      it.p0 = VECTOR ? it.i : 2 * it.i;
+      it.p1 = VECTOR ? it.i + per_head : 2 * it.i + 1;
       it.turned0 = turns && it.p0 * E < dim;
       it.turned1 = turns && it.p1 * E < dim;
     }
@@ -238,7 +243,13 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, Args a) {
   const int pieces = dm.d / (vector ? E : 1), per_head = (pieces + 1) / 2;
   const int heads = (a.in.q ? dm.Hq : 0) + (a.in.k ? dm.Hkv : 0) * (APPEND ? 2 : 1);
   const int64_t rows = (int64_t)dm.L * a.in.tokens;
-  a.per_group = rows >= 8 * 2048 ? 8 : rows >= 2 * 2048 ? 2 : 1;
+  // Tokens of a workgroup: 512 items, two for each thread, where that leaves a workgroup for every CU.  us, by tokens (items of one): 32749 tokens of 40
+  // and 8 heads (384) 1 / 2 / 4 131 / 139 / 146; 2048 appended of 28, 4 and 4 (288) 7.7 / 6.6 / 7.4; 64 in 36 layers of 40, 8 and 8 (448) 11.8 / 11.2 / 12.1;
+  // fp32, 8168 in 4 layers of 2 and 2, d = 64 (32) 4 / 8 / 16 / 32 18.8 / 14.0 / 13.0 / 13.1; 8 in 28 layers of 28 and 4 (256) 1 / 2 / 4 3.7 / 4.0 / 4.7.
+  const int64_t of_one = (int64_t)heads * per_head, wanted = (512 + of_one / 2) / of_one, most = rows / 256;
+  a.per_group = (int)(wanted > most ? most : wanted);
+  if (a.per_group < 1) a.per_group = 1;
+  if (a.per_group > MOST_TOKENS) a.per_group = MOST_TOKENS;
   a.groups = (a.in.tokens + a.per_group - 1) / a.per_group;
   a.by_groups = gkv_divisor(a.groups);
   a.by_per_head = gkv_divisor(per_head);
