@@ -867,6 +867,11 @@ static gkv_status check_rotary(const gkv_ctx* ctx, const GkvRotary& r) {
   if (r.layout != GKV_ROTARY_HALF && r.layout != GKV_ROTARY_INTERLEAVED) return GKV_ERR_INVALID_ARG;
   return isfinite(r.amplitude) ? GKV_OK : GKV_ERR_INVALID_ARG;
 }
+static bool whole_elements(const gkv_ctx* ctx, std::initializer_list<const void*> ptrs) {
+  uintptr_t bits = 0;
+  for (const void* p : ptrs) bits |= (uintptr_t)p;
+  return (bits & (ctx->esz - 1)) == 0;
+}
 // Elements between tokens; 0 stands for rows side by side.
 static bool row_stride(int32_t given, int32_t heads, int32_t d, int64_t* out) {
   *out = given == 0 ? (int64_t)heads * d : given;
@@ -883,6 +888,7 @@ extern "C" gkv_status gkv_rotate(gkv_ctx* ctx, const void* q, int32_t q_stride, 
   const gkv_status st = check_rotary(ctx, a.rotary);
   if (st != GKV_OK) return st;
   if (!row_stride(q_stride, d.Hq, d.d, &a.q_stride) || !row_stride(k_stride, d.Hkv, d.d, &a.k_stride)) return GKV_ERR_INVALID_ARG;
+  if (!whole_elements(ctx, {q, k, q_out, k_out})) return GKV_ERR_INVALID_ARG;
   if ((q && q == q_out && a.q_stride != (int64_t)d.Hq * d.d) || (k && k == k_out && a.k_stride != (int64_t)d.Hkv * d.d)) return GKV_ERR_INVALID_ARG;
   if ((int64_t)d.L * tokens > GKV_MOST_ROWS) return GKV_ERR_SHAPE;
   GkvLaunch ln{ctx, -1, (hipStream_t)stream};
@@ -909,7 +915,7 @@ extern "C" gkv_status gkv_paged_append(gkv_ctx* ctx, const void* q, int32_t q_st
   if (st != GKV_OK) return st;
   if (!freq) a.in.rotary = GkvRotary{nullptr, 0, GKV_ROTARY_HALF, 1.f, 0};
   if (!row_stride(q_stride, d.Hq, d.d, &a.in.q_stride) || !row_stride(k_stride, d.Hkv, d.d, &a.in.k_stride) ||
-      !row_stride(v_stride, d.Hkv, d.d, &a.in.v_stride) || (q && q == q_out && a.in.q_stride != (int64_t)d.Hq * d.d))
+      !row_stride(v_stride, d.Hkv, d.d, &a.in.v_stride) || !whole_elements(ctx, {q, k, v, K, V, q_out}) || (q && q == q_out && a.in.q_stride != (int64_t)d.Hq * d.d))
     return GKV_ERR_INVALID_ARG;
   if ((int64_t)d.L * tokens > GKV_MOST_ROWS) return GKV_ERR_SHAPE;
   a.pages.by_rows = gkv_divisor(page_rows);
@@ -961,7 +967,7 @@ extern "C" gkv_status gkv_paged_workspace_bytes(gkv_ctx* ctx, size_t* out_bytes)
 extern "C" gkv_status gkv_paged_attend_decode(gkv_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* page_table,
                                               int32_t table_width, int32_t page_rows, int32_t n_pages, const int32_t* d_len,
                                               int32_t len_max_host, void* out, void* workspace, void* stream) {
-  if (!ctx || !q || !K || !V || !d_len || !out || len_max_host < 0) return GKV_ERR_INVALID_ARG;
+  if (!ctx || !q || !K || !V || !d_len || !out || len_max_host < 0 || !whole_elements(ctx, {q, K, V, out})) return GKV_ERR_INVALID_ARG;
   const gkv_status st = check_pages(page_table, table_width, page_rows, n_pages);
   if (st != GKV_OK) return st;
   if (len_max_host > (int64_t)table_width * page_rows) return GKV_ERR_OVERFLOW;
@@ -971,7 +977,7 @@ extern "C" gkv_status gkv_paged_attend_decode(gkv_ctx* ctx, const void* q, const
   const int pieces = gkv_paged_pieces(((int64_t)len_max_host + 15) / 16, plan.iters, plan.soft, plan.long_iters);
   PagedAttendArgs a{q, K, V, {page_table, table_width, page_rows, n_pages, gkv_divisor(page_rows)}, d_len, out, (int32_t*)workspace,
                     (float*)((char*)workspace + paged_tickets_bytes(d)), plan.most,
-                    pieces < 1 ? 1 : pieces < plan.most ? pieces : plan.most, plan.iters, plan.soft, plan.long_iters};
+                    pieces < 1 ? 1 : pieces < plan.most ? pieces : plan.most, plan.iters, plan.soft, plan.long_iters, len_max_host};
   GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
   // (the matrix-core kernel counts rows in 32 bits where pages are not whole slices)
   const bool mfma = use_mfma(ctx, {q, K, V, out}) && (page_rows % 16 == 0 || (int64_t)n_pages * d.Hkv * page_rows <= INT32_MAX);

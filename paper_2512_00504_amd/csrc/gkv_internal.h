@@ -218,6 +218,7 @@ struct PagedAttendArgs {
   int32_t most;                                          // pieces of a unit that there is room for
   int32_t splits;                                        // pieces that the launch has
   int32_t split_iters, soft, long_iters;                 // as gkv_paged_pieces has them
+  int32_t len_max;
 };
 // Pieces of a unit of n slices of 16 rows: of split_iters slices, but not more than `soft`; of long_iters slices where those are more.
 static inline int gkv_paged_pieces(int64_t n, int split_iters, int soft, int long_iters) {

@@ -39,6 +39,8 @@ __device__ __forceinline__ float over_lanes(float x) {
   return x;
 }
 
+constexpr int pass(int D) { return 1024 / D; }   // heads whose sums go through LDS at a time
+
 struct PagedArgs {
   const int32_t *len, *table;
   const char *q, *K, *V;
@@ -55,6 +57,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
   using G = Geo<T, D>;
   constexpr bool WHOLE = !G::F32 && KT == 1;
   constexpr int KEYS = 16 * KT;                                // rows of a slice
+  constexpr int PASS = pass(D);
   constexpr int ROW_BYTES = G::ROW_BYTES, OSTR = G::OSTR, PSTR = G::PSTR;
   extern __shared__ __attribute__((aligned(16))) float smem[];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -195,26 +198,14 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
     }
   }
 
-  // ---- merge the wavefronts of this workgroup -------------------------------------------------
-  float* so = smem;                         // [NW][g][OSTR]
-  float* sm = so + NW * g * OSTR;           // [16][NW]
+  // ---- merge the wavefronts of this workgroup, PASS heads at a time ------------------------------
+  const int in_pass = min(g, PASS);
+  float* so = smem;                         // [NW][in_pass][OSTR]
+  float* sm = so + NW * in_pass * OSTR;     // [16][NW]
   float* sl = sm + NW * 16;                 // [16][NW]
   const float l_tot = over_head(st.l_run, false);      // the 4 lanes of a head hold partial sums
-  if (r < g) {
-    float* row = so + (wave * g + r) * OSTR;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-#pragma unroll
-      for (int q4 = 0; q4 < G::NC / 4; ++q4) {
-        const int ch = (G::F32 && D == 128) ? 64 * q4 + 4 * (4 * kb + e) : G::NC * (4 * kb + e) + 4 * q4;
-        *(f32x4*)(row + ch) = f32x4{st.oacc[4 * q4][e], st.oacc[4 * q4 + 1][e], st.oacc[4 * q4 + 2][e], st.oacc[4 * q4 + 3][e]};
-      }
-    }
-    if (kb == 0) { sm[r * NW + wave] = st.m_run; sl[r * NW + wave] = l_tot; }
-  }
+  if (r < g && kb == 0) { sm[r * NW + wave] = st.m_run; sl[r * NW + wave] = l_tot; }
   constexpr int TPH = D / 2;                // threads per head: two channels each
-  __syncthreads();
-
   T* out = (T*)a.out + head0 * D;
   float* part = a.partials + (size_t)unit * a.most * g * PSTR;        // outputs [most][g][D], then maximum and sum [g][most]
   float* part_ms = part + (size_t)a.most * g * D;
@@ -224,34 +215,42 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
       for (int p = 0; p * page_rows < n_tot; ++p) any |= (uint32_t)table[p] < (uint32_t)n_pages;
     store_row2(out + (uint32_t)(x * 2), o * inv_sum(L, any, false));
   };
-  for (int x = tid; x < g * TPH; x += NW * 64) {
-    const int h = x / TPH, c = (x % TPH) * 2;
-    float mw[NW], lw[NW];
+  for (int first = 0; first < g; first += PASS) {
+    if (first > 0) __syncthreads();
+    if (r >= first && r < min(g, first + PASS)) {
+      float* row = so + (wave * in_pass + r - first) * OSTR;
 #pragma unroll
-    for (int i = 0; i < NW / 4; ++i) {
-      const f32x4 m4 = *(const f32x4*)(sm + h * NW + 4 * i), l4 = *(const f32x4*)(sl + h * NW + 4 * i);
+      for (int e = 0; e < 4; ++e) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { mw[4 * i + e] = m4[e]; lw[4 * i + e] = l4[e]; }
+        for (int q4 = 0; q4 < G::NC / 4; ++q4) {
+          const int ch = (G::F32 && D == 128) ? 64 * q4 + 4 * (4 * kb + e) : G::NC * (4 * kb + e) + 4 * q4;
+          *(f32x4*)(row + ch) = f32x4{st.oacc[4 * q4][e], st.oacc[4 * q4 + 1][e], st.oacc[4 * q4 + 2][e], st.oacc[4 * q4 + 3][e]};
+        }
+      }
     }
-    float M = GKV_NO_MAX;
+    __syncthreads();
+    for (int x = first * TPH + tid; x < min(g, first + PASS) * TPH; x += NW * 64) {
+      const int h = x / TPH, c = (x % TPH) * 2;
+      float M = GKV_NO_MAX, mw[NW];
 #pragma unroll
-    for (int wv = 0; wv < NW; ++wv) M = fmaxf(M, mw[wv]);
-    float Lsum = 0.f;
-    f32x2 o = {0.f, 0.f};
+      for (int wv = 0; wv < NW; ++wv) M = fmaxf(M, mw[wv] = sm[h * NW + wv]);
+      float Lsum = 0.f;
+      f32x2 o = {0.f, 0.f};
 #pragma unroll
-    for (int wv = 0; wv < NW; ++wv) {
-      const float f = __builtin_amdgcn_exp2f(mw[wv] - M);
-      Lsum += lw[wv] * f;
-      o += *(const f32x2*)(so + (wv * g + h) * OSTR + c) * f;
-    }
-    if (ns == 1) {
-      finish(x, Lsum, o);
-    } else {
-      store_agent(part + (uint32_t)((sp * g + h) * D + c), o[0], o[1]);
-      if (c == 0) store_agent(part_ms + (uint32_t)((h * a.most + sp) * 2), M, Lsum);
+      for (int wv = 0; wv < NW; ++wv) {
+        const float f = __builtin_amdgcn_exp2f(mw[wv] - M);
+        Lsum += sl[h * NW + wv] * f;
+        o += *(const f32x2*)(so + (wv * in_pass + h - first) * OSTR + c) * f;
+      }
+      if (ns == 1) {
+        finish(x, Lsum, o);
+      } else {
+        store_agent(part + (uint32_t)((sp * g + h) * D + c), o[0], o[1]);
+        if (c == 0) store_agent(part_ms + (uint32_t)((h * a.most + sp) * 2), M, Lsum);
+      }
     }
   }
-  if (ns == 1 || wave * 64 >= g * TPH) return;
+  if (ns == 1 || wave * 64 >= g * TPH) return;                 // (uniform)
 
   // ---- pieces: whoever finishes last joins them -------------------------------------------------
   // A wavefront's outputs are whole heads and need the same heads of the other pieces only: a ticket for each wavefront and no barrier.
@@ -264,7 +263,8 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
   asm volatile("" ::: "memory");
   // A lane has maximum and sum of one piece and makes its factor, so all outputs can be asked for at once.  A wavefront has one head (D = 128) or two.
   constexpr int AT_A_TIME = TPH, AT_ONCE = 16;
-  for (int x = tid; x < g * TPH; x += NW * 64) {               // (the same for the lanes of a head)
+  for (int x = tid; x < g * TPH; x += NW * 64) {               // (a pass is a whole number of rounds, so these are the outputs whose parts this wavefront stored)
+    static_assert(PASS * TPH % (NW * 64) == 0);
     const int h = x / TPH, c = (x % TPH) * 2, in_head = lane % TPH, lane0 = lane - in_head;
     float M = GKV_NO_MAX, Lsum = 0.f;
     f32x2 o = {0.f, 0.f};
@@ -296,10 +296,10 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
   }
 }
 
-size_t lds_bytes(const GkvDims& dm, int waves) { return sizeof(float) * waves * ((size_t)dm.g * (dm.d + 4) + 2 * 16); }
-
 template <typename T, int D, int NW, int KT, int OCC>
 hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const PagedAttendArgs& a) {
+  constexpr int PASS = pass(D);
+  static_assert(sizeof(float) * NW * (PASS * (D + 4) + 2 * 16) <= GKV_LDS_LIMIT);
   const bool whole = a.pages.page_rows % 16 == 0;
   PagedArgs k;
   k.len = a.len; k.table = a.pages.table;
@@ -313,15 +313,23 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const PagedAttendArgs&
   k.width = a.pages.width; k.page_rows = a.pages.page_rows; k.n_pages = a.pages.n_pages;
   k.scale_hi = dm.scale_l2_hi; k.scale_lo = dm.scale_l2_lo;
   auto kern = whole ? paged_attend_mfma_kernel<T, D, NW, KT, OCC, true> : paged_attend_mfma_kernel<T, D, NW, KT, OCC, false>;
-  return gkv_launch(ln, kern, dim3(dm.L * dm.B * dm.Hkv * a.splits), dim3(NW * 64), lds_bytes(dm, NW), k);
+  return gkv_launch(ln, kern, dim3(dm.L * dm.B * dm.Hkv * a.splits), dim3(NW * 64), sizeof(float) * NW * ((size_t)(dm.g < PASS ? dm.g : PASS) * (D + 4) + 2 * 16), k);
+}
+
+// Wavefronts of a workgroup: 8, or fewer where the longest sequence has fewer slices.  A slice is a wavefront's then, and those without one add
+// zeros: the same bits (29344 units of up to 7 rows, d = 64, 125 -> 29 us).  4 also where many units' tables end at 512 rows: a workgroup of 8
+// has hardly begun then when it ends (us, 8 / 4: 14336 units of up to 100 rows 93 / 63, 300 209 / 201, 577 362 / 362; 3584 of up to 2100 330 / 345).
+template <typename T, int D, int KT, int OCC>
+hipError_t by_length(const GkvLaunch& ln, const GkvDims& dm, const PagedAttendArgs& a) {
+  const int64_t units = (int64_t)dm.L * dm.B * dm.Hkv, room = (int64_t)a.pages.width * a.pages.page_rows;
+  if (a.len_max <= 16 * KT) return launch<T, D, 1, KT, OCC>(ln, dm, a);
+  if (a.len_max <= 4 * 16 * KT || (units >= 1024 && room <= 512)) return launch<T, D, 4, KT, OCC>(ln, dm, a);
+  return launch<T, D, 8, KT, OCC>(ln, dm, a);
 }
 
 }  // namespace
 
 hipError_t gkv_launch_paged_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a) {
-  const bool f32 = dtype == GKV_F32;
-  if (dm.d == 64) return f32 ? launch<float, 64, 8, 1, 4>(ln, dm, a) : launch<uint16_t, 64, 8, 2, 4>(ln, dm, a);
-  if (lds_bytes(dm, 8) > GKV_LDS_LIMIT)                      // g = 16
-    return f32 ? launch<float, 128, 4, 1, 2>(ln, dm, a) : launch<uint16_t, 128, 4, 1, 4>(ln, dm, a);
-  return f32 ? launch<float, 128, 8, 1, 2>(ln, dm, a) : launch<uint16_t, 128, 8, 1, 4>(ln, dm, a);
+  if (dtype == GKV_F32) return dm.d == 64 ? by_length<float, 64, 1, 4>(ln, dm, a) : by_length<float, 128, 1, 2>(ln, dm, a);
+  return dm.d == 64 ? by_length<uint16_t, 64, 2, 4>(ln, dm, a) : by_length<uint16_t, 128, 1, 4>(ln, dm, a);
 }

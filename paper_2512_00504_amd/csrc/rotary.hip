@@ -37,22 +37,29 @@ __device__ __forceinline__ float2 turn(double freq, int position, float m, int t
   return make_float2(cs * m, sn * m);
 }
 
-// PIECE elements as they are in memory, and as floats.
-template <typename T, int PIECE> struct Piece;
-template <> struct Piece<float, 4> {
-  u32x4 w;
-  __device__ __forceinline__ void load(const float* p) { w = *(const u32x4*)p; }
-  __device__ __forceinline__ void store(float* p) const { __builtin_nontemporal_store(w, (u32x4*)p); }
-  __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
-  __device__ __forceinline__ void set2(int i, float a, float b) { w[i] = __float_as_uint(a); w[i + 1] = __float_as_uint(b); }
-};
-template <> struct Piece<uint16_t, 8> {
-  u32x4 w;
-  __device__ __forceinline__ void load(const uint16_t* p) { w = *(const u32x4*)p; }
-  __device__ __forceinline__ void store(uint16_t* p) const { __builtin_nontemporal_store(w, (u32x4*)p); }
-  __device__ __forceinline__ float get(int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+// E elements side by side as they are in memory, 16 bytes or less, and as floats.
+template <int WORDS> struct Words { typedef uint32_t type __attribute__((ext_vector_type(WORDS))); };
+template <> struct Words<1> { typedef uint32_t type; };
+template <typename T, int E>
+struct Piece {
+  typedef typename Words<E * (int)sizeof(T) / 4>::type W;
+  uint32_t w[E * sizeof(T) / 4];
+  __device__ __forceinline__ void load(const T* p) {
+    const W x = *(const W*)p;
+    __builtin_memcpy(w, &x, sizeof(x));
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    W x;
+    __builtin_memcpy(&x, w, sizeof(x));
+    __builtin_nontemporal_store(x, (W*)p);
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+  }
   __device__ __forceinline__ void set2(int i, float a, float b) {
-    w[i >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+    if constexpr (sizeof(T) == 4) { w[i] = __float_as_uint(a); w[i + 1] = __float_as_uint(b); }
+    else w[i >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
   }
 };
 template <typename T> struct Piece<T, 1> {
@@ -68,30 +75,24 @@ struct Args {
   const int32_t *start, *len;
   GkvPages pages; void *K, *V;
   int32_t groups, per_group;       // workgroups of a layer, tokens of each
+  int32_t look_first;
   GkvDivisor by_groups, by_per_head, by_heads, by_half;
 };
 
-// Which sequence token t is of, and its row there; row < 0: of none.  The wavefront looks through `start` 64 entries at a time.
+// Which sequence token t is of, and its row there; row < 0: of none.  `before`: entries of `start` at or below t.
 struct Place { int seq; int64_t row; };
-__device__ __forceinline__ Place place_of(int t, const int32_t* start, const int32_t* len, int B, int lane) {
-  int seq = t, end = t + 1;
-  if (start) {
-    int before = 0;                                          // entries at or below t
-    for (int i = lane; i - lane <= B; i += 64) before += __popcll(__ballot(i <= B && start[min(i, B)] <= t));
-    if (before == 0 || before > B) return Place{0, -1};
-    seq = before - 1;
-    end = start[seq + 1];
-  }
-  return Place{seq, (int64_t)len[seq] - ((int64_t)end - t)};
+__device__ __forceinline__ Place place_after(int t, int before, const int32_t* start, const int32_t* len, int B) {
+  if (before == 0 || before > B) return Place{0, -1};
+  return Place{before - 1, (int64_t)len[before - 1] - ((int64_t)start[before] - t)};
 }
 
 // An item is two pieces of a row: of its turned channels the two halves of some pairs (half layout), of the others, and in the interleaved layout,
 // one of the first half and one of the second, so that lanes have neighbours.
-//   VECTOR: pieces of 16 bytes, of which dim/2 (half layout) or dim (interleaved) has to be a whole number; else of one element.
+//   Pieces have E elements, 16 bytes where dim/2 (half layout) or dim (interleaved) is a whole number of them, else fewer.
 // Dynamic LDS: float2 angles[per_group][dim/2].
-template <typename T, bool VECTOR, bool HALF, bool APPEND>
+template <typename T, int E, bool HALF, bool APPEND>
 __global__ __launch_bounds__(THREADS) void rotate_kernel(GkvDims dm, Args a) {
-  constexpr int E = VECTOR ? 16 / (int)sizeof(T) : 1;
+  constexpr bool VECTOR = E > 1;
   using P = Piece<T, E>;
   extern __shared__ float2 angles[];
   __shared__ int64_t row_of[MOST_TOKENS];                     // in the pages of K and V, in rows of d elements; -1: the row is dropped
@@ -187,25 +188,48 @@ __global__ __launch_bounds__(THREADS) void rotate_kernel(GkvDims dm, Args a) {
       load(it[u], x0[u], x1[u]);
     }
   };
+  // (of many tokens some workgroups may have nothing but padding, which costs less than a trip to memory ahead of the loads)
+  if (APPEND && a.look_first && t0 >= a.start[dm.B]) return;
   load_all(tid);
-  for (int k = wave; k < n; k += THREADS / 64) {
+  auto note = [&](int k, const Place& place) {
     const int t = t0 + k;
     int64_t at = -1;
-    int there = 1, position;
-    if constexpr (APPEND) {
-      const Place place = place_of(t, a.start, a.len, dm.B, lane);
-      there = place.row >= 0;
-      position = a.in.positions ? a.in.positions[t] : (int)place.row;
-      if (there && place.row < (int64_t)a.pages.width * a.pages.page_rows) {
-        const int page = quotient((int)place.row, a.pages.by_rows);
-        const int32_t id = a.pages.table[(int64_t)place.seq * a.pages.width + page];
-        if (id >= 0 && id < a.pages.n_pages)
-          at = ((int64_t)layer * a.pages.n_pages + id) * dm.Hkv * a.pages.page_rows + ((int)place.row - page * a.pages.page_rows);
-      }
-    } else {
-      position = a.in.positions ? a.in.positions[t] : resolve_step(dm, a.in.step);
+    if (place.row >= 0 && place.row < (int64_t)a.pages.width * a.pages.page_rows) {
+      const int page = quotient((int)place.row, a.pages.by_rows);
+      const int32_t id = a.pages.table[(int64_t)place.seq * a.pages.width + page];
+      if (id >= 0 && id < a.pages.n_pages)
+        at = ((int64_t)layer * a.pages.n_pages + id) * dm.Hkv * a.pages.page_rows + ((int)place.row - page * a.pages.page_rows);
     }
-    if (lane == 0) { row_of[k] = at; present[k] = there; position_of[k] = position; }
+    row_of[k] = at;
+    present[k] = place.row >= 0;
+    position_of[k] = a.in.positions ? a.in.positions[t] : (int)place.row;
+  };
+  if constexpr (!APPEND) {
+    if (tid < n) {
+      present[tid] = 1;
+      position_of[tid] = a.in.positions ? a.in.positions[t0 + tid] : resolve_step(dm, a.in.step);
+    }
+  } else if (!a.start) {
+    if (tid < n) note(tid, Place{t0 + tid, (int64_t)a.len[t0 + tid] - 1});
+  } else if (a.per_group <= THREADS / 64) {
+    // a wavefront a token, which looks through `start` 64 entries at a time
+    if (wave < n) {
+      const int t = t0 + wave;
+      int before = 0;
+      for (int i = lane; i - lane <= dm.B; i += 64) before += __popcll(__ballot(i <= dm.B && a.start[min(i, dm.B)] <= t));
+      const Place place = place_after(t, before, a.start, a.len, dm.B);
+      if (lane == 0) note(wave, place);
+    }
+  } else if (tid < n) {
+    // a lane a token, by halves
+    const int t = t0 + tid;
+    int before = 0;                                          // entries below it are at or below t, from `end` on above
+    for (int end = dm.B + 1; before < end;) {
+      const int mid = (before + end) >> 1;
+      if (a.start[mid] <= t) before = mid + 1;
+      else end = mid;
+    }
+    note(tid, place_after(t, before, a.start, a.len, dm.B));
   }
   __syncthreads();
   for (int x = tid; x < n * half; x += THREADS) {
@@ -234,13 +258,14 @@ __global__ void advance_kernel(int32_t* len, const int32_t* start, int B) {
 template <typename T, bool APPEND>
 hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, Args a) {
   if (a.in.tokens == 0) return hipSuccess;
-  constexpr int E = 16 / (int)sizeof(T);
   const GkvRotary& r = a.in.rotary;
+  const bool is_half = r.layout == GKV_ROTARY_HALF;
+  // Bytes of a piece: whole numbers of them in everything
   const uintptr_t bits = (uintptr_t)a.in.q | (uintptr_t)a.in.k | (uintptr_t)a.in.v | (uintptr_t)a.in.q_out | (uintptr_t)a.in.k_out |
-                         (uintptr_t)a.K | (uintptr_t)a.V |
-                         (uintptr_t)((a.in.q_stride | a.in.k_stride | a.in.v_stride) * (int64_t)sizeof(T));
-  const bool vector = (bits & 15) == 0 && (r.layout == GKV_ROTARY_HALF ? r.dim / 2 : r.dim) % E == 0;
-  const int pieces = dm.d / (vector ? E : 1), per_head = (pieces + 1) / 2;
+                         (uintptr_t)a.K | (uintptr_t)a.V | 16 |
+                         (uintptr_t)((a.in.q_stride | a.in.k_stride | a.in.v_stride | dm.d | (is_half ? r.dim / 2 : r.dim)) * (int64_t)sizeof(T));
+  const int E = (int)((bits & (~bits + 1)) / sizeof(T));
+  const int pieces = dm.d / E, per_head = (pieces + 1) / 2;
   const int heads = (a.in.q ? dm.Hq : 0) + (a.in.k ? dm.Hkv : 0) * (APPEND ? 2 : 1);
   const int64_t rows = (int64_t)dm.L * a.in.tokens;
   // Tokens of a workgroup: 512 items, two for each thread, where that leaves a workgroup for every CU.  us, by tokens (items of one): 32749 tokens of 40
@@ -256,8 +281,14 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, Args a) {
   a.by_heads = gkv_divisor(heads);
   a.by_half = gkv_divisor(r.dim > 0 ? r.dim / 2 : 1);
   const size_t shmem = sizeof(float2) * a.per_group * (r.dim / 2);
-  auto kern = vector ? (r.layout == GKV_ROTARY_HALF ? rotate_kernel<T, true, true, APPEND> : rotate_kernel<T, true, false, APPEND>)
-                     : (r.layout == GKV_ROTARY_HALF ? rotate_kernel<T, false, true, APPEND> : rotate_kernel<T, false, false, APPEND>);
+  a.look_first = a.start && a.in.tokens > 256;
+  void (*kern)(GkvDims, Args);
+  if constexpr (sizeof(T) == 2) {
+    if (E == 8) kern = is_half ? rotate_kernel<T, 8, true, APPEND> : rotate_kernel<T, 8, false, APPEND>;
+  }
+  if (E == 4) kern = is_half ? rotate_kernel<T, 4, true, APPEND> : rotate_kernel<T, 4, false, APPEND>;
+  else if (E == 2) kern = is_half ? rotate_kernel<T, 2, true, APPEND> : rotate_kernel<T, 2, false, APPEND>;
+  else if (E < 2) kern = is_half ? rotate_kernel<T, 1, true, APPEND> : rotate_kernel<T, 1, false, APPEND>;
   return gkv_launch(ln, kern, dim3(dm.L * a.groups), dim3(THREADS), shmem, dm, a);
 }
 

@@ -133,6 +133,29 @@ def test_the_bound_of_lengths_does_not_show(dtype, d, page_rows):
     assert all(torch.equal(outs[0], x) for x in outs)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("page_rows", [16, 12])
+def test_short_sequences_whatever_the_bound(dtype, d, page_rows):
+    # launches of one, four and eight wavefronts a workgroup
+    gen = torch.Generator().manual_seed(12)
+    for lens in ([16, 1, 7, 0], [31, 32, 17, 5], [64, 63, 49, 33], [128, 100, 65, 2]):
+        B = len(lens)
+        ctx = _ctx(2, B, 2, 5, d, dtype)
+        n = sum(-(-x // page_rows) for x in lens)
+        K, V, q = _rows(gen, dtype, 2, n, 2, page_rows, d), _rows(gen, dtype, 2, n, 2, page_rows, d), _rows(gen, dtype, 2, B, 10, d)
+        table = _table(gen, lens, page_rows, n, 4000 // page_rows)
+        outs = [_attend(ctx, q, K.cuda(), V.cuda(), table, lens, bound) for bound in (max(lens), max(lens) + 1, 64, 65, 128, 129, 3000) if bound >= max(lens)]
+        assert all(torch.equal(outs[0], x) for x in outs)
+        ref, tol = attended(q, K, V, table, lens, scale_of(d), dtype)
+        assert ((outs[0].cpu().double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+def test_many_units_of_short_tables(dtype, d):
+    _case(dtype, d, 2, [(53 * i) % 301 for i in range(130)], 16, L=2, hkv=4, spoil=False)
+    _case(dtype, d, 2, [(5 * i) % 16 for i in range(300)], 16, L=1, hkv=4, spoil=False)
+
+
 def test_a_bound_that_is_too_low_still_covers_every_row():
     ctx = _ctx(1, 1, 1, 2, 64)
     gen = torch.Generator().manual_seed(5)
@@ -299,6 +322,12 @@ def test_append_rows_without_a_page():
     _append("bf16", 64, 16, [30, 10], [64, 20], width=3)
     _append("bf16", 64, 16, [30, 10], [64, 20], table=lambda n, w: torch.tensor([[0, 1, -1, n][:w] + [0] * (w - 4), [2, 10 ** 9] + [-1] * (w - 2)], dtype=torch.int32))
     _append("bf16", 64, 16, [30, 10], [12, 10])
+
+
+def test_append_many_tokens_with_more_padding():
+    _append("bf16", 64, 16, [100, 0, 170, 3], [100, 5, 200, 3], pad=300, dim=48, layout="interleaved")
+    _append("bf16", 64, 12, [0, 0, 0, 0], [100, 5, 200, 3], pad=300)
+    _append("f32", 64, 16, [120, 150], [150, 150], pad=40, rotate=False, L=1, hkv=1, g=1)
 
 
 def test_append_many_sequences_and_tokens():
