@@ -953,13 +953,16 @@ static PagedPlan paged_plan(const gkv_ctx* ctx) {
   if (p.soft > p.most) p.soft = p.most;
   return p;
 }
-static size_t paged_tickets_bytes(const GkvDims& d) { return gkv_align256(sizeof(int32_t) * GKV_PAGED_TICKET * GKV_TICKETS * (size_t)d.L * d.B * d.Hkv); }
+// (whole units need no workspace; 256 bytes so that there is one)
+static size_t paged_tickets_bytes(const GkvDims& d, const PagedPlan& plan) {
+  return plan.most > 1 ? gkv_align256(sizeof(int32_t) * GKV_PAGED_TICKET * GKV_TICKETS * (size_t)d.L * d.B * d.Hkv * gkv_paged_parts(d.g)) : 256;
+}
 
 extern "C" gkv_status gkv_paged_workspace_bytes(gkv_ctx* ctx, size_t* out_bytes) {
   if (!ctx || !out_bytes) return GKV_ERR_INVALID_ARG;
   const GkvDims& d = ctx->dims;
   const PagedPlan plan = paged_plan(ctx);
-  *out_bytes = paged_tickets_bytes(d);
+  *out_bytes = paged_tickets_bytes(d, plan);
   if (plan.most > 1) *out_bytes += gkv_align256(sizeof(float) * (size_t)d.L * d.B * d.Hkv * plan.most * d.g * (d.d + 2));
   return GKV_OK;
 }
@@ -976,13 +979,14 @@ extern "C" gkv_status gkv_paged_attend_decode(gkv_ctx* ctx, const void* q, const
   const PagedPlan plan = paged_plan(ctx);
   const int pieces = gkv_paged_pieces(((int64_t)len_max_host + 15) / 16, plan.iters, plan.soft, plan.long_iters);
   PagedAttendArgs a{q, K, V, {page_table, table_width, page_rows, n_pages, gkv_divisor(page_rows)}, d_len, out, (int32_t*)workspace,
-                    (float*)((char*)workspace + paged_tickets_bytes(d)), plan.most,
+                    (float*)((char*)workspace + paged_tickets_bytes(d, plan)), plan.most,
                     pieces < 1 ? 1 : pieces < plan.most ? pieces : plan.most, plan.iters, plan.soft, plan.long_iters, len_max_host};
   GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
   // (the matrix-core kernel counts rows in 32 bits where pages are not whole slices)
-  const bool mfma = use_mfma(ctx, {q, K, V, out}) && (page_rows % 16 == 0 || (int64_t)n_pages * d.Hkv * page_rows <= INT32_MAX);
+  const bool mfma = (d.d == 64 || d.d == 128) && !ctx->force_generic && aligned16({q, K, V, out}) &&
+                    (page_rows % 16 == 0 || (int64_t)n_pages * d.Hkv * page_rows <= INT32_MAX);
   return hip_status(mfma ? gkv_launch_paged_attend_mfma(ln, d, ctx->cfg.dtype, a)
-                         : gkv_launch_paged_attend_generic(ln, d, ctx->cfg.dtype, a));
+                         : gkv_launch_paged_attend_generic(ln, d, ctx->cfg.dtype, a, aligned16({K, V})));
 }
 
 // ---- profiling API ------------------------------------------------------------------------------

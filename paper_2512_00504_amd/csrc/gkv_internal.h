@@ -212,9 +212,11 @@ hipError_t gkv_launch_paged_advance(const GkvLaunch& ln, const GkvDims& dm, int3
 
 // A unit's ticket has a 128-byte line of its own: its pieces' additions to it come one after the other, and would wait for other units' too.
 constexpr int GKV_PAGED_TICKET = 32;
+// The matrix-core kernel takes a group's heads 16 at a time.
+constexpr int gkv_paged_parts(int g) { return (g + 15) / 16; }
 struct PagedAttendArgs {
   const void* q; const void* K; const void* V; GkvPages pages; const int32_t* len; void* out;
-  int32_t* ticket; float* partials;                      // [units][GKV_PAGED_TICKET]; [units][most][g][d + 2]
+  int32_t* ticket; float* partials;                      // [units][parts][GKV_TICKETS][GKV_PAGED_TICKET]; [units][most][g][d + 2]
   int32_t most;                                          // pieces of a unit that there is room for
   int32_t splits;                                        // pieces that the launch has
   int32_t split_iters, soft, long_iters;                 // as gkv_paged_pieces has them
@@ -226,7 +228,7 @@ static inline int gkv_paged_pieces(int64_t n, int split_iters, int soft, int lon
   if (a > soft) a = soft;
   return (int)(a > b ? a : b);
 }
-hipError_t gkv_launch_paged_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a);
+hipError_t gkv_launch_paged_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a, bool aligned);
 hipError_t gkv_launch_paged_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a);
 
 hipError_t gkv_launch_fill_zero(hipStream_t stream, int32_t* p, size_t n);

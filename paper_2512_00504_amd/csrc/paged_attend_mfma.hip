@@ -1,7 +1,7 @@
-// Decode attention over pages on the matrix cores: bf16 or fp32, head_dim 64 or 128, group size g <= 16, pages of any size.
+// Decode attention over pages on the matrix cores: bf16 or fp32, head_dim 64 or 128, groups of any size (16 heads at a time), pages of any size.
 //
 // One workgroup of NW wavefronts per (unit, piece).  A wavefront owns slices of 16 rows of its sequence (slice it, it + pieces*NW, ...) and
-// keeps running maxima, sums and accumulators of all g query heads, so K and V are read once per KV head.  Products and softmax are
+// keeps running maxima, sums and accumulators of up to 16 query heads, so K and V are read once per KV head where g is no more.  Products and softmax are
 // those of attend_slice.h; bf16 probabilities enter as the sum of two bf16 numbers, which leaves 2^-16 of them.
 //   WHOLE_SLICES: pages of a multiple of 16 rows, so a slice lies in one: its number comes by a scalar load, asked for a slice
 //   ahead, and addresses are a scalar base, a lane's constant offset and an immediate.
@@ -46,9 +46,9 @@ struct PagedArgs {
   const char *q, *K, *V;
   char* out;
   float* partials; int32_t* ticket;
-  GkvDivisor by_units, by_hkv, by_batch, by_iters, by_long, by_page;   // by_page: rows of a page, or slices
+  GkvDivisor by_blocks, by_parts, by_hkv, by_batch, by_iters, by_long, by_page;   // by_page: rows of a page, or slices
   int64_t layer_bytes;                                         // K of a layer
-  int32_t units, splits, most, split_iters, soft, long_iters, Hq, Hkv, g, B, width, page_rows, n_pages;
+  int32_t blocks, parts, splits, most, split_iters, soft, long_iters, Hq, Hkv, g, B, width, page_rows, n_pages;
   float scale_hi, scale_lo;
 };
 
@@ -63,12 +63,13 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, kb = lane >> 4;
-  const int g = a.g, page_rows = a.page_rows, n_pages = a.n_pages;
+  const int page_rows = a.page_rows, n_pages = a.n_pages;
   // (units first: workgroups go to the XCDs in turn, and the last pieces are those of the longest sequences only)
-  const int sp = quotient(blockIdx.x, a.by_units), unit = (int)blockIdx.x - sp * a.units;
+  const int sp = quotient(blockIdx.x, a.by_blocks), block = (int)blockIdx.x - sp * a.blocks;   // of up to 16 heads of a unit
+  const int unit = quotient(block, a.by_parts), part0 = (block - unit * a.parts) * 16, g = min(16, a.g - part0);
   const int lb = quotient(unit, a.by_hkv), j = unit - lb * a.Hkv;
   const int layer = quotient(lb, a.by_batch), seq = lb - layer * a.B;
-  const size_t head0 = (size_t)lb * a.Hq + j * g;
+  const size_t head0 = (size_t)lb * a.Hq + j * a.g + part0;
   const char* q_g = a.q + head0 * ROW_BYTES;
   const int32_t* table = a.table + (int64_t)seq * a.width;
   const char* K = a.K + layer * a.layer_bytes;
@@ -207,8 +208,9 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
   if (r < g && kb == 0) { sm[r * NW + wave] = st.m_run; sl[r * NW + wave] = l_tot; }
   constexpr int TPH = D / 2;                // threads per head: two channels each
   T* out = (T*)a.out + head0 * D;
-  float* part = a.partials + (size_t)unit * a.most * g * PSTR;        // outputs [most][g][D], then maximum and sum [g][most]
-  float* part_ms = part + (size_t)a.most * g * D;
+  // of a unit: outputs [most][its g][D], then maximum and sum [its g][most]
+  float* part = a.partials + (size_t)unit * a.most * a.g * PSTR + part0 * D;
+  float* part_ms = a.partials + (size_t)unit * a.most * a.g * PSTR + (size_t)a.most * a.g * D + (size_t)part0 * a.most * 2;
   auto finish = [&](int x, float L, f32x2 o) {
     bool any = false;
     if (L == 0.f)                                              // seldom: no row, or none with weight
@@ -245,7 +247,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
       if (ns == 1) {
         finish(x, Lsum, o);
       } else {
-        store_agent(part + (uint32_t)((sp * g + h) * D + c), o[0], o[1]);
+        store_agent(part + (uint32_t)((sp * a.g + h) * D + c), o[0], o[1]);
         if (c == 0) store_agent(part_ms + (uint32_t)((h * a.most + sp) * 2), M, Lsum);
       }
     }
@@ -258,7 +260,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   uint32_t arrived = 0;
   if (lane == 0)
-    arrived = __builtin_amdgcn_atomic_inc32((uint32_t*)a.ticket + ((size_t)unit * GKV_TICKETS + wave) * GKV_PAGED_TICKET, (uint32_t)ns - 1u, __ATOMIC_RELAXED, "agent");
+    arrived = __builtin_amdgcn_atomic_inc32((uint32_t*)a.ticket + ((size_t)block * GKV_TICKETS + wave) * GKV_PAGED_TICKET, (uint32_t)ns - 1u, __ATOMIC_RELAXED, "agent");
   if ((int)__builtin_amdgcn_readfirstlane(arrived) != ns - 1) return;
   asm volatile("" ::: "memory");
   // A lane has maximum and sum of one piece and makes its factor, so all outputs can be asked for at once.  A wavefront has one head (D = 128) or two.
@@ -271,7 +273,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
     float2 got[AT_ONCE];
     auto ask_for = [&](int s1) {
 #pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i) got[i] = load_agent(part + (uint32_t)((min(s1 + i, ns - 1) * g + h) * D + c));
+      for (int i = 0; i < AT_ONCE; ++i) got[i] = load_agent(part + (uint32_t)((min(s1 + i, ns - 1) * a.g + h) * D + c));
     };
     for (int s0 = 0; s0 < ns; s0 += AT_A_TIME) {
       float2 ms = load_agent(part_ms + (uint32_t)((h * a.most + min(s0 + in_head, ns - 1)) * 2));
@@ -305,7 +307,8 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const PagedAttendArgs&
   k.len = a.len; k.table = a.pages.table;
   k.q = (const char*)a.q; k.K = (const char*)a.K; k.V = (const char*)a.V; k.out = (char*)a.out;
   k.partials = a.partials; k.ticket = a.ticket;
-  k.units = dm.L * dm.B * dm.Hkv; k.by_units = gkv_divisor(k.units); k.by_hkv = dm.by_hkv; k.by_batch = gkv_divisor(dm.B); k.by_iters = gkv_divisor(a.split_iters); k.by_long = gkv_divisor(a.long_iters);
+  k.parts = gkv_paged_parts(dm.g); k.blocks = dm.L * dm.B * dm.Hkv * k.parts;
+  k.by_blocks = gkv_divisor(k.blocks); k.by_parts = gkv_divisor(k.parts); k.by_hkv = dm.by_hkv; k.by_batch = gkv_divisor(dm.B); k.by_iters = gkv_divisor(a.split_iters); k.by_long = gkv_divisor(a.long_iters);
   k.by_page = gkv_divisor(whole ? a.pages.page_rows / 16 : a.pages.page_rows);
   k.layer_bytes = (int64_t)a.pages.n_pages * dm.Hkv * a.pages.page_rows * Geo<T, D>::ROW_BYTES;
   k.splits = a.splits; k.most = a.most; k.split_iters = a.split_iters; k.soft = a.soft; k.long_iters = a.long_iters;
@@ -313,7 +316,7 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const PagedAttendArgs&
   k.width = a.pages.width; k.page_rows = a.pages.page_rows; k.n_pages = a.pages.n_pages;
   k.scale_hi = dm.scale_l2_hi; k.scale_lo = dm.scale_l2_lo;
   auto kern = whole ? paged_attend_mfma_kernel<T, D, NW, KT, OCC, true> : paged_attend_mfma_kernel<T, D, NW, KT, OCC, false>;
-  return gkv_launch(ln, kern, dim3(dm.L * dm.B * dm.Hkv * a.splits), dim3(NW * 64), sizeof(float) * NW * ((size_t)(dm.g < PASS ? dm.g : PASS) * (D + 4) + 2 * 16), k);
+  return gkv_launch(ln, kern, dim3(k.blocks * a.splits), dim3(NW * 64), sizeof(float) * NW * ((size_t)(dm.g < PASS ? dm.g : PASS) * (D + 4) + 2 * 16), k);
 }
 
 // Wavefronts of a workgroup: 8, or fewer where the longest sequence has fewer slices.  A slice is a wavefront's then, and those without one add

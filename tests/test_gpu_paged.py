@@ -73,7 +73,8 @@ def _case(dtype, d, g, lens, page_rows, L=1, hkv=2, params=None, seed=0, spoil=T
 
 
 SHAPES = [("bf16", 128, 7), ("bf16", 128, 1), ("bf16", 64, 5), ("f32", 64, 4), ("f32", 128, 2), ("bf16", 128, 16), ("f32", 128, 16), ("bf16", 64, 16),
-          ("bf16", 48, 3), ("f32", 20, 2), ("bf16", 64, 17), ("bf16", 512, 2)]
+          ("bf16", 48, 3), ("f32", 20, 2), ("bf16", 64, 17), ("bf16", 512, 2), ("bf16", 128, 33), ("f32", 64, 20), ("f32", 128, 17), ("bf16", 96, 5), ("f32", 256, 9),
+          ("bf16", 256, 4), ("f32", 100, 1), ("bf16", 8, 6)]
 LENS = [0, 1, 15, 16, 17, 33, 129, 255, 256, 257]
 
 
@@ -88,6 +89,7 @@ def test_lengths_and_pages(dtype, d, g, page_rows):
                                             ("f32", 64, {"force_generic": 1})])
 def test_long_sequences_in_pieces(dtype, d, params, page_rows):
     _case(dtype, d, 3, [5000], page_rows, hkv=1, params=params)
+    _case(dtype, d, 19, [2600], page_rows, hkv=1, params=params)
     _case(dtype, d, 2, [3001, 0, 17, 2048, 600], page_rows, L=2, hkv=2, params=params)
 
 

@@ -4,7 +4,7 @@ import torch
 
 import paper_2512_00504_amd as P
 from paper_2512_00504_amd import Rotary, make_config
-from paper_2512_00504_amd.state import DecodeState, Q8DecodeState
+from paper_2512_00504_amd.state import DecodeState, Q8DecodeState, SharedPrefix
 
 from paged_reference import DT, turned
 
@@ -201,6 +201,25 @@ def test_decode_steps_with_a_rotary_are_those_of_turned_inputs(cls, dtype):
         if a.is_trigger(t):
             a.evict(t); b.evict(t)
     assert torch.equal(a.pos, b.pos) and torch.equal(a.d_state, b.d_state) and torch.equal(a.F_hist, b.F_hist)
+
+
+@pytest.mark.parametrize("cls", [DecodeState, Q8DecodeState])
+def test_decode_steps_with_a_rotary_and_a_shared_prefix(cls):
+    # the prompt's keys at the positions before the first step's
+    cfg, rows = make_config(2, 3, 4, 2, 64, 16, 4, 8, 32, "bf16"), 21
+    a, b = cls(cfg), cls(cfg)
+    rotary, g = Rotary(64), torch.Generator().manual_seed(1)
+    pk, pv = (torch.randn(2, 2, rows, 64, generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    ctx, turned_pk = _ctx(2, 1, 4, 2), torch.empty(2, rows, 2, 64, dtype=torch.bfloat16, device="cuda")
+    ctx.rotate(None, pk.transpose(1, 2).contiguous(), torch.arange(rows, dtype=torch.int32).cuda(), 0, rotary, None, turned_pk)
+    prompts = [SharedPrefix(st, turned_pk.transpose(1, 2), pv) for st in (a, b)]
+    a.set_state(0, rows, 0, 0); b.set_state(0, rows, 0, 0)
+    for t in range(rows, rows + 10):
+        q, k, v = (torch.randn(2, 3, h, 64, generator=g).to(torch.bfloat16).cuda() for h in (4, 2, 2))
+        qt, kt = torch.empty_like(q), torch.empty_like(k)
+        b.ctx.rotate(q, k, torch.full((3,), t, dtype=torch.int32).cuda(), 0, rotary, qt, kt)
+        out = a.attend_decode(q, k, v, t, prefix=prompts[0], rotary=rotary).clone()
+        assert torch.equal(out, b.attend_decode(qt, kt, v, t, prefix=prompts[1]))
 
 
 def test_recorded_calls_replay():
