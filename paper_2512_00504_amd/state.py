@@ -355,10 +355,22 @@ class PagedDecodeState:
         self.workspace = z(self.ctx.paged_workspace_bytes(), dtype=torch.uint8)
         self._table = torch.full((B, width), -1, dtype=torch.int32)          # host mirror
         self._free = list(range(n_pages))[::-1]
-        self._pages, self._len = [0] * B, [0] * B                            # pages and rows of each sequence; -1 rows: takes no part
+        self._pages = [0] * B                                                # of each sequence
+        self._settle([0] * B)
+
+    def _settle(self, lens):
+        """Host mirror of the lengths (-1: takes no part), as of now; _grown rows later for all that take part, and at most _room of them
+        until one needs a page more."""
+        self._len0, self._grown = lens, 0
+        self._room = min([p * self.page_rows - n for p, n in zip(self._pages, lens) if n >= 0], default=1 << 30)
+
+    @property
+    def _len(self):
+        return [n + self._grown if n >= 0 else n for n in self._len0]
 
     @property
     def lengths(self):
+        """Rows of each sequence."""
         return [max(n, 0) for n in self._len]
 
     def reserve(self, rows):
@@ -377,36 +389,55 @@ class PagedDecodeState:
             for p in range(self._pages[i], n):
                 self._table[i, p] = self._free.pop()
         self._pages = want
+        self._settle(self._len)
         self.page_table.copy_(self._table)
 
     def release(self, i):
         """Sequence i's pages come back, and it takes no part until append() gives it tokens again."""
+        if not 0 <= i < self.cfg.batch:
+            raise ValueError(f"gkv: there is no sequence {i}")
         self._free += [int(p) for p in self._table[i, :self._pages[i]].flip(0)]
         self._table[i] = -1
-        self._pages[i], self._len[i] = 0, -1
+        self._pages[i] = 0
+        self._settle([-1 if k == i else n for k, n in enumerate(self._len)])
         self.page_table[i] = -1
         self.d_len[i] = -1
 
     def append(self, k, v, counts=None, q=None, positions=None, q_out=None):
         """New tokens k, v [L, tokens, h_kv, d], packed: counts of them for each sequence (None: one for each that takes part, tokens = B); tokens
         behind the last are padding.  Returns q [L, tokens, h_q, d] turned, in q_out or a new tensor, if it is given."""
-        cfg = self.cfg
+        cfg, ctx = self.cfg, self.ctx
+        # all that can be wrong is looked at before anything grows
+        ctx._heads(k, k.shape[1], cfg.n_kv_heads, "k")
+        ctx._heads(v, k.shape[1], cfg.n_kv_heads, "v")
+        ctx._heads(q, k.shape[1], cfg.n_q_heads, "q")
+        ctx._heads(q_out, k.shape[1], cfg.n_q_heads, "q_out", False)
+        ctx._ints(positions, (k.shape[1],), "positions", True)
+        if any(x is not None and x.device != self.K.device for x in (k, v, q, q_out, positions)):
+            raise ValueError(f"gkv: tensors have to be on {self.K.device}")
+        if self.K.is_cuda and self.K.device.index != torch.cuda.current_device():
+            raise ValueError(f"gkv: the state is on {self.K.device}, which is not the current GPU")
         if counts is not None and (len(counts) != cfg.batch or min(counts) < 0 or sum(counts) > k.shape[1]):
             raise ValueError(f"gkv: {cfg.batch} counts of {k.shape[1]} tokens are wanted")
         if counts is None and k.shape[1] != cfg.batch:
             raise ValueError(f"gkv: one token for each of {cfg.batch} sequences is wanted")
         if self.rotary is None and q is not None:
             raise ValueError("gkv: queries are turned where there is a rotary")
-        lens = [n + 1 if n >= 0 else n for n in self._len] if counts is None else [max(n, 0) + m if m else n for n, m in zip(self._len, counts)]
-        self.reserve(lens)
         start = None
         if counts is not None:
+            lens = [max(n, 0) + m if m else n for n, m in zip(self._len, counts)]
+            self.reserve(lens)
+            self._settle(lens)
             start = torch.tensor([0, *counts], dtype=torch.int32).cumsum(0, dtype=torch.int32).to(self.device)
+        else:
+            if self._room < 1:
+                self.reserve([n + 1 if n >= 0 else 0 for n in self._len])
+            self._grown += 1
+            self._room -= 1
         if q is not None and q_out is None:
             q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        self.ctx.paged_advance(self.d_len, start)
-        self._len = lens
-        self.ctx.paged_append(q, k, v, start, self.d_len, positions, self.rotary, self.page_table, self.K, self.V, q_out)
+        ctx.paged_advance(self.d_len, start)
+        ctx.paged_append(q, k, v, start, self.d_len, positions, self.rotary, self.page_table, self.K, self.V, q_out)
         return q_out
 
     def attend(self, q):
@@ -416,6 +447,7 @@ class PagedDecodeState:
 
     def attend_decode(self, q, k_new, v_new, positions=None):
         """One decode step: q [L, B, h_q, d], k_new, v_new [L, B, h_kv, d]."""
+        self.ctx._heads(q, self.cfg.batch, self.cfg.n_q_heads, "q", self.rotary is not None)
         if self.rotary is None:
             self.append(k_new, v_new)
         else:
@@ -423,8 +455,9 @@ class PagedDecodeState:
         return self.attend(q)
 
     def replayed(self, steps=1):
-        """So many recorded decode steps were replayed: what was not told to this object otherwise."""
-        self._len = [n + steps if n >= 0 else n for n in self._len]
+        """So many decode steps were made by replays of recorded ones that this object does not know of (recording a step counts it once)."""
+        self._grown += steps
+        self._room -= steps
 
 
 class SharedPrefix:

@@ -207,3 +207,19 @@ def test_state_refuses_what_its_pages_have_no_room_for():
         st.append(k, k)
     with pytest.raises(ValueError, match="rotary"):
         st.append(k[:, :2], k[:, :2], None, torch.zeros(1, 2, 4, 64))
+    for i in (-1, 2):
+        with pytest.raises(ValueError):
+            st.release(i)
+
+
+def test_a_refused_call_leaves_the_state_as_it_was():
+    cfg = P.make_config(1, 2, 4, 2, 64, 64, 8, 16, 96, "f32")
+    st = PagedDecodeState(cfg, max_rows=40, page_rows=16, rotary=P.Rotary(64, device="cpu"), device="cpu")
+    q, k = torch.zeros(1, 2, 4, 64), torch.zeros(1, 2, 2, 64)
+    before = (st._len, list(st._pages), len(st._free), st.d_len.clone())
+    for call in (lambda: st.append(k[..., :32], k), lambda: st.append(k, k[:, :1]), lambda: st.append(k.half(), k.half()), lambda: st.append(k, k, [40, 2]),
+                 lambda: st.append(k, k, None, q[:, :, :3]), lambda: st.append(k, k, None, q, torch.zeros(2)), lambda: st.append(k, k, None, q, None, q[:, :1]),
+                 lambda: st.append(k, k.to("meta")), lambda: st.attend_decode(q[:, :1], k, k), lambda: st.append(k, k, None, q, torch.zeros(3, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            call()
+        assert (st._len, list(st._pages), len(st._free)) == before[:3] and torch.equal(st.d_len, before[3])
