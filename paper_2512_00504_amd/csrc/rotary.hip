@@ -9,8 +9,8 @@
 // Bound: memory, each element read and written once.  A workgroup has the cosines and sines of its tokens in LDS, made once for all
 // heads (an angle is some 40 instructions, a turned pair 6), while its first loads are on their way.  Neighbouring lanes have neighbouring 16
 // bytes in every load and store, and stores are non-temporal: 32749 tokens of 40 and 8 heads, three quarters of 128 channels interleaved, 805 MB, 162 us
-// with two neighbouring pieces a lane, 142 so, 131 with those stores (6.1 TB/s, where a copy of 1 GiB makes 5.1; non-temporal loads as well 10% slower); appends
-// of 67 MB 14.5 -> 11.8, of 625 MB 113 -> 107.
+// with two neighbouring pieces a lane, 142 so, 131 with those stores; appends of 66 MB 14.5 -> 11.8, of 625 MB 113 -> 107 (non-temporal loads as well:
+// 10% slower).  Two items a thread at a time where those had four: the smallest calls 3.06 -> 2.82, 805 MB 138 (5.8 TB/s; a copy of 1 GiB makes 5.1), 625 MB 105.
 #include "gkv_internal.h"
 
 namespace {
