@@ -418,7 +418,7 @@ gkv_status gkv_rotary_frequencies(int32_t dim, double base, int32_t scaling, dou
  * positions: device, int32 [tokens], the same in every layer, any value; NULL: `step` for every token (relative to the step base if one is set).
  * q_out may be the ring slot of the step, whose gkv_attend_decode then copies nothing.
  * transposed = 1: by -a instead of a, which takes the gradient of the outputs to that of the inputs.
- * Rows and strides of whole 16-byte pieces, with dim/2 (interleaved: dim) a whole number of them, are fastest.  L * tokens at most 2^30. */
+ * Rows and strides of whole 16-byte pieces, with dim/2 (interleaved: dim) a whole number of them, are fastest.  L * tokens less than 2^24 (else GKV_ERR_SHAPE). */
 gkv_status gkv_rotate(gkv_ctx* ctx, const void* q, int32_t q_stride, const void* k, int32_t k_stride, int32_t tokens,
                       const int32_t* positions, int32_t step, const double* freq, int32_t dim, int32_t layout,
                       float amplitude, int32_t transposed, void* q_out, void* k_out, void* stream);
@@ -445,7 +445,7 @@ gkv_status gkv_paged_advance(gkv_ctx* ctx, int32_t* d_len, const int32_t* d_star
  * k, v (and q): [L,tokens,heads,d] with strides as gkv_rotate takes them.  With freq, keys are turned on the way, by positions[token] (device, int32 [tokens])
  * or, where that is NULL, by the row they become; and so are queries, if given, to q_out [L,tokens,h_q,d] (in place as in gkv_rotate).  freq == NULL: keys are stored
  * as they are, dim, layout and amplitude mean nothing, and q has to be NULL.
- * Tokens at or beyond d_start[B], before d_start[0], or whose row would be below 0 are not looked at: their q_out stays as it is. */
+ * L * tokens less than 2^24.  Tokens at or beyond d_start[B], before d_start[0], or whose row would be below 0 are not looked at: their q_out stays as it is. */
 gkv_status gkv_paged_append(gkv_ctx* ctx, const void* q, int32_t q_stride, const void* k, int32_t k_stride, const void* v,
                             int32_t v_stride, int32_t tokens, const int32_t* d_start, const int32_t* d_len,
                             const int32_t* positions, const double* freq, int32_t dim, int32_t layout, float amplitude,
@@ -453,13 +453,13 @@ gkv_status gkv_paged_append(gkv_ctx* ctx, const void* q, int32_t q_stride, const
                             void* K, void* V, void* q_out, void* stream);
 
 /* One new token's queries over each sequence's rows: out[i] = softmax(q[i] . K[i/g]^T * scale) V[i/g] over rows [0, d_len).  q, out [L,B,h_q,d].
- * A sequence without rows gets zeros.  Long sequences are cut into pieces that the same launch joins.
+ * A sequence without rows gets zeros.  out may be q.  Long sequences are cut into pieces that the same launch joins.
  * len_max_host: host bound with every d_len <= len_max_host <= table_width * page_rows (else GKV_ERR_OVERFLOW); it sizes the launch and does not show
  * in the result.
- * workspace: device memory of gkv_paged_workspace_bytes() bytes, 16-byte aligned, zeroed once by the caller; calls that may overlap in time (also replays
- * of recorded ones) need one each.  gkv_workspace_bytes' is another.
+ * workspace: device memory of gkv_paged_workspace_bytes() bytes, 16-byte aligned, zeroed once by the caller and of one context alone; calls that may
+ * overlap in time (also replays of recorded ones) need one each.  gkv_workspace_bytes' is another.
  * Logits, weights, sums and outputs are formed in 32 bits; with bf16 the matrix-core kernel takes a weight as the sum of two bf16 numbers for its product
- * with V (2^-16 of it). */
+ * with V (within 2^-15 of it; d = 64: three, all of its bits). */
 gkv_status gkv_paged_workspace_bytes(gkv_ctx* ctx, size_t* out_bytes);
 gkv_status gkv_paged_attend_decode(gkv_ctx* ctx, const void* q, const void* K, const void* V, const int32_t* page_table,
                                    int32_t table_width, int32_t page_rows, int32_t n_pages, const int32_t* d_len,

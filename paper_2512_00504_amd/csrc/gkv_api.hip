@@ -862,6 +862,9 @@ extern "C" gkv_status gkv_rotary_frequencies(int32_t dim, double base, int32_t s
   return GKV_OK;
 }
 
+// A launch has less than 2^32 threads: a workgroup of 256 a token at most, and of 512 a piece.
+constexpr int64_t GKV_MOST_TURNED = (1 << 24) - 1, GKV_MOST_PIECES = (1 << 23) - 1;
+
 static gkv_status check_rotary(const gkv_ctx* ctx, const GkvRotary& r) {
   if (r.dim < 2 || r.dim % 2 != 0 || r.dim > ctx->dims.d || ((uintptr_t)r.freq & 7) != 0) return GKV_ERR_INVALID_ARG;
   if (r.layout != GKV_ROTARY_HALF && r.layout != GKV_ROTARY_INTERLEAVED) return GKV_ERR_INVALID_ARG;
@@ -890,7 +893,7 @@ extern "C" gkv_status gkv_rotate(gkv_ctx* ctx, const void* q, int32_t q_stride, 
   if (!row_stride(q_stride, d.Hq, d.d, &a.q_stride) || !row_stride(k_stride, d.Hkv, d.d, &a.k_stride)) return GKV_ERR_INVALID_ARG;
   if (!whole_elements(ctx, {q, k, q_out, k_out})) return GKV_ERR_INVALID_ARG;
   if ((q && q == q_out && a.q_stride != (int64_t)d.Hq * d.d) || (k && k == k_out && a.k_stride != (int64_t)d.Hkv * d.d)) return GKV_ERR_INVALID_ARG;
-  if ((int64_t)d.L * tokens > GKV_MOST_ROWS) return GKV_ERR_SHAPE;
+  if ((int64_t)d.L * tokens > GKV_MOST_TURNED) return GKV_ERR_SHAPE;
   GkvLaunch ln{ctx, -1, (hipStream_t)stream};
   return hip_status(gkv_launch_rotate(ln, d, ctx->cfg.dtype, a));
 }
@@ -917,7 +920,7 @@ extern "C" gkv_status gkv_paged_append(gkv_ctx* ctx, const void* q, int32_t q_st
   if (!row_stride(q_stride, d.Hq, d.d, &a.in.q_stride) || !row_stride(k_stride, d.Hkv, d.d, &a.in.k_stride) ||
       !row_stride(v_stride, d.Hkv, d.d, &a.in.v_stride) || !whole_elements(ctx, {q, k, v, K, V, q_out}) || (q && q == q_out && a.in.q_stride != (int64_t)d.Hq * d.d))
     return GKV_ERR_INVALID_ARG;
-  if ((int64_t)d.L * tokens > GKV_MOST_ROWS) return GKV_ERR_SHAPE;
+  if ((int64_t)d.L * tokens > GKV_MOST_TURNED) return GKV_ERR_SHAPE;
   a.pages.by_rows = gkv_divisor(page_rows);
   GkvLaunch ln{ctx, -1, (hipStream_t)stream};
   return hip_status(gkv_launch_paged_append(ln, d, ctx->cfg.dtype, a));
@@ -981,6 +984,7 @@ extern "C" gkv_status gkv_paged_attend_decode(gkv_ctx* ctx, const void* q, const
   PagedAttendArgs a{q, K, V, {page_table, table_width, page_rows, n_pages, gkv_divisor(page_rows)}, d_len, out, (int32_t*)workspace,
                     (float*)((char*)workspace + paged_tickets_bytes(d, plan)), plan.most,
                     pieces < 1 ? 1 : pieces < plan.most ? pieces : plan.most, plan.iters, plan.soft, plan.long_iters, len_max_host};
+  if ((int64_t)d.L * d.B * d.Hkv * gkv_paged_parts(d.g) * a.splits > GKV_MOST_PIECES) return GKV_ERR_SHAPE;
   GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
   // (the matrix-core kernel counts rows in 32 bits where pages are not whole slices)
   const bool mfma = (d.d == 64 || d.d == 128) && !ctx->force_generic && aligned16({q, K, V, out}) &&

@@ -2,7 +2,8 @@
 //
 // One workgroup of NW wavefronts per (unit, piece).  A wavefront owns slices of 16 rows of its sequence (slice it, it + pieces*NW, ...) and
 // keeps running maxima, sums and accumulators of up to 16 query heads, so K and V are read once per KV head where g is no more.  Products and softmax are
-// those of attend_slice.h; bf16 probabilities enter as the sum of two bf16 numbers, which leaves 2^-16 of them.
+// those of attend_slice.h; bf16 probabilities enter as the sum of two bf16 numbers, within 2^-15 of them (the upper half of their
+// bits, and the rest rounded), at d = 64 of three, which have all bits.
 //   WHOLE_SLICES: pages of a multiple of 16 rows, so a slice lies in one: its number comes by a scalar load, asked for a slice
 //   ahead, and addresses are a scalar base, a lane's constant offset and an immediate.
 //   Else a lane asks for the page of row r of a slice (one row of K), and for its four rows of V gets theirs from the lanes that have them.

@@ -241,6 +241,20 @@ def test_pages_beyond_32_bits_of_offset():
         assert torch.equal(K[0, page, :, row], k[0, i]) and torch.equal(V[0, page, :, row], v[0, i])
 
 
+@pytest.mark.parametrize("dtype,d,g,params", [("bf16", 128, 7, None), ("f32", 64, 16, None), ("bf16", 128, 20, None), ("bf16", 128, 5, {"force_generic": 1}), ("bf16", 96, 5, None)])
+def test_outputs_in_place_of_the_queries(dtype, d, g, params):
+    lens, page_rows = [1, 40, 3000, 700], 16
+    ctx = _ctx(1, 4, 2, g, d, dtype, params)
+    gen = torch.Generator().manual_seed(9)
+    n = sum(-(-x // page_rows) for x in lens)
+    K, V, q = _rows(gen, dtype, 1, n, 2, page_rows, d).cuda(), _rows(gen, dtype, 1, n, 2, page_rows, d).cuda(), _rows(gen, dtype, 1, 4, 2 * g, d).cuda()
+    table = _table(gen, lens, page_rows, n, 200)
+    ref = _attend(ctx, q, K, V, table, lens)
+    ws = torch.zeros(ctx.paged_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    ctx.paged_attend_decode(q, K, V, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), 3000, q, ws)
+    assert torch.equal(q, ref)
+
+
 def test_sequences_that_share_pages():
     ctx = _ctx(1, 3, 2, 3, 128)
     gen = torch.Generator().manual_seed(6)

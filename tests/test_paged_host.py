@@ -32,11 +32,11 @@ REFUSED = [
     *[("gkv_rotate", at, v, INVALID) for at, v in [(0, None), (2, None), (7, None), (12, None), (13, None), (1, 511), (1, -512), (3, 127), (4, -1), (6, -1),
                                                    (7, AT + 4), (8, 0), (8, 63), (8, 66), (8, -2), (9, 2), (9, -1),
                                                    (10, float("nan")), (10, float("inf")), (0, AT + 1), (2, AT + 3), (12, AT + 1), (13, AT + 1)]],
-    ("gkv_rotate", 4, 2 ** 29 + 1, SHAPE),
+    ("gkv_rotate", 4, 2 ** 23, SHAPE),
     ("gkv_paged_advance", 0, None, INVALID),
     *[("gkv_paged_append", at, v, INVALID) for at, v in [(i, None) for i in (0, 2, 4, 7, 8, 10, 14, 18, 19, 20)]
       + [(1, 511), (3, 127), (5, 127), (6, -1), (10, AT + 4), (11, 0), (11, 63), (11, 66), (12, 2), (13, float("nan")), (15, 0), (16, 0), (17, 0), (15, -4), (0, AT + 1), (2, AT + 1), (4, AT + 1), (18, AT + 1), (19, AT + 1), (20, AT + 1)]],
-    ("gkv_paged_append", 6, 2 ** 29 + 1, SHAPE), ("gkv_paged_append", 15, 2 ** 26 + 1, SHAPE),
+    ("gkv_paged_append", 6, 2 ** 23, SHAPE), ("gkv_paged_append", 15, 2 ** 26 + 1, SHAPE),
     *[("gkv_paged_attend_decode", at, v, INVALID) for at, v in [(i, None) for i in (0, 1, 2, 3, 7, 9)] + [(4, 0), (5, 0), (6, 0), (8, -1), (0, AT + 1), (1, AT + 1), (2, AT + 1), (9, AT + 1)]],
     ("gkv_paged_attend_decode", 4, 2 ** 26 + 1, SHAPE), ("gkv_paged_attend_decode", 8, 65, OVERFLOW),
     ("gkv_paged_attend_decode", 10, None, WORKSPACE), ("gkv_paged_attend_decode", 10, AT + 8, WORKSPACE),
@@ -70,6 +70,12 @@ def test_nothing_to_turn_and_queries_without_frequencies_are_refused():
     args = list(GOOD["gkv_paged_append"])
     args[7] = None                                                # one token each: not five of three sequences
     assert LIB.gkv_paged_append(ctx.h, *args, None) == INVALID
+    ctx.close()
+
+
+def test_more_units_than_a_launch_has_room_for_are_refused():
+    ctx = _ctx(n_layers=1, batch=1 << 22)
+    assert LIB.gkv_paged_attend_decode(ctx.h, *GOOD["gkv_paged_attend_decode"], None) == SHAPE
     ctx.close()
 
 
