@@ -941,7 +941,9 @@ extern "C" gkv_status gkv_paged_advance(gkv_ctx* ctx, int32_t* d_len, const int3
 //            350 / 336 / 329 / 322; bf16, d = 64 96 units of up to 3001 16 / 24 / 32 11.4 / 11.3 / 11.5.
 //     soft   pieces of a unit: 256 workgroups in all (4 units of 131071 rows 32 / 64 / 128 pieces 50.0 / 45.2 / 49.4), or 8 (32 units of 8192 rows,
 //            4 / 8 / 16 27.6 / 23.7 / 24.3).
-//     long_iters  in batches, where the longest sequence would end alone: 4096 rows a piece, up to what 512 workgroups of one sequence are.
+//     long_iters  in batches the longest sequences would end alone: so many slices a piece, up to what 512 workgroups of one sequence are (36 units of up
+//            to 16354 rows 64 / 96 / 256 32.5 / 39.5 / 46.9, 64 of up to 16384 51.0 / 50.9 / 56.0, 128 89.8 / 95.2 / 99.4, 256 195 / 196 / 202; but 128 of
+//            16384 each 177 / 177 / 168, 32 of up to 32768 58.1 / 61.1 / 55.7).
 struct PagedPlan { int32_t most, iters, soft, long_iters; };
 static PagedPlan paged_plan(const gkv_ctx* ctx) {
   const GkvDims& d = ctx->dims;
@@ -950,7 +952,7 @@ static PagedPlan paged_plan(const gkv_ctx* ctx) {
   PagedPlan p;
   p.iters = units >= 512 ? 256 : within(units / 4, d.d == 64 && ctx->cfg.dtype == GKV_BF16 ? 16 : 8, 32);
   p.soft = within(256 / units, 8, 64);
-  p.long_iters = units >= 32 ? 256 : GKV_MOST_ROWS;
+  p.long_iters = units >= 512 ? 256 : units >= 32 ? 64 : GKV_MOST_ROWS;
   p.most = within(512 / of_one, 1, within(32768 / units, 1, 64));
   if (units < 32 && p.most < p.soft) p.most = p.soft;
   if (p.soft > p.most) p.soft = p.most;
