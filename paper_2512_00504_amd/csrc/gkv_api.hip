@@ -932,30 +932,36 @@ extern "C" gkv_status gkv_paged_advance(gkv_ctx* ctx, int32_t* d_len, const int3
   return hip_status(gkv_launch_paged_advance(ln, ctx->dims, d_len, d_start));
 }
 
-// How units are cut (gkv_paged_pieces), and the pieces there is room for.  By the configuration alone: the same call gives the same bits
+// How units are cut, and the pieces there is room for.  By the configuration alone: the same call gives the same bits
 // whatever bound of the lengths it comes with.
 //   A workgroup (8 wavefronts) takes as many slices at a time as it has wavefronts, of 32 rows at bf16, d = 64 and of 16 else; the chip holds 512
 //   workgroups.  A piece more costs its start and its part of the joining, some 2 us beside others' reading.  us, by slices a piece:
 //     iters  4 units of 577 rows 8 / 16 / 32: 6.4 / 7.5 / 8.3, of 4096 7.6 / 7.6 / 9.8; 128 units of 577 16 / 32 / whole 10.1 / 9.4 / 9.7; 256 units
 //            of up to 4000 16 / 32 / 64 / 128 45.1 / 45.1 / 47.5 / 53; 512 units of up to 16384 64 / 128 / 256 / 512 362 / 353 / 356 / 374, of 8192
 //            350 / 336 / 329 / 322; bf16, d = 64 96 units of up to 3001 16 / 24 / 32 11.4 / 11.3 / 11.5.
+//     twice, four_times  of few units: joining a piece takes its time too, and more with more heads (2 units of 700 slices, g = 16 22 / 44 / 64 pieces 13.3 / 14.3 /
+//            16.0, of 4, g = 7 10.0 / 10.2 / 11.0; 2 of 256, g = 16 16 / 32 9.9 / 11.0; 4 of 2048 32 / 64 17.4 / 16.9).
 //     soft   pieces of a unit: 256 workgroups in all (4 units of 131071 rows 32 / 64 / 128 pieces 50.0 / 45.2 / 49.4), or 8 (32 units of 8192 rows,
 //            4 / 8 / 16 27.6 / 23.7 / 24.3).
 //     long_iters  in batches the longest sequences would end alone: so many slices a piece, up to what 512 workgroups of one sequence are (36 units of up
 //            to 16354 rows 64 / 96 / 256 32.5 / 39.5 / 46.9, 64 of up to 16384 51.0 / 50.9 / 56.0, 128 89.8 / 95.2 / 99.4, 256 195 / 196 / 202; but 128 of
 //            16384 each 177 / 177 / 168, 32 of up to 32768 58.1 / 61.1 / 55.7).
-struct PagedPlan { int32_t most, iters, soft, long_iters; };
+struct PagedPlan { int32_t most; GkvPagedCut cut; };
 static PagedPlan paged_plan(const gkv_ctx* ctx) {
   const GkvDims& d = ctx->dims;
   const int64_t units = (int64_t)d.L * d.B * d.Hkv, of_one = (int64_t)d.L * d.Hkv;
   auto within = [](int64_t x, int64_t lo, int64_t hi) { return (int32_t)(x < lo ? lo : x > hi ? hi : x); };
   PagedPlan p;
-  p.iters = units >= 512 ? 256 : within(units / 4, d.d == 64 && ctx->cfg.dtype == GKV_BF16 ? 16 : 8, 32);
-  p.soft = within(256 / units, 8, 64);
-  p.long_iters = units >= 512 ? 256 : units >= 32 ? 64 : GKV_MOST_ROWS;
+  GkvPagedCut& c = p.cut;
+  const bool pairs = d.d == 64 && ctx->cfg.dtype == GKV_BF16;          // 32 rows at a time
+  c.iters = units >= 512 ? 256 : within(units / 4, pairs ? 16 : 8, 32);
+  c.soft = within(256 / units, 8, 64);
+  c.long_iters = units >= 512 ? 256 : units >= 32 ? 64 : GKV_MOST_ROWS;
+  c.twice = units >= 32 ? GKV_MOST_ROWS : pairs ? 768 : 192;
+  c.four_times = units >= 32 ? GKV_MOST_ROWS : pairs ? 4096 : 1024;
   p.most = within(512 / of_one, 1, within(32768 / units, 1, 64));
-  if (units < 32 && p.most < p.soft) p.most = p.soft;
-  if (p.soft > p.most) p.soft = p.most;
+  if (units < 32 && p.most < c.soft) p.most = c.soft;
+  if (c.soft > p.most) c.soft = p.most;
   return p;
 }
 // (whole units need no workspace; 256 bytes so that there is one)
@@ -982,10 +988,10 @@ extern "C" gkv_status gkv_paged_attend_decode(gkv_ctx* ctx, const void* q, const
   if (!workspace || ((uintptr_t)workspace & 15) != 0) return GKV_ERR_WORKSPACE;
   const GkvDims& d = ctx->dims;
   const PagedPlan plan = paged_plan(ctx);
-  const int pieces = gkv_paged_pieces(((int64_t)len_max_host + 15) / 16, plan.iters, plan.soft, plan.long_iters);
+  const int pieces = plan.cut.most((int)(((int64_t)len_max_host + 15) / 16));
   PagedAttendArgs a{q, K, V, {page_table, table_width, page_rows, n_pages, gkv_divisor(page_rows)}, d_len, out, (int32_t*)workspace,
                     (float*)((char*)workspace + paged_tickets_bytes(d, plan)), plan.most,
-                    pieces < 1 ? 1 : pieces < plan.most ? pieces : plan.most, plan.iters, plan.soft, plan.long_iters, len_max_host};
+                    pieces < 1 ? 1 : pieces < plan.most ? pieces : plan.most, plan.cut, len_max_host};
   if ((int64_t)d.L * d.B * d.Hkv * gkv_paged_parts(d.g) * a.splits > GKV_MOST_PIECES) return GKV_ERR_SHAPE;
   GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
   // (the matrix-core kernel counts rows in 32 bits where pages are not whole slices)

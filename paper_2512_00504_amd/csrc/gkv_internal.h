@@ -214,20 +214,31 @@ hipError_t gkv_launch_paged_advance(const GkvLaunch& ln, const GkvDims& dm, int3
 constexpr int GKV_PAGED_TICKET = 32;
 // The matrix-core kernel takes a group's heads 16 at a time.
 constexpr int gkv_paged_parts(int g) { return (g + 15) / 16; }
+// How a unit is cut, by its own n slices of 16 rows alone: `iters` slices a piece, twice and four times as many from `twice` and `four_times` slices on, not
+// more than `soft` pieces; of long_iters slices where those are more.
+struct GkvPagedCut {
+  int32_t iters, twice, four_times, soft, long_iters;
+  constexpr int pieces(int n) const {
+    const int by = iters << ((n >= twice) + (n >= four_times));
+    const int a = (n + by - 1) / by, b = (n + long_iters - 1) / long_iters;
+    return (a < soft ? a : soft) > b ? (a < soft ? a : soft) : b;
+  }
+  // of any unit of up to n slices
+  constexpr int most(int n) const {
+    int x = pieces(n);
+    if (n >= twice && pieces(twice - 1) > x) x = pieces(twice - 1);
+    if (n >= four_times && pieces(four_times - 1) > x) x = pieces(four_times - 1);
+    return x;
+  }
+};
 struct PagedAttendArgs {
   const void* q; const void* K; const void* V; GkvPages pages; const int32_t* len; void* out;
   int32_t* ticket; float* partials;                      // [units][parts][GKV_TICKETS][GKV_PAGED_TICKET]; [units][most][g][d + 2]
   int32_t most;                                          // pieces of a unit that there is room for
   int32_t splits;                                        // pieces that the launch has
-  int32_t split_iters, soft, long_iters;                 // as gkv_paged_pieces has them
+  GkvPagedCut cut;
   int32_t len_max;
 };
-// Pieces of a unit of n slices of 16 rows: of split_iters slices, but not more than `soft`; of long_iters slices where those are more.
-static inline int gkv_paged_pieces(int64_t n, int split_iters, int soft, int long_iters) {
-  int64_t a = (n + split_iters - 1) / split_iters, b = (n + long_iters - 1) / long_iters;
-  if (a > soft) a = soft;
-  return (int)(a > b ? a : b);
-}
 hipError_t gkv_launch_paged_attend_generic(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a, bool aligned);
 hipError_t gkv_launch_paged_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a);
 

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(NWG * 64) void paged_attend_generic_kernel(GkvDims 
   const int64_t room = (int64_t)a.pages.width * pr;
   const int len = (int)min((int64_t)max(a.len[i], 0), room);
   const int n_iter = (len + 15) >> 4;
-  const int ns = max(1, min(a.splits, max(min((n_iter + a.split_iters - 1) / a.split_iters, a.soft), (n_iter + a.long_iters - 1) / a.long_iters)));
+  const int ns = max(1, min(a.splits, a.cut.pieces(n_iter)));
   if (sp >= ns) return;
   const int per = (n_iter + ns - 1) / ns;
   const int n0 = min(len, sp * per * 16), n1 = min(len, (sp + 1) * per * 16);

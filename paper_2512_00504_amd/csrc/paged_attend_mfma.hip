@@ -49,7 +49,8 @@ struct PagedArgs {
   float* partials; int32_t* ticket;
   GkvDivisor by_blocks, by_parts, by_hkv, by_batch, by_iters, by_long, by_page;   // by_page: rows of a page, or slices
   int64_t layer_bytes;                                         // K of a layer
-  int32_t blocks, parts, splits, most, split_iters, soft, long_iters, Hq, Hkv, g, B, width, page_rows, n_pages;
+  GkvPagedCut cut;
+  int32_t blocks, parts, splits, most, Hq, Hkv, g, B, width, page_rows, n_pages;
   float scale_hi, scale_lo;
 };
 
@@ -96,7 +97,10 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
   const Pages pages0 = ask(it_first);
   const int n_tot = max(0, min(held, a.width * page_rows));
   const int n_tiles = (n_tot + 15) >> 4, n_iter = (int)((uint32_t)(n_tot + KEYS - 1) / KEYS);
-  const int ns = max(1, min(a.splits, max(min(quotient(n_tiles + a.split_iters - 1, a.by_iters), a.soft), quotient(n_tiles + a.long_iters - 1, a.by_long))));
+  // (GkvPagedCut::pieces)
+  const int more = (n_tiles >= a.cut.twice) + (n_tiles >= a.cut.four_times);
+  const int by_iters = (quotient(n_tiles + a.cut.iters - 1, a.by_iters) + (1 << more) - 1) >> more;
+  const int ns = max(1, min(a.splits, max(min(by_iters, a.cut.soft), quotient(n_tiles + a.cut.long_iters - 1, a.by_long))));
   if (sp >= ns) return;
   const int it0 = it_first, stride = ns * NW;
 
@@ -309,10 +313,10 @@ hipError_t launch(const GkvLaunch& ln, const GkvDims& dm, const PagedAttendArgs&
   k.q = (const char*)a.q; k.K = (const char*)a.K; k.V = (const char*)a.V; k.out = (char*)a.out;
   k.partials = a.partials; k.ticket = a.ticket;
   k.parts = gkv_paged_parts(dm.g); k.blocks = dm.L * dm.B * dm.Hkv * k.parts;
-  k.by_blocks = gkv_divisor(k.blocks); k.by_parts = gkv_divisor(k.parts); k.by_hkv = dm.by_hkv; k.by_batch = gkv_divisor(dm.B); k.by_iters = gkv_divisor(a.split_iters); k.by_long = gkv_divisor(a.long_iters);
+  k.by_blocks = gkv_divisor(k.blocks); k.by_parts = gkv_divisor(k.parts); k.by_hkv = dm.by_hkv; k.by_batch = gkv_divisor(dm.B); k.by_iters = gkv_divisor(a.cut.iters); k.by_long = gkv_divisor(a.cut.long_iters);
   k.by_page = gkv_divisor(whole ? a.pages.page_rows / 16 : a.pages.page_rows);
   k.layer_bytes = (int64_t)a.pages.n_pages * dm.Hkv * a.pages.page_rows * Geo<T, D>::ROW_BYTES;
-  k.splits = a.splits; k.most = a.most; k.split_iters = a.split_iters; k.soft = a.soft; k.long_iters = a.long_iters;
+  k.splits = a.splits; k.most = a.most; k.cut = a.cut;
   k.Hq = dm.Hq; k.Hkv = dm.Hkv; k.g = dm.g; k.B = dm.B;
   k.width = a.pages.width; k.page_rows = a.pages.page_rows; k.n_pages = a.pages.n_pages;
   k.scale_hi = dm.scale_l2_hi; k.scale_lo = dm.scale_l2_lo;
