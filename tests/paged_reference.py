@@ -51,10 +51,10 @@ def place(lens, starts, t):
 def gathered(pool, table, n):
     """Rows 0 .. n-1 of one sequence and layer, [n, h_kv, d] float64, and which of them are there.  pool [n_pages, h_kv, page_rows, d]."""
     pages, _, rows, _ = pool.shape
-    ids = [int(table[r // rows]) for r in range(n)]
-    ok = torch.tensor([0 <= i < pages for i in ids], dtype=torch.bool)
-    out = torch.stack([pool[i if 0 <= i < pages else 0, :, r % rows] for r, i in enumerate(ids)]) if n else pool.new_zeros(0, pool.shape[1], pool.shape[3])
-    return out.double(), ok
+    row = torch.arange(n)
+    ids = table.long()[row // rows]
+    ok = (ids >= 0) & (ids < pages)
+    return pool[torch.where(ok, ids, torch.zeros_like(ids)), :, row % rows].double(), ok
 
 
 def attended(q, K, V, table, lens, scale, dtype):

@@ -135,6 +135,28 @@ def test_the_bound_of_lengths_does_not_show(dtype, d, page_rows):
     assert all(torch.equal(outs[0], x) for x in outs)
 
 
+@pytest.mark.parametrize("dtype,d,params", [("bf16", 128, None), ("bf16", 64, None), ("f32", 64, None), ("f32", 64, {"force_generic": 1})])
+@pytest.mark.parametrize("lens", [[3050], [3056], [3057], [12272], [12273], [16368], [16369, 100]])
+def test_lengths_where_the_cut_changes(dtype, d, params, lens):
+    # 191, 192, 767, 768, 1023 and 1024 slices of 16 rows, under bounds on either side
+    B = len(lens)
+    ctx = _ctx(1, B, 1, 2, d, dtype, params)
+    gen = torch.Generator().manual_seed(lens[0])
+    n = sum(-(-x // 64) for x in lens)
+    K, V, q = _rows(gen, dtype, 1, n, 1, 64, d), _rows(gen, dtype, 1, n, 1, 64, d), _rows(gen, dtype, 1, B, 2, d)
+    table = _table(gen, lens, 64, n, 320)
+    outs = [_attend(ctx, q, K.cuda(), V.cuda(), table, lens, max(lens[0], bound)) for bound in (0, 3056, 3057, 12273, 16368, 16369, 320 * 64)]
+    assert all(torch.equal(outs[0], x) for x in outs)
+    ref, tol = attended(q, K, V, table, lens, scale_of(d), dtype)
+    assert ((outs[0].cpu().double() - ref).abs() <= tol).all()
+
+
+def test_long_sequences_of_batches():
+    _case("bf16", 128, 3, [9000, 16, 500, 7000, 0, 30, 100, 300, 64], 32, hkv=4, spoil=False)
+    _case("f32", 64, 2, [9000, 16, 500, 2000, 0, 30, 100, 300, 64], 12, hkv=4, spoil=False)
+    _case("bf16", 64, 2, [40, 12000, 700, 33], 20, L=3, hkv=3, spoil=False)
+
+
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
 @pytest.mark.parametrize("page_rows", [16, 12])
 def test_short_sequences_whatever_the_bound(dtype, d, page_rows):
