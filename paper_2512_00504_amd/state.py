@@ -52,7 +52,7 @@ class DecodeState:
         dev = torch.device(device)
         self.device = dev
         z = lambda *s, dtype: torch.zeros(*s, dtype=dtype, device=dev)
-        self._k_turned = None
+        self._k_turned = z(L, B, Hkv, d, dtype=dt)       # the newest keys, where they come not turned by their positions
         self._allocate_cache()
         self.pos = torch.full((L, B, Hkv, cap), -1, dtype=torch.int32, device=dev)
         self.qwin = z(w, L, B, Hq, d, dtype=dt)          # ring of the last w q tensors
@@ -168,9 +168,6 @@ class DecodeState:
     # one call each -------------------------------------------------------------------------
     def _turned(self, q, k_new, step, rotary):
         """q turned by the step into its slot of the window ring, where the decode kernel finds it, and k_new."""
-        if self._k_turned is None:
-            self._k_turned = torch.empty(self.out.shape[0], self.out.shape[1], self.cfg.n_kv_heads, self.cfg.head_dim, dtype=self.out.dtype,
-                                         device=self.device)
         slot, k_turned = self.qwin[step % self.cfg.window], None if k_new is None else self._k_turned
         self.ctx.rotate(q, k_new, None, step, rotary, slot, k_turned)
         return slot, k_turned
