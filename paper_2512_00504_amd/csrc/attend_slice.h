@@ -30,18 +30,22 @@ struct Geo {
   static constexpr int RP = ROW_BYTES / 16;      // 16-byte pieces per row
   static constexpr int NC = D / 16;              // channels per lane, accumulators per lane
   static constexpr int VW = ROW_BYTES / 64;      // 32-bit words of V per lane and key
+  static constexpr int V_BYTES = VW == 8 ? 16 : 4 * VW;   // of a row's bytes from a lane's first on, with VW == 8 twice
   static constexpr int OSTR = D + 4;             // padded LDS row of the per-wave partial outputs
   static constexpr int PSTR = D + 2;             // split partial: o[D], m, l
 };
 
-// V words of one key for lane r: channels [r*NC, +NC), except fp32 at D = 128, whose lanes take 4
-// channels from each half of the row so that both 16-byte loads are contiguous over the lanes.
+// V words of one key for lane r: channels [r*NC, +NC), except rows of 512 bytes, whose lanes take 16
+// bytes from each half of the row so that both loads are contiguous over the lanes.
 template <int VW> struct VWords { uint32_t w[VW]; };
 template <typename T, int D>
 __device__ __forceinline__ void ld_v(VWords<Geo<T, D>::VW>& o, const char* p) {
   if constexpr (Geo<T, D>::VW == 2) {
     const u32x2 a = __builtin_nontemporal_load((const u32x2*)p);
     o.w[0] = a[0]; o.w[1] = a[1];
+  } else if constexpr (Geo<T, D>::VW == 3) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) o.w[i] = __builtin_nontemporal_load((const uint32_t*)p + i);
   } else {
     const u32x4 a = __builtin_nontemporal_load((const u32x4*)p);
 #pragma unroll

@@ -995,7 +995,7 @@ extern "C" gkv_status gkv_paged_attend_decode(gkv_ctx* ctx, const void* q, const
   if ((int64_t)d.L * d.B * d.Hkv * gkv_paged_parts(d.g) * a.splits > GKV_MOST_PIECES) return GKV_ERR_SHAPE;
   GkvLaunch ln{ctx, GKV_K_ATTEND, (hipStream_t)stream};
   // (the matrix-core kernel counts rows in 32 bits where pages are not whole slices)
-  const bool mfma = (d.d == 64 || d.d == 128) && !ctx->force_generic && aligned16({q, K, V, out}) &&
+  const bool mfma = (d.d == 64 || d.d == 128 || (ctx->cfg.dtype == GKV_BF16 && (d.d == 96 || d.d == 256))) && !ctx->force_generic && aligned16({q, K, V, out}) &&
                     (page_rows % 16 == 0 || (int64_t)n_pages * d.Hkv * page_rows <= INT32_MAX);
   return hip_status(mfma ? gkv_launch_paged_attend_mfma(ln, d, ctx->cfg.dtype, a)
                          : gkv_launch_paged_attend_generic(ln, d, ctx->cfg.dtype, a, aligned16({K, V})));

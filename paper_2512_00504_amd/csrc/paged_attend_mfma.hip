@@ -1,4 +1,4 @@
-// Decode attention over pages on the matrix cores: bf16 or fp32, head_dim 64 or 128, groups of any size (16 heads at a time), pages of any size.
+// Decode attention over pages on the matrix cores: bf16, head_dim 64, 96, 128 or 256, or fp32, 64 or 128, groups of any size (16 heads at a time), pages of any size.
 //
 // One workgroup of NW wavefronts per (unit, piece).  A wavefront owns slices of 16 rows of its sequence (slice it, it + pieces*NW, ...) and
 // keeps running maxima, sums and accumulators of up to 16 query heads, so K and V are read once per KV head where g is no more.  Products and softmax are
@@ -40,7 +40,7 @@ __device__ __forceinline__ float over_lanes(float x) {
   return x;
 }
 
-constexpr int pass(int D) { return 1024 / D; }   // heads whose sums go through LDS at a time
+constexpr int pass(int D) { return D <= 64 ? 16 : D <= 128 ? 8 : 4; }   // heads whose sums go through LDS at a time
 
 struct PagedArgs {
   const int32_t *len, *table;
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
     }
     return w;
   };
-  uint32_t k_off = r * ROW_BYTES + kb * 16, v_off = kb * 4 * ROW_BYTES + r * (G::VW == 2 ? 8 : 16);
+  uint32_t k_off = r * ROW_BYTES + kb * 16, v_off = kb * 4 * ROW_BYTES + r * G::V_BYTES;
   asm volatile("" : "+v"(k_off), "+v"(v_off));                 // (offsets stay offsets)
   auto request = [&](Slice<T, D, KT>& s, Place w) {
 #pragma unroll
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if constexpr (WHOLE_SLICES) ld_v<T, D>(s.vR[4 * t + e], V + w.at[t] + v_off + e * ROW_BYTES);
-        else ld_v<T, D>(s.vR[4 * t + e], V + (uint64_t)w.v_row[t][e] * ROW_BYTES + r * (G::VW == 2 ? 8 : 16));
+        else ld_v<T, D>(s.vR[4 * t + e], V + (uint64_t)w.v_row[t][e] * ROW_BYTES + r * G::V_BYTES);
       }
   };
   Running<G::NC> st;
@@ -211,16 +211,20 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
   float* sl = sm + NW * 16;                 // [16][NW]
   const float l_tot = over_head(st.l_run, false);      // the 4 lanes of a head hold partial sums
   if (r < g && kb == 0) { sm[r * NW + wave] = st.m_run; sl[r * NW + wave] = l_tot; }
-  constexpr int TPH = D / 2;                // threads per head: two channels each
+  // threads per head, of CPT channels each (D = 96: some have none)
+  constexpr int TPH = D <= 64 ? 32 : 64, CPT = D <= 128 ? 2 : 4;
+  typedef float Channels __attribute__((ext_vector_type(CPT)));
   T* out = (T*)a.out + head0 * D;
   // of a unit: outputs [most][its g][D], then maximum and sum [its g][most]
   float* part = a.partials + (size_t)unit * a.most * a.g * PSTR + part0 * D;
   float* part_ms = a.partials + (size_t)unit * a.most * a.g * PSTR + (size_t)a.most * a.g * D + (size_t)part0 * a.most * 2;
-  auto finish = [&](int x, float L, f32x2 o) {
+  auto finish = [&](int h, int c, float L, Channels o) {
     bool any = false;
     if (L == 0.f)                                              // seldom: no row, or none with weight
       for (int p = 0; p * page_rows < n_tot; ++p) any |= (uint32_t)table[p] < (uint32_t)n_pages;
-    store_row2(out + (uint32_t)(x * 2), o * inv_sum(L, any, false));
+    o *= inv_sum(L, any, false);
+    if constexpr (CPT == 2) store_row2(out + (uint32_t)(h * D + c), o);
+    else store_row4(out + (uint32_t)(h * D + c), o);
   };
   for (int first = 0; first < g; first += PASS) {
     if (first > 0) __syncthreads();
@@ -228,36 +232,43 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
       float* row = so + (wave * in_pass + r - first) * OSTR;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
+        // neighbouring channels: a lane's are NC from NC (4 kb + e) on, of rows of 512 bytes half as many in either half
+        constexpr int W = G::NC % 4 == 0 ? 4 : 2, SIDE = G::VW == 8 ? G::NC / 2 : G::NC;
+        typedef float Some __attribute__((ext_vector_type(W)));
 #pragma unroll
-        for (int q4 = 0; q4 < G::NC / 4; ++q4) {
-          const int ch = (G::F32 && D == 128) ? 64 * q4 + 4 * (4 * kb + e) : G::NC * (4 * kb + e) + 4 * q4;
-          *(f32x4*)(row + ch) = f32x4{st.oacc[4 * q4][e], st.oacc[4 * q4 + 1][e], st.oacc[4 * q4 + 2][e], st.oacc[4 * q4 + 3][e]};
+        for (int m = 0; m < G::NC; m += W) {
+          Some x;
+#pragma unroll
+          for (int i = 0; i < W; ++i) x[i] = st.oacc[m + i][e];
+          *(Some*)(row + m / SIDE * (D / 2) + SIDE * (4 * kb + e) + m % SIDE) = x;
         }
       }
     }
     __syncthreads();
     for (int x = first * TPH + tid; x < min(g, first + PASS) * TPH; x += NW * 64) {
-      const int h = x / TPH, c = (x % TPH) * 2;
+      const int h = x / TPH, c = (x % TPH) * CPT;
+      if (c >= D) continue;
       float M = GKV_NO_MAX, mw[NW];
 #pragma unroll
       for (int wv = 0; wv < NW; ++wv) M = fmaxf(M, mw[wv] = sm[h * NW + wv]);
       float Lsum = 0.f;
-      f32x2 o = {0.f, 0.f};
+      Channels o = 0.f;
 #pragma unroll
       for (int wv = 0; wv < NW; ++wv) {
         const float f = __builtin_amdgcn_exp2f(mw[wv] - M);
         Lsum += sl[h * NW + wv] * f;
-        o += *(const f32x2*)(so + (wv * in_pass + h - first) * OSTR + c) * f;
+        o += *(const Channels*)(so + (wv * in_pass + h - first) * OSTR + c) * f;
       }
       if (ns == 1) {
-        finish(x, Lsum, o);
+        finish(h, c, Lsum, o);
       } else {
-        store_agent(part + (uint32_t)((sp * a.g + h) * D + c), o[0], o[1]);
+#pragma unroll
+        for (int i = 0; i < CPT; i += 2) store_agent(part + (uint32_t)((sp * a.g + h) * D + c + i), o[i], o[i + 1]);
         if (c == 0) store_agent(part_ms + (uint32_t)((h * a.most + sp) * 2), M, Lsum);
       }
     }
   }
-  if (ns == 1 || wave * 64 >= g * TPH) return;                 // (uniform)
+  if (ns == 1 || wave * 64 >= in_pass * TPH) return;           // (uniform)
 
   // ---- pieces: whoever finishes last joins them -------------------------------------------------
   // A wavefront's outputs are whole heads and need the same heads of the other pieces only: a ticket for each wavefront and no barrier.
@@ -268,39 +279,47 @@ __global__ __launch_bounds__(NW * 64, OCC) void paged_attend_mfma_kernel(PagedAr
     arrived = __builtin_amdgcn_atomic_inc32((uint32_t*)a.ticket + ((size_t)block * GKV_TICKETS + wave) * GKV_PAGED_TICKET, (uint32_t)ns - 1u, __ATOMIC_RELAXED, "agent");
   if ((int)__builtin_amdgcn_readfirstlane(arrived) != ns - 1) return;
   asm volatile("" ::: "memory");
-  // A lane has maximum and sum of one piece and makes its factor, so all outputs can be asked for at once.  A wavefront has one head (D = 128) or two.
-  constexpr int AT_A_TIME = TPH, AT_ONCE = 16;
-  for (int x = tid; x < g * TPH; x += NW * 64) {               // (a pass is a whole number of rounds, so these are the outputs whose parts this wavefront stored)
-    static_assert(PASS * TPH % (NW * 64) == 0);
-    const int h = x / TPH, c = (x % TPH) * 2, in_head = lane % TPH, lane0 = lane - in_head;
-    float M = GKV_NO_MAX, Lsum = 0.f;
-    f32x2 o = {0.f, 0.f};
-    float2 got[AT_ONCE];
-    auto ask_for = [&](int s1) {
+  // A lane has maximum and sum of one piece and makes its factor, so all outputs can be asked for at once.  A wavefront has one head (D > 64) or two.
+  constexpr int AT_A_TIME = TPH, AT_ONCE = 32 / CPT;
+  for (int first = 0; first < g; first += PASS)
+    for (int x = first * TPH + tid; x < min(g, first + PASS) * TPH; x += NW * 64) {   // (the outputs whose parts this wavefront stored)
+      const int h = x / TPH, c = min((x % TPH) * CPT, D - CPT), in_head = lane % TPH, lane0 = lane - in_head;   // (lanes without channels go along)
+      float M = GKV_NO_MAX, Lsum = 0.f;
+      Channels o = 0.f;
+      float2 got[AT_ONCE][CPT / 2];
+      auto ask_for = [&](int s1) {
 #pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i) got[i] = load_agent(part + (uint32_t)((min(s1 + i, ns - 1) * a.g + h) * D + c));
-    };
-    for (int s0 = 0; s0 < ns; s0 += AT_A_TIME) {
-      float2 ms = load_agent(part_ms + (uint32_t)((h * a.most + min(s0 + in_head, ns - 1)) * 2));
-      ask_for(s0);
-      if (s0 + in_head >= ns) ms = make_float2(GKV_NO_MAX, 0.f);
-      const float Mn = fmaxf(M, over_lanes<TPH, true>(ms.x));
-      const float f = __builtin_amdgcn_exp2f(ms.x - Mn), f0 = __builtin_amdgcn_exp2f(M - Mn);
-      M = Mn;
-      Lsum = Lsum * f0 + over_lanes<TPH, false>(ms.y * f);
-      o *= f0;
-      for (int s1 = s0; s1 < min(ns, s0 + AT_A_TIME); s1 += AT_ONCE) {
-        if (s1 > s0) ask_for(s1);
+        for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) {
-          const int from = (s1 + i - s0) & (TPH - 1);
-          const float fi = TPH == 64 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), from)) : __shfl(f, lane0 + from);
-          if (s1 + i < ns) o += f32x2{got[i].x, got[i].y} * fi;
+          for (int k = 0; k < CPT / 2; ++k) got[i][k] = load_agent(part + (uint32_t)((min(s1 + i, ns - 1) * a.g + h) * D + c + 2 * k));
+      };
+      for (int s0 = 0; s0 < ns; s0 += AT_A_TIME) {
+        float2 ms = load_agent(part_ms + (uint32_t)((h * a.most + min(s0 + in_head, ns - 1)) * 2));
+        ask_for(s0);
+        if (s0 + in_head >= ns) ms = make_float2(GKV_NO_MAX, 0.f);
+        const float Mn = fmaxf(M, over_lanes<TPH, true>(ms.x));
+        const float f = __builtin_amdgcn_exp2f(ms.x - Mn), f0 = __builtin_amdgcn_exp2f(M - Mn);
+        M = Mn;
+        Lsum = Lsum * f0 + over_lanes<TPH, false>(ms.y * f);
+        o *= f0;
+        for (int s1 = s0; s1 < min(ns, s0 + AT_A_TIME); s1 += AT_ONCE) {
+          if (s1 > s0) ask_for(s1);
+#pragma unroll
+          for (int i = 0; i < AT_ONCE; ++i) {
+            const int from = (s1 + i - s0) & (TPH - 1);
+            const float fi = TPH == 64 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), from)) : __shfl(f, lane0 + from);
+            if (s1 + i < ns) {
+#pragma unroll
+              for (int k = 0; k < CPT / 2; ++k) {
+                o[2 * k] = fmaf(got[i][k].x, fi, o[2 * k]);
+                o[2 * k + 1] = fmaf(got[i][k].y, fi, o[2 * k + 1]);
+              }
+            }
+          }
         }
       }
+      if ((x % TPH) * CPT < D) finish(h, c, Lsum, o);
     }
-    finish(x, Lsum, o);
-  }
 }
 
 template <typename T, int D, int NW, int KT, int OCC>
@@ -339,5 +358,10 @@ hipError_t by_length(const GkvLaunch& ln, const GkvDims& dm, const PagedAttendAr
 
 hipError_t gkv_launch_paged_attend_mfma(const GkvLaunch& ln, const GkvDims& dm, int dtype, const PagedAttendArgs& a) {
   if (dtype == GKV_F32) return dm.d == 64 ? by_length<float, 64, 1, 4>(ln, dm, a) : by_length<float, 128, 1, 2>(ln, dm, a);
-  return dm.d == 64 ? by_length<uint16_t, 64, 2, 4>(ln, dm, a) : by_length<uint16_t, 128, 1, 4>(ln, dm, a);
+  switch (dm.d) {
+    case 64: return by_length<uint16_t, 64, 2, 4>(ln, dm, a);
+    case 96: return by_length<uint16_t, 96, 1, 4>(ln, dm, a);
+    case 128: return by_length<uint16_t, 128, 1, 4>(ln, dm, a);
+    default: return by_length<uint16_t, 256, 1, 2>(ln, dm, a);
+  }
 }

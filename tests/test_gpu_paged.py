@@ -73,7 +73,7 @@ def _case(dtype, d, g, lens, page_rows, L=1, hkv=2, params=None, seed=0, spoil=T
 
 
 SHAPES = [("bf16", 128, 7), ("bf16", 128, 1), ("bf16", 64, 5), ("f32", 64, 4), ("f32", 128, 2), ("bf16", 128, 16), ("f32", 128, 16), ("bf16", 64, 16),
-          ("bf16", 48, 3), ("f32", 20, 2), ("bf16", 64, 17), ("bf16", 512, 2), ("bf16", 128, 33), ("f32", 64, 20), ("f32", 128, 17), ("bf16", 96, 5), ("f32", 256, 9),
+          ("bf16", 48, 3), ("f32", 20, 2), ("bf16", 64, 17), ("bf16", 512, 2), ("bf16", 128, 33), ("f32", 64, 20), ("f32", 128, 17), ("bf16", 96, 5), ("bf16", 96, 17), ("f32", 256, 9), ("f32", 96, 4), ("bf16", 80, 7), ("bf16", 256, 18),
           ("bf16", 256, 4), ("f32", 100, 1), ("bf16", 8, 6)]
 LENS = [0, 1, 15, 16, 17, 33, 129, 255, 256, 257]
 
@@ -85,8 +85,8 @@ def test_lengths_and_pages(dtype, d, g, page_rows):
 
 
 @pytest.mark.parametrize("page_rows", [16, 12])
-@pytest.mark.parametrize("dtype,d,params", [("bf16", 128, None), ("bf16", 64, None), ("f32", 64, None), ("f32", 128, None), ("bf16", 128, {"force_generic": 1}),
-                                            ("f32", 64, {"force_generic": 1})])
+@pytest.mark.parametrize("dtype,d,params", [("bf16", 128, None), ("bf16", 64, None), ("bf16", 96, None), ("bf16", 256, None), ("f32", 64, None), ("f32", 128, None),
+                                            ("bf16", 128, {"force_generic": 1}), ("f32", 64, {"force_generic": 1})])
 def test_long_sequences_in_pieces(dtype, d, params, page_rows):
     _case(dtype, d, 3, [5000], page_rows, hkv=1, params=params)
     _case(dtype, d, 19, [2600], page_rows, hkv=1, params=params)
@@ -102,7 +102,7 @@ def test_ragged_batch_with_one_long_sequence():
     _case("bf16", 128, 2, [20000] + [(31 * i) % 300 for i in range(70)], 64, hkv=8, spoil=False)
 
 
-@pytest.mark.parametrize("dtype,d,params", [("bf16", 128, None), ("f32", 64, None), ("bf16", 128, {"force_generic": 1})])
+@pytest.mark.parametrize("dtype,d,params", [("bf16", 128, None), ("bf16", 64, None), ("bf16", 256, None), ("f32", 64, None), ("bf16", 128, {"force_generic": 1})])
 @pytest.mark.parametrize("page_rows", [16, 12, 64])
 def test_pages_that_are_not_there(dtype, d, params, page_rows):
     # a hole at the start, in the middle, at the end; all of them; numbers far outside
@@ -157,7 +157,7 @@ def test_long_sequences_of_batches():
     _case("bf16", 64, 2, [40, 12000, 700, 33], 20, L=3, hkv=3, spoil=False)
 
 
-@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("bf16", 96), ("bf16", 256), ("f32", 64), ("f32", 128)])
 @pytest.mark.parametrize("page_rows", [16, 12])
 def test_short_sequences_whatever_the_bound(dtype, d, page_rows):
     # launches of one, four and eight wavefronts a workgroup
@@ -191,7 +191,8 @@ def test_a_bound_that_is_too_low_still_covers_every_row():
         assert ((out.cpu().double() - ref).abs() <= tol).all()
 
 
-@pytest.mark.parametrize("dtype,d,params", [("bf16", 128, None), ("bf16", 64, None), ("f32", 64, None), ("f32", 128, None), ("bf16", 128, {"force_generic": 1})])
+@pytest.mark.parametrize("dtype,d,params", [("bf16", 128, None), ("bf16", 64, None), ("bf16", 96, None), ("bf16", 256, None), ("f32", 64, None), ("f32", 128, None),
+                                            ("bf16", 128, {"force_generic": 1})])
 @pytest.mark.parametrize("page_rows", [16, 12])
 @pytest.mark.parametrize("n", [70, 1500])
 def test_hard_logits_and_values(dtype, d, params, page_rows, n):
@@ -513,6 +514,33 @@ def test_recorded_steps_replay(page_rows, d, dtype):
         assert torch.equal(second, b.attend_decode(*ins))
         assert torch.equal(a.d_len, b.d_len)
     assert a.lengths == b.lengths == a.d_len.tolist()
+
+
+def test_layer_by_layer():
+    # as a program that goes through its layers calls it: lengths are counted once, each layer's pages are a slice of the cache
+    L, B, hkv, g, d, page_rows = 3, 3, 2, 4, 128, 16
+    ctx, rotary = _ctx(1, B, hkv, g, d), Rotary(d)
+    gen = torch.Generator().manual_seed(10)
+    lens, n = [700, 0, 33], 60
+    K, V = _rows(gen, "bf16", L, n, hkv, page_rows, d).cuda(), _rows(gen, "bf16", L, n, hkv, page_rows, d).cuda()
+    table = _table(gen, [x + 20 for x in lens], page_rows, n, 50)
+    d_len, ws = torch.tensor(lens, dtype=torch.int32).cuda(), torch.zeros(ctx.paged_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    for step in range(3):
+        qkv = _rows(gen, "bf16", L, 1, B, hkv * (g + 2), d).cuda()
+        ctx.paged_advance(d_len, None)
+        qs, outs = [], []
+        for l in range(L):
+            q, k, v = qkv[l].split([hkv * g, hkv, hkv], dim=2)
+            qt, out = torch.empty(1, B, hkv * g, d, dtype=torch.bfloat16, device="cuda"), torch.empty(1, B, hkv * g, d, dtype=torch.bfloat16, device="cuda")
+            ctx.paged_append(q, k, v, None, d_len, None, rotary, table.cuda(), K[l:l + 1], V[l:l + 1], qt)
+            ctx.paged_attend_decode(qt, K[l:l + 1], V[l:l + 1], table.cuda(), d_len, 720, out, ws)
+            qs.append(qt.cpu()); outs.append(out.cpu())
+        now = [x + step + 1 for x in lens]
+        assert d_len.tolist() == now
+        ref, tol = turned(qkv[:, 0, :, :hkv * g].cpu(), torch.tensor([x - 1 for x in now]), rotary.freq.cpu(), "half")
+        assert ((torch.cat(qs).double() - ref).abs() <= tol).all()
+        ref, tol = attended(torch.cat(qs), K.cpu(), V.cpu(), table, now, scale_of(d), "bf16")
+        assert ((torch.cat(outs).double() - ref).abs() <= tol).all()
 
 
 def test_calls_on_two_streams_with_a_workspace_each():
