@@ -342,12 +342,18 @@ class PagedDecodeState:
             self.ctx.set_param(name, val)
         L, B, Hq, Hkv, d = cfg.n_layers, cfg.batch, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
         self.device, dt = torch.device(device), _TORCH_DTYPE[cfg.dtype]
+        if max_rows < 1 or page_rows < 1:
+            raise ValueError("gkv: sequences and pages have at least one row")
         width = -(-max_rows // page_rows)
         n_pages = B * width if n_pages is None else n_pages
+        if n_pages < 1 or width * page_rows > 1 << 30:
+            raise ValueError("gkv: a cache has at least one page, and a sequence at most 2^30 rows")
         z = lambda *s, dtype=dt: torch.zeros(*s, dtype=dtype, device=self.device)
         self.K, self.V = z(L, n_pages, Hkv, page_rows, d), z(L, n_pages, Hkv, page_rows, d)
         self.page_table = torch.full((B, width), -1, dtype=torch.int32, device=self.device)
         self.d_len = z(B, dtype=torch.int32)
+        if rotary is not None and (rotary.dim > d or rotary.freq.device != self.d_len.device):
+            raise ValueError(f"gkv: the rotary turns {rotary.dim} of {d} channels on {rotary.freq.device}, the state is on {self.d_len.device}")
         self.out, self.q_turned = z(L, B, Hq, d), z(L, B, Hq, d)
         self.workspace = z(self.ctx.paged_workspace_bytes(), dtype=torch.uint8)
         self._table = torch.full((B, width), -1, dtype=torch.int32)          # host mirror
@@ -418,6 +424,8 @@ class PagedDecodeState:
             raise ValueError(f"gkv: {cfg.batch} counts of {k.shape[1]} tokens are wanted")
         if counts is None and k.shape[1] != cfg.batch:
             raise ValueError(f"gkv: one token for each of {cfg.batch} sequences is wanted")
+        if cfg.n_layers * k.shape[1] >= 1 << 24:
+            raise ValueError(f"gkv: {k.shape[1]} tokens of {cfg.n_layers} layers are too many for one call")
         if self.rotary is None and q is not None:
             raise ValueError("gkv: queries are turned where there is a rotary")
         start = None

@@ -229,3 +229,16 @@ def test_a_refused_call_leaves_the_state_as_it_was():
         with pytest.raises(ValueError):
             call()
         assert (st._len, list(st._pages), len(st._free)) == before[:3] and torch.equal(st.d_len, before[3])
+
+
+def test_a_state_refuses_what_no_call_could_take():
+    make = lambda **kw: PagedDecodeState(P.make_config(1, 2, 4, 2, 64, 64, 8, 16, 96, "f32"), **{**dict(max_rows=40, page_rows=16, device="cpu"), **kw})
+    for kw in (dict(max_rows=0), dict(page_rows=0), dict(n_pages=0), dict(max_rows=(1 << 30) + 1, page_rows=1 << 29, n_pages=1), dict(rotary=P.Rotary(66, device="cpu"))):
+        with pytest.raises(ValueError):
+            make(**kw)
+    # more tokens than a call takes: refused before the sequences grow
+    st = PagedDecodeState(P.make_config(1, 2, 1, 1, 4, 64, 8, 16, 96, "f32"), max_rows=1 << 24, page_rows=1 << 20, n_pages=1, device="cpu")
+    k = torch.zeros(1, 1 << 24, 1, 4)
+    with pytest.raises(ValueError, match="too many"):
+        st.append(k, k, [5, 5])
+    assert st._len == [0, 0] and st._pages == [0, 0]
