@@ -416,7 +416,7 @@ gkv_status gkv_rotary_frequencies(int32_t dim, double base, int32_t scaling, dou
  * output can be given as they are.  q_out, k_out: [L,tokens,heads,d] side by side.  Either of q and k may be NULL, and its output then too.
  * In place (q_out == q) where rows lie side by side; other overlaps are not allowed.
  * positions: device, int32 [tokens], the same in every layer, any value; NULL: `step` for every token (relative to the step base if one is set).
- * q_out may be the ring slot of the step, whose gkv_attend_decode then copies nothing.
+ * q_out may be the ring slot of the step, whose gkv_attend_decode then copies nothing; the query of step - w is gone then, also where that call is refused.
  * transposed = 1: by -a instead of a, which takes the gradient of the outputs to that of the inputs.
  * Rows and strides of whole 16-byte pieces, with dim/2 (interleaved: dim) a whole number of them, are fastest.  L * tokens less than 2^24 (else GKV_ERR_SHAPE). */
 gkv_status gkv_rotate(gkv_ctx* ctx, const void* q, int32_t q_stride, const void* k, int32_t k_stride, int32_t tokens,

@@ -52,7 +52,8 @@ class DecodeState:
         dev = torch.device(device)
         self.device = dev
         z = lambda *s, dtype: torch.zeros(*s, dtype=dtype, device=dev)
-        self._k_turned = z(L, B, Hkv, d, dtype=dt)       # the newest keys, where they come not turned by their positions
+        # the newest queries and keys, where they come not turned by their positions
+        self._q_turned, self._k_turned = z(L, B, Hq, d, dtype=dt), z(L, B, Hkv, d, dtype=dt)
         self._allocate_cache()
         self.pos = torch.full((L, B, Hkv, cap), -1, dtype=torch.int32, device=dev)
         self.qwin = z(w, L, B, Hq, d, dtype=dt)          # ring of the last w q tensors
@@ -167,10 +168,11 @@ class DecodeState:
 
     # one call each -------------------------------------------------------------------------
     def _turned(self, q, k_new, step, rotary):
-        """q turned by the step into its slot of the window ring, where the decode kernel finds it, and k_new."""
-        slot, k_turned = self.qwin[step % self.cfg.window], None if k_new is None else self._k_turned
-        self.ctx.rotate(q, k_new, None, step, rotary, slot, k_turned)
-        return slot, k_turned
+        """q and k_new turned by the step.  Not in the step's slot of the window ring, whose query the next compression still needs where the
+        decode call is refused: that call puts q there."""
+        k_turned = None if k_new is None else self._k_turned
+        self.ctx.rotate(q, k_new, None, step, rotary, self._q_turned, k_turned)
+        return self._q_turned, k_turned
 
     def attend_decode(self, q, k_new, v_new, step, prefix=None, rotary=None):
         """prefix: a SharedPrefix, attended to together with the sequences' own rows.  rotary: a Rotary; q and k_new are not turned yet, `step` is

@@ -1,0 +1,50 @@
+"""Decode states that turn queries and keys themselves: steps that are refused, prompts shared by parts of a batch."""
+import pytest
+import torch
+
+from paper_2512_00504_amd import GkvError, Rotary, make_config
+from paper_2512_00504_amd.state import DecodeState, Q8DecodeState, SharedPrefix
+
+from paged_reference import DT
+
+pytestmark = pytest.mark.gpu
+
+
+def _token(gen, dtype):
+    return [torch.randn(2, 3, h, 64, generator=gen).to(DT[dtype]).cuda() for h in (4, 2, 2)]
+
+
+def _full(cls, dtype):
+    """A state without room for a row more, the rotary and a generator of tokens."""
+    st = cls(make_config(2, 3, 4, 2, 64, 16, 4, 8, 32, dtype))
+    rotary, gen = Rotary(64), torch.Generator().manual_seed(7)
+    for t in range(32):
+        st.attend_decode(*_token(gen, dtype), t, rotary=rotary)
+    return st, rotary, gen
+
+
+@pytest.mark.parametrize("why", ["full", "no values", "values apart", "prefix of another state"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cls", [DecodeState, Q8DecodeState])
+def test_a_refused_step_leaves_the_window_as_it_was(cls, dtype, why):
+    # what the next compression keeps is that of a state which never tried the step
+    a, rotary, gen = _full(cls, dtype)
+    b, _, _ = _full(cls, dtype)
+    q, k, v = _token(gen, dtype)
+    values, prefix = v, None
+    if why == "no values":
+        values = None
+    elif why == "values apart":
+        values = torch.empty(2, 3, 2, 128, dtype=v.dtype, device="cuda")[..., ::2]
+    elif why == "prefix of another state":
+        other = cls(make_config(2, 3, 4, 2, 64, 16, 4, 8, 32, dtype))
+        prefix = SharedPrefix(other, *(torch.zeros(2, 2, 5, 64) for _ in range(2)))
+    with pytest.raises((GkvError, ValueError)):
+        a.attend_decode(q, k, values, 32, prefix=prefix, rotary=rotary)
+    assert torch.equal(a.qwin, b.qwin) and a._len == b._len
+    for st in (a, b):
+        st.evict(31)
+    for x in ("S", "F", "keep_idx", "pos", "d_state", "F_hist"):
+        assert torch.equal(getattr(a, x), getattr(b, x)), x
+    assert torch.equal(a.attend_decode(q, k, v, 32, rotary=rotary), b.attend_decode(q, k, v, 32, rotary=rotary))
+    assert torch.equal(a.qwin, b.qwin)
