@@ -176,7 +176,8 @@ class DecodeState:
 
     def attend_decode(self, q, k_new, v_new, step, prefix=None, rotary=None):
         """prefix: a SharedPrefix, attended to together with the sequences' own rows.  rotary: a Rotary; q and k_new are not turned yet, `step` is
-        their position, and the rows that the cache holds are turned by theirs."""
+        their position, in every sequence, and the rows that the cache and prefixes hold are turned by theirs: row r of a prompt of n rows before the
+        first step t by t - n + r.  With another prefix of the step, its attend() takes the same step and rotary."""
         if rotary is not None:
             q, k_new = self._turned(q, k_new, step, rotary)
         if prefix is None:
@@ -473,13 +474,13 @@ class SharedPrefix:
 
     def __init__(self, state: DecodeState, k, v, first=0, count=None, part=None):
         """part: another SharedPrefix of the same state whose sequences are others: one step then joins both, through
-        attend() of this one and attend_decode(..., prefix=the other)."""
+        attend() of this one and attend_decode(..., prefix=the other); where that has a rotary, attend(q, step=step, rotary=rotary)."""
         dt, cfg = state.qwin.dtype, state.cfg
         if k.dim() != 4 or (k.shape[0], k.shape[1], k.shape[3]) != (cfg.n_layers, cfg.n_kv_heads, cfg.head_dim) or v.shape != k.shape:
             raise ValueError(f"gkv: a prefix's k and v have to be [{cfg.n_layers}, {cfg.n_kv_heads}, rows, {cfg.head_dim}]")
         if part is not None and part.ctx is not state.ctx:
             raise ValueError("gkv: the other prefix is of another state")
-        self.ctx = state.ctx
+        self.ctx, self._q_turned = state.ctx, state._q_turned
         self.K, self.V = k.to(state.device, dt).contiguous(), v.to(state.device, dt).contiguous()
         self.rows, self.first = k.shape[2], first
         self.count = state.cfg.batch - first if count is None else count
@@ -488,8 +489,14 @@ class SharedPrefix:
         if self.part.numel() < need:
             raise ValueError("gkv: make the longer prefix first, its buffer holds the shorter one's pieces too")
 
-    def attend(self, q, state=None):
-        """The newest queries over the prefix; attend_decode() with a prefix does it by itself."""
+    def attend(self, q, state=None, step=None, rotary=None):
+        """The newest queries over the prefix; attend_decode() with a prefix does it by itself.  rotary: a Rotary; q is not turned yet, `step` is
+        its position.  Without one q is taken as it is: turned, where the prefix's keys are."""
         if state is not None and state.ctx is not self.ctx:
             raise ValueError("gkv: the prefix is of another state")
+        if rotary is not None:
+            if step is None:
+                raise ValueError("gkv: a rotary needs the step that queries are turned by")
+            self.ctx.rotate(q, None, None, step, rotary, self._q_turned, None)
+            q = self._q_turned
         self.ctx.prefix_attend(q, self.K, self.V, self.rows, self.rows, self.first, self.count, self.part)

@@ -48,3 +48,27 @@ def test_a_refused_step_leaves_the_window_as_it_was(cls, dtype, why):
         assert torch.equal(getattr(a, x), getattr(b, x)), x
     assert torch.equal(a.attend_decode(q, k, v, 32, rotary=rotary), b.attend_decode(q, k, v, 32, rotary=rotary))
     assert torch.equal(a.qwin, b.qwin)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cls", [DecodeState, Q8DecodeState])
+def test_two_shared_prefixes_of_a_step(cls, dtype):
+    # sequence 0 has one prompt, 1 and 2 another: both turned by the step are both of queries that were turned before
+    a, b = (cls(make_config(2, 3, 4, 2, 64, 16, 4, 8, 32, dtype)) for _ in range(2))
+    rotary, gen, rows = Rotary(64), torch.Generator().manual_seed(5), (33, 20)
+    prompts = [[torch.randn(2, 2, n, 64, generator=gen) for _ in range(2)] for n in rows]
+    first, second = [], []
+    for st in (a, b):
+        first.append(SharedPrefix(st, *prompts[0], first=0, count=1))
+        second.append(SharedPrefix(st, *prompts[1], first=1, count=2, part=first[-1]))
+        st.set_state(0, 40, 0, 0)
+    for t in range(40, 47):
+        q, k, v = _token(gen, dtype)
+        qt, kt = torch.empty_like(q), torch.empty_like(k)
+        b.ctx.rotate(q, k, None, t, rotary, qt, kt)
+        first[0].attend(q, step=t, rotary=rotary)
+        out = a.attend_decode(q, k, v, t, prefix=second[0], rotary=rotary).clone()
+        first[1].attend(qt)
+        assert torch.equal(out, b.attend_decode(qt, kt, v, t, prefix=second[1]))
+    with pytest.raises(ValueError, match="step"):
+        first[0].attend(q, rotary=rotary)
