@@ -463,7 +463,12 @@ class PagedDecodeState:
         return self.attend(q)
 
     def replayed(self, steps=1):
-        """So many decode steps were made by replays of recorded ones that this object does not know of (recording a step counts it once)."""
+        """So many decode steps are made by replays of recorded ones that this object does not know of (recording a step counts it once).
+        Say so before they run: steps beyond the reserved rows are refused, since rows without a page are not stored."""
+        if steps < 0:
+            raise ValueError("gkv: a number of steps is wanted")
+        if steps > self._room:
+            raise ValueError(f"gkv: {steps} steps of {self._room} that there are pages for: reserve() comes first")
         self._grown += steps
         self._room -= steps
 

@@ -1,0 +1,41 @@
+"""What a paged decode state refuses before anything grows: host code only."""
+import pytest
+import torch
+
+import paper_2512_00504_amd as P
+from paper_2512_00504_amd.state import PagedDecodeState
+
+
+def _state(rotary=True, **kw):
+    cfg = P.make_config(1, 2, 4, 2, 64, 64, 8, 16, 96, "f32")
+    return PagedDecodeState(cfg, **{**dict(max_rows=64, page_rows=16, rotary=P.Rotary(64, device="cpu") if rotary else None, device="cpu"), **kw})
+
+
+def _is(st):
+    return st._len, st._room, list(st._pages), sorted(st._free), st.d_len.tolist(), st.page_table.tolist(), st._table.tolist()
+
+
+def _refuses(st, call, match):
+    before = _is(st)
+    with pytest.raises(ValueError, match=match):
+        call()
+    assert _is(st) == before
+
+
+def test_replayed_steps_beyond_the_reserved_rows_are_refused():
+    # their rows would have no page, and a page handed out later would not hold them
+    st = _state()
+    _refuses(st, lambda: st.replayed(1), "reserve")
+    st.reserve([16, 40])
+    st.replayed(10)
+    _refuses(st, lambda: st.replayed(7), "reserve")
+    _refuses(st, lambda: st.replayed(-1), "number")
+    st.replayed(6)
+    assert st.lengths == [16, 16] and st._room == 0
+    _refuses(st, lambda: st.replayed(1), "reserve")
+    st.reserve(33)
+    st.replayed(17)
+    assert st.lengths == [33, 33]
+    st.release(0)
+    st.replayed(15)                                          # (a sequence that takes no part needs no pages)
+    assert st.lengths == [0, 48]
