@@ -332,6 +332,10 @@ class Q8DecodeState(DecodeState):
         self._after_compression()
 
 
+def _recording():
+    return torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing()
+
+
 class PagedDecodeState:
     """Device state of L layers x B sequences whose rows are all kept, in pages: full attention beside the capped caches, or to compare
     with.  Of cfg the shapes, type and scale count.  Pages are handed out as sequences grow and come back with release().
@@ -391,6 +395,8 @@ class PagedDecodeState:
             raise ValueError(f"gkv: a sequence of {max(rows)} rows is longer than {self._table.shape[1]} pages of {self.page_rows}")
         if sum(want) - sum(self._pages) > len(self._free):
             raise ValueError(f"gkv: {sum(want) - sum(self._pages)} pages are needed, {len(self._free)} are free")
+        if _recording():
+            raise ValueError("gkv: pages are not handed out while steps are recorded: reserve() comes first")
         for i, n in enumerate(want):
             for p in range(self._pages[i], n):
                 self._table[i, p] = self._free.pop()
@@ -402,6 +408,8 @@ class PagedDecodeState:
         """Sequence i's pages come back, and it takes no part until append() gives it tokens again."""
         if not 0 <= i < self.cfg.batch:
             raise ValueError(f"gkv: there is no sequence {i}")
+        if _recording():
+            raise ValueError("gkv: a sequence does not leave while steps are recorded")
         self._free += [int(p) for p in self._table[i, :self._pages[i]].flip(0)]
         self._table[i] = -1
         self._pages[i] = 0
@@ -431,6 +439,8 @@ class PagedDecodeState:
             raise ValueError(f"gkv: {k.shape[1]} tokens of {cfg.n_layers} layers are too many for one call")
         if self.rotary is None and q is not None:
             raise ValueError("gkv: queries are turned where there is a rotary")
+        if counts is not None and _recording():
+            raise ValueError("gkv: counts come from the host and are not recorded")
         start = None
         if counts is not None:
             lens = [max(n, 0) + m if m else n for n, m in zip(self._len, counts)]

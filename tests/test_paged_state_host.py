@@ -39,3 +39,24 @@ def test_replayed_steps_beyond_the_reserved_rows_are_refused():
     st.release(0)
     st.replayed(15)                                          # (a sequence that takes no part needs no pages)
     assert st.lengths == [0, 48]
+
+
+def test_pages_are_not_handed_out_while_a_step_is_recorded(monkeypatch):
+    # the table's copy would be part of the recording
+    st = _state()
+    k = torch.zeros(1, 2, 2, 64)
+
+    def recording():
+        for name in ("is_initialized", "is_current_stream_capturing"):
+            monkeypatch.setattr(torch.cuda, name, lambda: True)
+
+    recording()
+    _refuses(st, lambda: st.reserve(1), "record")
+    _refuses(st, lambda: st.append(k, k), "record")
+    _refuses(st, lambda: st.append(k, k, [2, 0]), "record")
+    monkeypatch.undo()
+    st.reserve(20)
+    recording()
+    st.reserve(32)                                           # (there already)
+    _refuses(st, lambda: st.append(k, k, [2, 0]), "record")
+    _refuses(st, lambda: st.release(0), "record")
