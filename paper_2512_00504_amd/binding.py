@@ -11,6 +11,7 @@ There is no other way to the kernels: if libgkv.so is missing, loading raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import warnings
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
@@ -171,6 +172,8 @@ class Rotary:
         values, own = rotary_frequencies(dim, base, scaling, factor, trained_length, low, high)
         self.dim, self.layout = dim, ROTARY_LAYOUT[layout] if isinstance(layout, str) else int(layout)
         self.amplitude = own if amplitude is None else float(amplitude)
+        if not 0 <= self.layout <= 1 or not math.isfinite(self.amplitude):
+            raise ValueError(f"gkv: a rotary's layout is one of {list(ROTARY_LAYOUT)}, its amplitude a finite number")
         self.freq = torch.tensor(values, dtype=torch.float64).to(device) if freq is None else freq.to(device, torch.float64).contiguous()
         if self.freq.shape != (dim // 2,):
             raise ValueError(f"gkv: freq has to be [{dim // 2}]")
@@ -221,6 +224,7 @@ class Context:
         import torch
         self._spec = GkvConfig.from_buffer_copy(cfg)           # as the library has it
         self._spec_at, self._dtype, self._paged_bytes = ctypes.addressof(self._spec), (torch.float32, torch.bfloat16)[cfg.dtype], None
+        self._double = torch.float64
         self._prefix_bytes, self._prefix_rows = {}, -1       # rows -> size of a buffer for them; the most rows asked for
 
     def part(self, sequences: int) -> "Context":
@@ -467,6 +471,14 @@ class Context:
         import torch
         if rotary.freq.dtype is not torch.float64 or rotary.freq.numel() < rotary.dim // 2:
             raise ValueError(f"gkv: frequencies have to be float64 [{rotary.dim // 2}]")
+
+    def _turns(self, rotary, device):
+        """Refuses a rotary that no call takes."""
+        d, dim, f = self._spec.head_dim, rotary.dim, rotary.freq
+        if (dim < 2 or dim % 2 or dim > d or not 0 <= rotary.layout <= 1 or not math.isfinite(rotary.amplitude) or f.dtype is not self._double
+                or f.numel() < dim // 2 or f.device != device or not f.is_contiguous()):
+            raise ValueError(f"gkv: the rotary does not turn {dim} of {d} channels on {device}: layout {rotary.layout}, amplitude {rotary.amplitude}, "
+                             f"frequencies {list(f.shape)} of {f.dtype} on {f.device}")
 
     # Rotary positions: q, k [L, tokens, heads, d], slices of one projection's output too; rotary: a Rotary.
     # Paged cache: K, V [L, n_pages, h_kv, page_rows, d], page_table int32 [B, table_width], d_len int32 [B].

@@ -359,8 +359,8 @@ class PagedDecodeState:
         self.K, self.V = z(L, n_pages, Hkv, page_rows, d), z(L, n_pages, Hkv, page_rows, d)
         self.page_table = torch.full((B, width), -1, dtype=torch.int32, device=self.device)
         self.d_len = z(B, dtype=torch.int32)
-        if rotary is not None and (rotary.dim > d or rotary.freq.device != self.d_len.device):
-            raise ValueError(f"gkv: the rotary turns {rotary.dim} of {d} channels on {rotary.freq.device}, the state is on {self.d_len.device}")
+        if rotary is not None:
+            self.ctx._turns(rotary, self.K.device)
         self.out, self.q_turned = z(L, B, Hq, d), z(L, B, Hq, d)
         self.workspace = z(self.ctx.paged_workspace_bytes(), dtype=torch.uint8)
         self._table = torch.full((B, width), -1, dtype=torch.int32)          # host mirror
@@ -422,15 +422,25 @@ class PagedDecodeState:
         behind the last are padding.  Returns q [L, tokens, h_q, d] turned, in q_out or a new tensor, if it is given."""
         cfg, ctx = self.cfg, self.ctx
         # all that can be wrong is looked at before anything grows
+        if k is None or v is None:
+            raise ValueError("gkv: keys and values are wanted")
+        if q is None and q_out is not None:
+            raise ValueError("gkv: q_out is for queries that are given")
         ctx._heads(k, k.shape[1], cfg.n_kv_heads, "k")
         ctx._heads(v, k.shape[1], cfg.n_kv_heads, "v")
         ctx._heads(q, k.shape[1], cfg.n_q_heads, "q")
         ctx._heads(q_out, k.shape[1], cfg.n_q_heads, "q_out", False)
         ctx._ints(positions, (k.shape[1],), "positions", True)
-        if any(x is not None and x.device != self.K.device for x in (k, v, q, q_out, positions)):
-            raise ValueError(f"gkv: tensors have to be on {self.K.device}")
-        if self.K.is_cuda and self.K.device.index != torch.cuda.current_device():
-            raise ValueError(f"gkv: the state is on {self.K.device}, which is not the current GPU")
+        if positions is not None and not positions.is_contiguous():
+            raise ValueError("gkv: positions must be contiguous")
+        here = self.K.device
+        for x in (k, v, q, q_out, positions):
+            if x is not None and x.device != here:
+                raise ValueError(f"gkv: tensors have to be on {here}")
+        if self.K.is_cuda and here.index != torch.cuda.current_device():
+            raise ValueError(f"gkv: the state is on {here}, which is not the current GPU")
+        if q_out is not None and q_out.data_ptr() == q.data_ptr() and not q.is_contiguous():
+            raise ValueError("gkv: queries that lie apart are not turned in place")
         if counts is not None and (len(counts) != cfg.batch or min(counts) < 0 or sum(counts) > k.shape[1]):
             raise ValueError(f"gkv: {cfg.batch} counts of {k.shape[1]} tokens are wanted")
         if counts is None and k.shape[1] != cfg.batch:
@@ -439,21 +449,22 @@ class PagedDecodeState:
             raise ValueError(f"gkv: {k.shape[1]} tokens of {cfg.n_layers} layers are too many for one call")
         if self.rotary is None and q is not None:
             raise ValueError("gkv: queries are turned where there is a rotary")
+        if self.rotary is not None:
+            ctx._turns(self.rotary, here)
         if counts is not None and _recording():
             raise ValueError("gkv: counts come from the host and are not recorded")
-        start = None
+        start = None if counts is None else torch.tensor([0, *counts], dtype=torch.int32).cumsum(0, dtype=torch.int32).to(self.device)
+        if q is not None and q_out is None:
+            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
         if counts is not None:
             lens = [max(n, 0) + m if m else n for n, m in zip(self._len, counts)]
             self.reserve(lens)
             self._settle(lens)
-            start = torch.tensor([0, *counts], dtype=torch.int32).cumsum(0, dtype=torch.int32).to(self.device)
         else:
             if self._room < 1:
                 self.reserve([n + 1 if n >= 0 else 0 for n in self._len])
             self._grown += 1
             self._room -= 1
-        if q is not None and q_out is None:
-            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
         ctx.paged_advance(self.d_len, start)
         ctx.paged_append(q, k, v, start, self.d_len, positions, self.rotary, self.page_table, self.K, self.V, q_out)
         return q_out

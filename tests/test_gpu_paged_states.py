@@ -30,3 +30,12 @@ def test_a_step_that_needs_pages_is_not_recorded():
     for t in range(3):
         assert torch.equal(a.attend_decode(*ins), b.attend_decode(*ins))
         assert a.lengths == b.lengths == a.d_len.tolist() and torch.equal(a.page_table, b.page_table)
+
+
+def test_queries_that_lie_apart_are_not_turned_in_place():
+    a, = _states(1)
+    q, k, v = _token(torch.Generator().manual_seed(1))
+    both = torch.cat([q, q], dim=2)
+    with pytest.raises(ValueError, match="place"):
+        a.append(k, v, None, both[:, :, :4], None, both.view(-1)[:q.numel()].view(q.shape))
+    assert a.lengths == a.d_len.tolist() == [0, 0, 0] and not any(a._pages)

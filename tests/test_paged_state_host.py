@@ -60,3 +60,26 @@ def test_pages_are_not_handed_out_while_a_step_is_recorded(monkeypatch):
     st.reserve(32)                                           # (there already)
     _refuses(st, lambda: st.append(k, k, [2, 0]), "record")
     _refuses(st, lambda: st.release(0), "record")
+
+
+def test_appends_that_the_call_would_refuse_are_refused_before_the_sequences_grow():
+    q, k = torch.zeros(1, 2, 4, 64), torch.zeros(1, 2, 2, 64)
+    for counts in (None, [1, 1]):
+        st = _state()
+        _refuses(st, lambda: st.append(k, k, counts, None, None, q), "q_out")
+        _refuses(st, lambda: st.append(k, None, counts), "wanted")
+        _refuses(st, lambda: st.append(None, k, counts), "wanted")
+        _refuses(st, lambda: st.append(k, k, counts, q, torch.zeros(4, dtype=torch.int32)[::2]), "contiguous")
+    for name, value in (("layout", 2), ("layout", -1), ("amplitude", float("nan")), ("amplitude", float("inf")), ("dim", 66), ("dim", 63), ("dim", 0),
+                        ("freq", torch.ones(32)), ("freq", torch.ones(31, dtype=torch.float64)), ("freq", torch.ones(64, dtype=torch.float64)[::2]),
+                        ("freq", torch.ones(32, dtype=torch.float64, device="meta"))):
+        st = _state()
+        setattr(st.rotary, name, value)
+        _refuses(st, lambda: st.append(k, k, None, q), "rotary")
+        _refuses(st, lambda: st.append(k, k), "rotary")
+
+
+@pytest.mark.parametrize("kw", [dict(layout=2), dict(layout=-1), dict(amplitude=float("nan")), dict(amplitude=float("inf"))])
+def test_a_rotary_refuses_what_no_call_takes(kw):
+    with pytest.raises(ValueError):
+        P.Rotary(64, device="cpu", **kw)
