@@ -476,7 +476,12 @@ class PagedDecodeState:
 
     def attend_decode(self, q, k_new, v_new, positions=None):
         """One decode step: q [L, B, h_q, d], k_new, v_new [L, B, h_kv, d]."""
+        # (queries that attend() would refuse, before anything grows)
+        if q is None:
+            raise ValueError("gkv: q is wanted")
         self.ctx._heads(q, self.cfg.batch, self.cfg.n_q_heads, "q", self.rotary is not None)
+        if q.device != self.K.device:
+            raise ValueError(f"gkv: tensors have to be on {self.K.device}")
         if self.rotary is None:
             self.append(k_new, v_new)
         else:

@@ -83,3 +83,12 @@ def test_appends_that_the_call_would_refuse_are_refused_before_the_sequences_gro
 def test_a_rotary_refuses_what_no_call_takes(kw):
     with pytest.raises(ValueError):
         P.Rotary(64, device="cpu", **kw)
+
+
+@pytest.mark.parametrize("rotary", [False, True])
+def test_steps_whose_queries_are_refused_leave_the_state_as_it_was(rotary):
+    q, k = torch.zeros(1, 2, 4, 64), torch.zeros(1, 2, 2, 64)
+    st = _state(rotary)
+    _refuses(st, lambda: st.attend_decode(None, k, k), "q")
+    _refuses(st, lambda: st.attend_decode(q.to("meta"), k, k), "device|have to be on")
+    _refuses(st, lambda: st.attend_decode(q.half(), k, k), "q has to be")
