@@ -92,3 +92,22 @@ def test_steps_whose_queries_are_refused_leave_the_state_as_it_was(rotary):
     _refuses(st, lambda: st.attend_decode(None, k, k), "q")
     _refuses(st, lambda: st.attend_decode(q.to("meta"), k, k), "device|have to be on")
     _refuses(st, lambda: st.attend_decode(q.half(), k, k), "q has to be")
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(batch=1, n_q_heads=1, n_kv_heads=1), dict(batch=64, n_q_heads=40, n_kv_heads=8), dict(n_layers=36, batch=64, n_q_heads=40, n_kv_heads=8),
+                                dict(batch=3, n_q_heads=40, n_kv_heads=2, head_dim=256), dict(batch=512, n_q_heads=128, n_kv_heads=1, head_dim=512), dict(batch=20, n_q_heads=33, n_kv_heads=1),
+                                dict(batch=700, n_q_heads=64, n_kv_heads=64, head_dim=64), dict(n_layers=28, batch=1, n_q_heads=28, n_kv_heads=4, dtype="f32")])
+def test_workspace_is_a_line_a_ticket_and_room_for_every_piece(kw):
+    ctx = P.Context(P.make_config(**{**dict(n_layers=1, batch=1, n_q_heads=8, n_kv_heads=2, head_dim=128, budget=64, window=8, interval=16, capacity=96, dtype="bf16"), **kw}))
+    c = ctx.cfg
+    g, of_one = c.n_q_heads // c.n_kv_heads, c.n_layers * c.n_kv_heads
+    units = of_one * c.batch
+    # pieces of a unit: what 512 workgroups of one sequence are, up to 64 and 32768 of all; of few units at least what 256 workgroups of all are, from 8 to 64
+    most = max(1, min(512 // of_one, max(1, min(32768 // units, 64))))
+    if units < 32:
+        most = max(most, min(max(256 // units, 8), 64))
+    up = lambda n: -(-n // 256) * 256
+    # a 128-byte line for each of 8 wavefronts and 16 heads of a unit; outputs, maximum and sum of a piece's heads in 32 bits
+    want = up(128 * 8 * units * -(-g // 16)) + up(4 * units * most * g * (c.head_dim + 2)) if most > 1 else 256
+    assert ctx.paged_workspace_bytes() == want
+    ctx.close()
