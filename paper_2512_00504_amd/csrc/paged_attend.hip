@@ -5,7 +5,8 @@
 // 16-byte pieces, each used for all GB heads; for the values it has CH neighbouring channels of every key.  Wavefronts are joined through LDS,
 // pieces of a unit by the workgroup that finishes last, in their order.
 // Bound: instructions, 2 d GB of the vector ALU a key and lane and as many reads of LDS.  us, one element at a time and one head a wavefront -> so:
-// 8 sequences of 4096 rows, 8 KV heads of 4 heads, fp32, d = 96 531 -> 97 (2.1 TB/s); 32 KV heads of one, bf16, d = 80 728 -> 220 (1.5).
+// 8 sequences of 4096 rows, 8 KV heads of 4 heads, fp32, d = 96 531 -> 97 (201 MB, part of them in the memory-side cache; cold 124, 1.6 TB/s); 32 KV heads
+// of one, bf16, d = 80 728 -> 220 (1.5 TB/s).
 #include "gkv_internal.h"
 
 namespace {

@@ -384,7 +384,8 @@ class PagedDecodeState:
         return [max(n, 0) for n in self._len]
 
     def reserve(self, rows):
-        """Pages for sequences of so many rows (one number, or one for each): steps up to there change the lengths alone and can be recorded."""
+        """Pages for sequences of so many rows (one number, or one for each): steps up to there change the lengths alone and can be recorded.
+        Calls that need pages send the whole table and wait for it, so a growing batch reserves ahead."""
         rows = [rows] * self.cfg.batch if isinstance(rows, int) else list(rows)
         if len(rows) != self.cfg.batch:
             raise ValueError(f"gkv: lengths of {self.cfg.batch} sequences are wanted")
