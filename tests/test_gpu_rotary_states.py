@@ -72,3 +72,49 @@ def test_two_shared_prefixes_of_a_step(cls, dtype):
         assert torch.equal(out, b.attend_decode(qt, kt, v, t, prefix=second[1]))
     with pytest.raises(ValueError, match="step"):
         first[0].attend(q, rotary=rotary)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cls", [DecodeState, Q8DecodeState])
+def test_a_recorded_cycle_with_a_rotary_replays(cls, dtype):
+    # a compression cycle, positions from the step base: each replay against eager steps of another state
+    b, w, s, cycles = 16, 4, 8, 3
+    t0 = b + s
+    ref, st = (cls(make_config(2, 3, 4, 2, 64, b, w, s, 32, dtype)) for _ in range(2))
+    rotary, gen = Rotary(64, scaling="linear", factor=2.0), torch.Generator().manual_seed(3)
+    tokens = [_token(gen, dtype) for _ in range(t0 + cycles * s)]
+
+    def eager(x, lo, hi):
+        outs = []
+        for t in range(lo, hi):
+            outs.append(x.attend_decode(*tokens[t], t, rotary=rotary).clone())
+            if x.is_trigger(t):
+                x.evict(t)
+        return outs
+
+    want = eager(ref, 0, t0 + cycles * s)
+    eager(st, 0, t0)
+    assert st._len == [b] * 3
+    base = torch.tensor([t0], dtype=torch.int32, device="cuda")
+    st.ctx.set_step_base(base)
+    ins = [torch.stack([tok[i] for tok in tokens[t0:t0 + s]]) for i in range(3)]
+    outs = torch.zeros(s, *st.out.shape, dtype=st.out.dtype, device="cuda")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        for i in range(s):
+            outs[i].copy_(st.attend_decode(ins[0][i], ins[1][i], ins[2][i], i, rotary=rotary))
+        st.evict(s - 1)
+        st.ctx.advance_step_base(s)
+    for c in range(cycles):
+        lo = t0 + c * s
+        for i in range(3):
+            ins[i].copy_(torch.stack([tok[i] for tok in tokens[lo:lo + s]]))
+        outs.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i in range(s):
+            assert torch.equal(outs[i], want[lo + i]), (c, i)
+    for name in ("pos", "F_hist", "d_state", "keep_idx", "qwin"):
+        assert torch.equal(getattr(st, name), getattr(ref, name)), name
