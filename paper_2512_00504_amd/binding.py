@@ -11,7 +11,6 @@ There is no other way to the kernels: if libgkv.so is missing, loading raises.
 from __future__ import annotations
 
 import ctypes
-import math
 import os
 import warnings
 from ctypes import POINTER, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
@@ -35,6 +34,7 @@ EXPORTS = [
     "gkv_prefix_bytes", "gkv_prefix_attend", "gkv_attend_decode_prefix",
     "gkv_rotary_frequencies", "gkv_rotate", "gkv_paged_append", "gkv_paged_advance", "gkv_paged_workspace_bytes", "gkv_paged_attend_decode",
 ]
+MOST_F32 = 2.0 ** 128 - 2.0 ** 104
 ROTARY_LAYOUT = {"half": 0, "interleaved": 1}
 ROTARY_SCALING = {"none": 0, "linear": 1, "base": 2, "by_parts": 3, "smooth": 4}
 
@@ -172,8 +172,8 @@ class Rotary:
         values, own = rotary_frequencies(dim, base, scaling, factor, trained_length, low, high)
         self.dim, self.layout = dim, ROTARY_LAYOUT[layout] if isinstance(layout, str) else int(layout)
         self.amplitude = own if amplitude is None else float(amplitude)
-        if not 0 <= self.layout <= 1 or not math.isfinite(self.amplitude):
-            raise ValueError(f"gkv: a rotary's layout is one of {list(ROTARY_LAYOUT)}, its amplitude a finite number")
+        if not 0 <= self.layout <= 1 or not abs(self.amplitude) <= MOST_F32:
+            raise ValueError(f"gkv: a rotary's layout is one of {list(ROTARY_LAYOUT)}, its amplitude a finite number of 32 bits")
         self.freq = torch.tensor(values, dtype=torch.float64).to(device) if freq is None else freq.to(device, torch.float64).contiguous()
         if self.freq.shape != (dim // 2,):
             raise ValueError(f"gkv: freq has to be [{dim // 2}]")
@@ -475,7 +475,7 @@ class Context:
     def _turns(self, rotary, device):
         """Refuses a rotary that no call takes."""
         d, dim, f = self._spec.head_dim, rotary.dim, rotary.freq
-        if (dim < 2 or dim % 2 or dim > d or not 0 <= rotary.layout <= 1 or not math.isfinite(rotary.amplitude) or f.dtype is not self._double
+        if (dim < 2 or dim % 2 or dim > d or not 0 <= rotary.layout <= 1 or not abs(rotary.amplitude) <= MOST_F32 or f.dtype is not self._double
                 or f.numel() < dim // 2 or f.device != device or not f.is_contiguous()):
             raise ValueError(f"gkv: the rotary does not turn {dim} of {d} channels on {device}: layout {rotary.layout}, amplitude {rotary.amplitude}, "
                              f"frequencies {list(f.shape)} of {f.dtype} on {f.device}")

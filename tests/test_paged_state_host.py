@@ -70,7 +70,7 @@ def test_appends_that_the_call_would_refuse_are_refused_before_the_sequences_gro
         _refuses(st, lambda: st.append(k, None, counts), "wanted")
         _refuses(st, lambda: st.append(None, k, counts), "wanted")
         _refuses(st, lambda: st.append(k, k, counts, q, torch.zeros(4, dtype=torch.int32)[::2]), "contiguous")
-    for name, value in (("layout", 2), ("layout", -1), ("amplitude", float("nan")), ("amplitude", float("inf")), ("dim", 66), ("dim", 63), ("dim", 0),
+    for name, value in (("layout", 2), ("layout", -1), ("amplitude", float("nan")), ("amplitude", float("inf")), ("amplitude", -1e39), ("dim", 66), ("dim", 63), ("dim", 0),
                         ("freq", torch.ones(32)), ("freq", torch.ones(31, dtype=torch.float64)), ("freq", torch.ones(64, dtype=torch.float64)[::2]),
                         ("freq", torch.ones(32, dtype=torch.float64, device="meta"))):
         st = _state()
@@ -79,7 +79,7 @@ def test_appends_that_the_call_would_refuse_are_refused_before_the_sequences_gro
         _refuses(st, lambda: st.append(k, k), "rotary")
 
 
-@pytest.mark.parametrize("kw", [dict(layout=2), dict(layout=-1), dict(amplitude=float("nan")), dict(amplitude=float("inf"))])
+@pytest.mark.parametrize("kw", [dict(layout=2), dict(layout=-1), dict(amplitude=float("nan")), dict(amplitude=float("inf")), dict(amplitude=1e39)])
 def test_a_rotary_refuses_what_no_call_takes(kw):
     with pytest.raises(ValueError):
         P.Rotary(64, device="cpu", **kw)
